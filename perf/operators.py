@@ -439,14 +439,15 @@ def _exact_kept(x, codes):
     full = torch.nn.functional.pad(x, (0, -cols % 32)).reshape(rows, -1, 32)
     top = full.abs().max(2, keepdim=True).values
     most = 127.0 if codes == "i8" else 448.0
-    # log2 is off by a rounding at worst: the candidate below or at the wanted power is stepped up where it is too small
-    unit = torch.exp2(torch.floor(torch.log2((top / most).clamp_min(2.0 ** -140))) - 1)
+    # (frexp and ldexp: powers of two to the bit, which the GPU's 64-bit exp2 is not)
+    one = torch.ones_like(top)
+    unit = torch.ldexp(one, torch.frexp((top / most).clamp_min(2.0 ** -140))[1] - 2)
     for _ in range(3):
         unit = torch.where(top > most * unit, 2 * unit, unit)
     unit = unit.clamp_min(2.0 ** -126)
     q = full / unit
     if codes == "e4m3":     # three bits behind the leading one, and a smallest spacing of 2^-9
-        grid = torch.exp2(torch.floor(torch.log2(q.abs().clamp_min(2.0 ** -6))) - 3)
+        grid = torch.ldexp(torch.ones_like(q), torch.frexp(q.abs().clamp_min(2.0 ** -6))[1] - 4)
         q = torch.round(q / grid) * grid
     else:
         q = torch.round(q)
