@@ -249,7 +249,7 @@ def _pack(x, codes):
     else:
         power = torch.where(part > 448 / 512, power - 8, power - 9)
     power = power.clamp_min(-126)[:, :, None]
-    scaled = torch.ldexp(padded, -power)
+    scaled = padded * _pow2(-power)
     if codes == "i8":
         return scaled.round().to(torch.int8), power
     return scaled.to(torch.float8_e4m3fn), power
@@ -257,7 +257,12 @@ def _pack(x, codes):
 
 def _unpack(kept, power, shape):
     rows, cols = shape
-    return torch.ldexp(kept.float(), power).view(rows, -1)[:, :cols]
+    return (kept.float() * _pow2(power)).view(rows, -1)[:, :cols]
+
+
+def _pow2(k):
+    """2^k from its bits (torch's ldexp multiplies by exp2(k), which is not a power of two to the bit everywhere)."""
+    return ((k + 127) << 23).to(torch.int32).view(torch.float32)
 
 
 def _act(act, x):
@@ -439,15 +444,16 @@ def _exact_kept(x, codes):
     full = torch.nn.functional.pad(x, (0, -cols % 32)).reshape(rows, -1, 32)
     top = full.abs().max(2, keepdim=True).values
     most = 127.0 if codes == "i8" else 448.0
-    # (frexp and ldexp: powers of two to the bit, which the GPU's 64-bit exp2 is not)
-    one = torch.ones_like(top)
-    unit = torch.ldexp(one, torch.frexp((top / most).clamp_min(2.0 ** -140))[1] - 2)
+    def pow2(k):            # from its bits: the GPU's 64-bit exp2 is off by a unit in the last place at some whole numbers
+        return ((k.to(torch.int64) + 1023) << 52).view(torch.float64)
+
+    unit = pow2(torch.frexp((top / most).clamp_min(2.0 ** -140))[1] - 2)
     for _ in range(3):
         unit = torch.where(top > most * unit, 2 * unit, unit)
     unit = unit.clamp_min(2.0 ** -126)
     q = full / unit
     if codes == "e4m3":     # three bits behind the leading one, and a smallest spacing of 2^-9
-        grid = torch.ldexp(torch.ones_like(q), torch.frexp(q.abs().clamp_min(2.0 ** -6))[1] - 4)
+        grid = pow2(torch.frexp(q.abs().clamp_min(2.0 ** -6))[1] - 4)
         q = torch.round(q / grid) * grid
     else:
         q = torch.round(q)
