@@ -18,6 +18,9 @@
  *   ewf_run                       launch on the caller's stream              (asynchronous)
  *   ewf_run_static                the same without a caller's workspace      (asynchronous)
  *
+ * Beside the expressions the library has operators of sequence models with kernels of their own
+ * (ewf_layer_norm, ewf_activation, ewf_recurrence and their backward passes, below).
+ *
  * Conventions
  *   - Every function returns 0 (EWF_OK) or a negative ewf_status.  No C++ exception crosses
  *     this boundary.  ewf_last_error() gives a thread-local message for the last failure on
@@ -69,7 +72,11 @@ enum {
 /* Storage types of tensors; value types of scalar nodes are EWF_F32 or EWF_I32 only
  * (float16 is a storage format: it is widened to float32 on load, rounded to nearest even
  * on store; section 3.1.5 of the paper: half-precision storage in the new back-end). */
-typedef enum { EWF_F32 = 0, EWF_F16 = 1, EWF_I32 = 2 } ewf_dtype;
+typedef enum {
+    EWF_F32 = 0, EWF_F16 = 1, EWF_I32 = 2,
+    /* storage of the operator calls below; graphs refuse them (EWF_ETYPE) */
+    EWF_BF16 = 3, EWF_I8 = 4, EWF_E4M3 = 5
+} ewf_dtype;
 
 /* Scalar operations.  Arithmetic needs operands of equal value type; there is no implicit
  * promotion (use ewf_cast).  Comparisons return int32 0/1.  EWF_WHERE(c,a,b) = a if c != 0
@@ -267,6 +274,95 @@ ewf_status ewf_run_call(const ewf_call *call);
  * the loop over a function's nodes in C (section 2.3).  Stops at the first failing call,
  * returns its status and, when `failed` is not NULL, stores its index there. */
 ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *failed);
+
+/* ---- operators of sequence models ----
+ *
+ * Three operators whose kernels are written by hand, beside the expressions above: layer normalisation, activations
+ * whose argument is kept in 8 bits for the backward pass, and a gated linear recurrence over time; each with
+ * its backward pass.  The conventions above hold: tensors are strided views of the caller's device memory, strides in
+ * elements and >= 0, nothing is allocated, synchronised or kept between calls, launches go to the caller's stream (of
+ * the current device) and may be captured into a HIP graph, sums are folded in a fixed order (equal calls give equal
+ * bits), errors are statuses with a text.  A workspace needs no initialisation; calls that may overlap in time must not
+ * share one (that includes two captured graphs).
+ *
+ * An argument structure is zeroed by the caller and filled in: a tensor whose ptr and shape are both NULL is absent.
+ * Tensors are EWF_F32, EWF_F16 or EWF_BF16 as the structure's `dtype` says; arithmetic, sums, statistics and states
+ * are float32.  The last axis of every tensor of full size must be contiguous (stride 1, or extent 1); other axes may
+ * have any strides; a result may lie exactly over the operands that are named, and over nothing else (EWF_EALIAS). */
+
+/* Layer normalisation along the last axis (`cols` elements, 1 .. 2^24) of x, rank ndim 1 .. EWF_MAX_DIMS:
+ *     mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),  n = (x - mean) rstd,  y = n weight + bias
+ * and, with g = dy weight,
+ *     dx = rstd (g - sum g / cols - n sum (g n) / cols),  dweight = sum over rows of dy n,  dbias = sum over rows of dy.
+ * The axes before the last are the rows (fewer than 2^31); where they do not merge into at most two axes
+ * common to all tensors the call is EWF_EUNSUPPORTED.
+ *
+ * ewf_layer_norm reads x and writes y; optional: weight, bias (absent: 1 and 0), mean and rstd (float32, the shape
+ * of x without its last axis) to be written, codes and scales to be written (n in 8 bits, see ewf_activation).
+ * y may lie over x.
+ * ewf_layer_norm_grad reads dy, rstd and either x and mean or codes and scales (which then stand for n), and writes
+ * dx; optional: weight, dweight, dbias.  dx may lie over dy or x.  The gradients of no rows are zero.
+ * weight, bias, dweight and dbias have shape [cols], stride 1 and type param_dtype: dtype or EWF_F32. */
+typedef struct {
+    ewf_tensor x, weight, bias, y, mean, rstd, codes, scales, dy, dx, dweight, dbias;
+    int32_t dtype, param_dtype, code_dtype;   /* ewf_dtype                                  */
+    int32_t ndim;
+    float eps;                /* not negative                                               */
+    int32_t reserved;         /* 0                                                          */
+} ewf_layer_norm_args;
+ewf_status ewf_layer_norm(const ewf_layer_norm_args *a, void *hip_stream);
+/* Bytes of workspace that ewf_layer_norm_grad needs for these tensors (checks the arguments, launches nothing). */
+ewf_status ewf_layer_norm_grad_workspace(const ewf_layer_norm_args *a, size_t *workspace_bytes);
+ewf_status ewf_layer_norm_grad(const ewf_layer_norm_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Activations kept in 8 bits.  Blocks of 32 elements along the last axis (the last block of a row may be shorter) share
+ * a scale 2^k, the smallest with k >= -126 and max |x| <= L 2^k, L = 127 (EWF_I8) or 448 (EWF_E4M3); an element's code
+ * is x 2^-k rounded to nearest, ties to even, as a signed byte or as a float of 4 exponent and 3 mantissa bits; it
+ * stands for code 2^k.  The scale is stored as the byte k + 127.  Both steps are exact but for the one rounding, so codes are
+ * defined to the bit.  A block that holds a NaN or an infinity has scale byte 255 and codes 0, and stands for NaN.
+ * codes has the shape of x, scales that of x with ceil(cols / 32) as its last extent; both are bytes.
+ *
+ * ewf_activation reads x and writes y = act(x) (may lie over x) and codes and scales of x; either may be absent.
+ * ewf_activation_grad reads dy, codes and scales and writes dx = dy act'(x8), x8 what the codes stand for (dx may lie
+ * over dy).  The slope of relu at 0 is 0; gelu is x times the normal distribution function.
+ * ewf_read8 writes x, what codes and scales stand for, rounded to dtype (numbers near the type's largest may round to
+ * an infinity: code 2^k may be the next power of two).  EWF_IDENTITY with y absent keeps a tensor. */
+typedef enum { EWF_IDENTITY = 0, EWF_RELU, EWF_ACT_TANH, EWF_ACT_SIGMOID, EWF_SILU, EWF_GELU, EWF_ACT_COUNT } ewf_act;
+typedef struct {
+    ewf_tensor x, y, codes, scales, dy, dx;
+    int32_t dtype, code_dtype;                /* ewf_dtype                                  */
+    int32_t ndim;
+    int32_t act;              /* ewf_act                                                    */
+} ewf_activation_args;
+ewf_status ewf_activation(const ewf_activation_args *a, void *hip_stream);
+ewf_status ewf_activation_grad(const ewf_activation_args *a, void *hip_stream);
+ewf_status ewf_read8(const ewf_activation_args *a, void *hip_stream);
+
+/* Gated linear recurrence over time, channel by channel, from state h_(-1) = h0 (absent: 0):
+ *     f = sigmoid(u),  i = sigmoid(w), or 1 - f with w absent,  h_t = f_t h_(t-1) + i_t v_t
+ * u, v, w, h have shape [batch, steps, channels] (steps and batch may have any strides: column blocks of one
+ * projection, time-major tensors); h0 and last, the state behind the last step, are float32 [batch, channels]
+ * with contiguous channels.  With one step this is the form for single tokens: last may lie over h0, and the state is
+ * updated in place; h may lie over u, v or w.  lengths (optional): int32 [batch] on the device; steps from
+ * lengths[b] on (taken as 0 or `steps` where it is outside 0 .. steps) do not exist: what the inputs hold there has no
+ * effect, results there are left as they were, and last is the state behind the sequence's own last step.
+ *
+ * ewf_recurrence_grad: with G_t the gradient of h_t through all later steps (G = dh at the last step, plus dlast where
+ * it is given; G_t = dh_t + f_(t+1) G_(t+1)),
+ *     dv = G i,  dw = G v i (1 - i),  du = G h_(t-1) f (1 - f), less G v f (1 - f) with w absent,  dh0 = f_0 G_0
+ * it reads u, v, w, h (as ewf_recurrence stored it), h0, dh, dlast and writes du, dv and dw (present with w), and dh0
+ * (float32, optional).  du, dv and dw may lie over u, v, w or dh, dh0 over dlast.
+ * States and gradients are expected to be finite: an infinite or NaN element makes its channel's later states (earlier
+ * gradients) infinite or NaN and touches no other channel. */
+typedef struct {
+    ewf_tensor u, v, w, h, h0, last, lengths, dh, dlast, du, dv, dw, dh0;
+    int32_t dtype;            /* ewf_dtype                                                  */
+    int32_t reserved;         /* 0                                                          */
+} ewf_recurrence_args;
+ewf_status ewf_recurrence_workspace(const ewf_recurrence_args *a, size_t *workspace_bytes);
+ewf_status ewf_recurrence(const ewf_recurrence_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
+ewf_status ewf_recurrence_grad_workspace(const ewf_recurrence_args *a, size_t *workspace_bytes);
+ewf_status ewf_recurrence_grad(const ewf_recurrence_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 const char *ewf_last_error(void);
 

@@ -54,7 +54,7 @@ static void byte_range(const RawView &v, uint64_t &lo, uint64_t &hi)
 }
 
 // True if no two distinct coordinates of the view address the same element.
-static bool self_disjoint(const RawView &v)
+bool self_disjoint(const RawView &v)
 {
     std::vector<std::pair<int64_t, int64_t>> ds;   // (stride, extent)
     for (int d = 0; d < v.rank; d++) if (v.ext[d] > 1) ds.push_back({v.str[d], v.ext[d]});
@@ -81,7 +81,7 @@ static bool lattice_hit(const std::vector<std::pair<int64_t, int64_t>> &ds, size
     return false;
 }
 
-static bool views_overlap(const RawView &a, const RawView &b)
+bool views_overlap(const RawView &a, const RawView &b)
 {
     // a view without elements overlaps nothing, whatever its pointer
     for (int d = 0; d < a.rank; d++) if (a.ext[d] == 0) return false;
@@ -105,7 +105,7 @@ static bool views_overlap(const RawView &a, const RawView &b)
     return lattice_hit(ds, 0, diff / a.isz);
 }
 
-static bool same_view(const RawView &a, const RawView &b)
+bool same_view(const RawView &a, const RawView &b)
 {
     if (a.addr != b.addr || a.isz != b.isz) return false;
     for (int d = 0; d < a.rank; d++) {

@@ -315,6 +315,9 @@ ewf_status canonicalize(const Exec &e, const ReduceInfo &red, const ewf_tensor *
                         int64_t full_out[kMaxDims], std::vector<RawView> *raw_out = nullptr);
 // Overlap rules between outputs and inputs / other outputs, on the caller's views.
 ewf_status check_aliasing(const std::vector<RawView> &raw, int nin, int nout);
+bool self_disjoint(const RawView &v);
+bool views_overlap(const RawView &a, const RawView &b);
+bool same_view(const RawView &a, const RawView &b);
 // `open_axes` (optional): extents for the axes that no input fixes (otherwise 1).
 ewf_status infer_full_extents(const Graph &g, const ewf_tensor *in, int nin, int64_t full[kMaxDims],
                               const int64_t *open_axes = nullptr);

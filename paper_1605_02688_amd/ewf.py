@@ -33,6 +33,8 @@ OK = 0
 EINVAL, ETYPE, ESHAPE, EALIAS, ECOMPILE, EHIP, ENOMEM, EUNSUPPORTED = -1, -2, -3, -4, -5, -6, -7, -8
 F32, F16, I32 = 0, 1, 2
 DTYPES = {"f32": F32, "f16": F16, "i32": I32}
+BF16, I8, E4M3 = 3, 4, 5          # storage of the operators of sequence models; graphs refuse them
+ACTIVATIONS = {"identity": 0, "relu": 1, "tanh": 2, "sigmoid": 3, "silu": 4, "gelu": 5}
 OPS = {name: i for i, name in enumerate(
     ["add", "sub", "mul", "div", "neg", "abs", "exp", "log", "log1p", "sqrt", "tanh", "sigmoid", "max", "min",
      "pow", "where", "gt", "ge", "lt", "le", "eq", "ne", "expm1", "sqr", "recip"])}
@@ -68,6 +70,23 @@ class ewf_call(ctypes.Structure):
                 ("scalars", ctypes.POINTER(ctypes.c_double)), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t), ("hip_stream", ctypes.c_void_p),
                 ("nin", ctypes.c_int32), ("nout", ctypes.c_int32), ("nscalars", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def _args(name, tensors, numbers):
+    """An operator's argument structure: its tensors, then its numbers (of 32 bits each)."""
+    return type(name, (ctypes.Structure,), {"_fields_": [(t, ewf_tensor) for t in tensors] + numbers})
+
+
+ewf_layer_norm_args = _args(
+    "ewf_layer_norm_args", ("x", "weight", "bias", "y", "mean", "rstd", "codes", "scales", "dy", "dx", "dweight", "dbias"),
+    [("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32), ("code_dtype", ctypes.c_int32), ("ndim", ctypes.c_int32),
+     ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)])
+ewf_activation_args = _args(
+    "ewf_activation_args", ("x", "y", "codes", "scales", "dy", "dx"),
+    [("dtype", ctypes.c_int32), ("code_dtype", ctypes.c_int32), ("ndim", ctypes.c_int32), ("act", ctypes.c_int32)])
+ewf_recurrence_args = _args(
+    "ewf_recurrence_args", ("u", "v", "w", "h", "h0", "last", "lengths", "dh", "dlast", "du", "dv", "dw", "dh0"),
+    [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)])
 
 
 class ewf_plan_info(ctypes.Structure):
@@ -115,6 +134,16 @@ _sigs = {
                               ctypes.POINTER(ewf_tensor), _i32, _vp]),
     "ewf_run_call": (_i32, [ctypes.POINTER(ewf_call)]),
     "ewf_run_sequence": (_i32, [ctypes.POINTER(ewf_call), _i32, ctypes.POINTER(_i32)]),
+    "ewf_layer_norm": (_i32, [ctypes.POINTER(ewf_layer_norm_args), _vp]),
+    "ewf_layer_norm_grad_workspace": (_i32, [ctypes.POINTER(ewf_layer_norm_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "ewf_layer_norm_grad": (_i32, [ctypes.POINTER(ewf_layer_norm_args), _vp, ctypes.c_size_t, _vp]),
+    "ewf_activation": (_i32, [ctypes.POINTER(ewf_activation_args), _vp]),
+    "ewf_activation_grad": (_i32, [ctypes.POINTER(ewf_activation_args), _vp]),
+    "ewf_read8": (_i32, [ctypes.POINTER(ewf_activation_args), _vp]),
+    "ewf_recurrence_workspace": (_i32, [ctypes.POINTER(ewf_recurrence_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "ewf_recurrence": (_i32, [ctypes.POINTER(ewf_recurrence_args), _vp, ctypes.c_size_t, _vp]),
+    "ewf_recurrence_grad_workspace": (_i32, [ctypes.POINTER(ewf_recurrence_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "ewf_recurrence_grad": (_i32, [ctypes.POINTER(ewf_recurrence_args), _vp, ctypes.c_size_t, _vp]),
     "ewf_last_error": (ctypes.c_char_p, []),
     "ewf_debug_graph_count": (_i32, [_vp]),
     "ewf_debug_graph_node": (_i32, [_vp, _i32, ctypes.POINTER(ewf_node_info)]),
@@ -223,10 +252,12 @@ def exec_destroy(e: int) -> None:
 
 @dataclass
 class TensorRef:
-    """A pointer + shape + element strides, for planning without device memory."""
+    """A pointer + shape + element strides, for planning without device memory (the operators of
+    sequence models also ask for the storage type)."""
     ptr: int
     shape: Tuple[int, ...]
     strides: Tuple[int, ...]
+    dtype: Optional[int] = None
 
     def data_ptr(self) -> int:
         return self.ptr
@@ -578,3 +609,247 @@ class CallSequence:
         st = _lib.ewf_run_sequence(self._arr, len(self._calls), ctypes.byref(self._failed))
         if st < 0:
             raise EwfError(st, f"call {self._failed.value}: {last_error()}")
+
+
+# ------------------------------------------------------------------ operators of sequence models
+
+_DTYPE_CODES = {}
+try:
+    _DTYPE_CODES = {torch.float32: F32, torch.float16: F16, torch.int32: I32, torch.bfloat16: BF16, torch.int8: I8,
+                    torch.float8_e4m3fn: E4M3}
+except (NameError, AttributeError):
+    pass
+_NAMES = {F32: "float32", F16: "float16", I32: "int32", BF16: "bfloat16", I8: "int8", E4M3: "float8_e4m3fn"}
+
+
+def _refuse(status: int, message: str):
+    raise EwfError(status, message)
+
+
+def _dtype_of(t, name: str) -> int:
+    code = _DTYPE_CODES.get(t.dtype) if not isinstance(t, TensorRef) else t.dtype
+    if code is None:
+        _refuse(ETYPE, f"{name}: storage type {t.dtype} is not one of the operators'")
+    return code
+
+
+class _Filler:
+    """Fills an operator's argument structure from tensors, keeping what it points to alive."""
+
+    def __init__(self, args):
+        self.args = args
+        self.tensors = []
+        self._keep = []
+        self._device = None
+
+    def tensor(self, name: str, t, ndim: int, required: bool = False) -> bool:
+        if t is None:
+            if required:
+                _refuse(EINVAL, f"{name} is needed")
+            return False
+        shape, strides = tuple(t.shape), tuple(t.stride())
+        if len(shape) != ndim:
+            _refuse(ESHAPE, f"{name}: rank {len(shape)}, expected {ndim}")
+        device = getattr(t, "device", None)
+        if device is not None:
+            if device.type != "cuda":
+                _refuse(EINVAL, f"{name}: not in device memory")
+            if self._device is None:
+                self._device = device
+                if device.index != torch.cuda.current_device():
+                    _refuse(EINVAL, f"{name}: on device {device.index}, the current one is {torch.cuda.current_device()}")
+            elif device != self._device:
+                _refuse(EINVAL, f"{name}: on device {device.index}, other tensors on {self._device.index}")
+        words = (ctypes.c_int64 * max(1, 2 * ndim))(*shape, *strides)
+        rec = getattr(self.args, name)
+        rec.ptr = t.data_ptr()
+        rec.shape = ctypes.cast(words, ctypes.POINTER(ctypes.c_int64))
+        rec.strides = ctypes.cast(ctypes.byref(words, 8 * ndim), ctypes.POINTER(ctypes.c_int64))
+        self._keep.append(words)
+        self.tensors.append(t)
+        return True
+
+    def typed(self, name: str, t, ndim: int, dtype: int, required: bool = False) -> None:
+        if self.tensor(name, t, ndim, required):
+            got = _dtype_of(t, name)
+            if got != dtype:
+                _refuse(ETYPE, f"{name}: {_NAMES[got]}, expected {_NAMES[dtype]}")
+
+    def kept(self, codes, scales, ndim: int) -> None:
+        """codes (int8 or float8_e4m3fn) and scales (bytes)."""
+        if self.tensor("codes", codes, ndim):
+            self.args.code_dtype = _dtype_of(codes, "codes")
+        if self.tensor("scales", scales, ndim) and not isinstance(scales, TensorRef) and scales.dtype != torch.uint8:
+            _refuse(ETYPE, f"scales: {scales.dtype}, expected bytes (uint8)")
+
+
+def _rank(t, name: str) -> int:
+    if t is None:
+        _refuse(EINVAL, f"{name} is needed")
+    return len(t.shape)
+
+
+def _layer_norm(x, weight, bias, y, *, mean=None, rstd=None, eps=1e-5, codes=None, scales=None):
+    f = _Filler(ewf_layer_norm_args())
+    a, nd = f.args, _rank(x, "x")
+    a.ndim, a.dtype, a.eps = nd, _dtype_of(x, "x"), eps
+    some = weight if weight is not None else bias
+    a.param_dtype = a.dtype if some is None else _dtype_of(some, "weight")
+    f.tensor("x", x, nd)
+    f.typed("weight", weight, 1, a.param_dtype)
+    f.typed("bias", bias, 1, a.param_dtype)
+    f.typed("y", y, nd, a.dtype)
+    f.typed("mean", mean, nd - 1, F32)
+    f.typed("rstd", rstd, nd - 1, F32)
+    f.kept(codes, scales, nd)
+    return f
+
+
+def _layer_norm_grad(dy, weight, rstd, dx, *, dweight=None, dbias=None, x=None, mean=None, codes=None, scales=None):
+    f = _Filler(ewf_layer_norm_args())
+    a, nd = f.args, _rank(dy, "dy")
+    a.ndim, a.dtype = nd, _dtype_of(dy, "dy")
+    some = next((t for t in (weight, dweight, dbias) if t is not None), None)
+    a.param_dtype = a.dtype if some is None else _dtype_of(some, "weight")
+    f.tensor("dy", dy, nd)
+    f.typed("weight", weight, 1, a.param_dtype)
+    f.typed("rstd", rstd, nd - 1, F32)
+    f.typed("dx", dx, nd, a.dtype)
+    f.typed("dweight", dweight, 1, a.param_dtype)
+    f.typed("dbias", dbias, 1, a.param_dtype)
+    f.typed("x", x, nd, a.dtype)
+    f.typed("mean", mean, nd - 1, F32)
+    f.kept(codes, scales, nd)
+    return f
+
+
+def _act_code(act: str) -> int:
+    if act not in ACTIVATIONS:
+        _refuse(EINVAL, f"unknown activation {act!r}: one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _activation(act, x, y=None, *, codes=None, scales=None):
+    f = _Filler(ewf_activation_args())
+    a, nd = f.args, _rank(x, "x")
+    a.ndim, a.dtype, a.act = nd, _dtype_of(x, "x"), _act_code(act)
+    f.tensor("x", x, nd)
+    f.typed("y", y, nd, a.dtype)
+    f.kept(codes, scales, nd)
+    return f
+
+
+def _activation_grad(act, dy, dx, *, codes, scales):
+    f = _Filler(ewf_activation_args())
+    a, nd = f.args, _rank(dy, "dy")
+    a.ndim, a.dtype, a.act = nd, _dtype_of(dy, "dy"), _act_code(act)
+    f.tensor("dy", dy, nd)
+    f.typed("dx", dx, nd, a.dtype)
+    f.kept(codes, scales, nd)
+    return f
+
+
+def _keep8(x, codes, scales):
+    return _activation("identity", x, None, codes=codes, scales=scales)
+
+
+def _read8(codes, scales, x):
+    f = _Filler(ewf_activation_args())
+    a, nd = f.args, _rank(x, "x")
+    a.ndim, a.dtype = nd, _dtype_of(x, "x")
+    f.tensor("x", x, nd)
+    f.kept(codes, scales, nd)
+    return f
+
+
+def _recurrence(u, v, h, *, w=None, h0=None, last=None, lengths=None):
+    f = _Filler(ewf_recurrence_args())
+    a = f.args
+    _rank(u, "u")
+    a.dtype = _dtype_of(u, "u")
+    f.tensor("u", u, 3)
+    for name, t in (("v", v), ("h", h), ("w", w)):
+        f.typed(name, t, 3, a.dtype)
+    f.typed("h0", h0, 2, F32)
+    f.typed("last", last, 2, F32)
+    f.typed("lengths", lengths, 1, I32)
+    return f
+
+
+def _recurrence_grad(u, v, h, dh, du, dv, *, w=None, dw=None, h0=None, dh0=None, dlast=None, lengths=None):
+    f = _recurrence(u, v, h, w=w, h0=h0, lengths=lengths)
+    for name, t in (("dh", dh), ("du", du), ("dv", dv), ("dw", dw)):
+        f.typed(name, t, 3, f.args.dtype)
+    f.typed("dh0", dh0, 2, F32)
+    f.typed("dlast", dlast, 2, F32)
+    return f
+
+
+class BoundOperator:
+    """An operator's call with its argument structure prepared once (see ``Operator.bind``).  Keeps the
+    tensors alive."""
+
+    def __init__(self, operator: "Operator", filler: _Filler, workspace=None, stream: int = 0):
+        self._keep = (filler, workspace)
+        self._ref = ctypes.byref(filler.args)
+        self._fn = operator._fn
+        self._with_workspace = operator._ws is not None
+        self._ws = workspace.data_ptr() if workspace is not None else None
+        self._ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+        self._stream = stream or None
+
+    def launch(self, stream: Optional[int] = None) -> None:
+        """Launches on `stream`, or on the stream that the call was bound to."""
+        s = self._stream if stream is None else (stream or None)
+        st = self._fn(self._ref, self._ws, self._ws_bytes, s) if self._with_workspace else self._fn(self._ref, s)
+        if st < 0:
+            raise EwfError(st, last_error())
+
+
+class Operator:
+    """One of the C ABI's operators of sequence models, called with tensors::
+
+        ewf.layer_norm(x, weight, bias, y, mean=m, rstd=r, stream=s)
+
+    Results are written into the caller's tensors; ``workspace`` is a tensor of at least
+    ``workspace_bytes(...)`` bytes (operators without one need none).  ``bind(...)`` marshals the arguments
+    once; its ``launch()`` is then a single call of the library."""
+
+    def __init__(self, name: str, fill, workspace: bool, doc: str):
+        self.name, self._fill, self.__doc__ = name, fill, doc
+        self._fn = getattr(_lib, name)
+        self._ws = getattr(_lib, name + "_workspace") if workspace else None
+
+    def workspace_bytes(self, *args, **kw) -> int:
+        f = self._fill(*args, **kw)
+        if self._ws is None:
+            return 0
+        n = ctypes.c_size_t()
+        _check(self._ws(ctypes.byref(f.args), ctypes.byref(n)))
+        return n.value
+
+    def bind(self, *args, workspace=None, stream: int = 0, **kw) -> BoundOperator:
+        return BoundOperator(self, self._fill(*args, **kw), workspace, stream)
+
+    def __call__(self, *args, workspace=None, stream: int = 0, **kw) -> None:
+        self.bind(*args, workspace=workspace, stream=stream, **kw).launch()
+
+
+layer_norm = Operator("ewf_layer_norm", _layer_norm, False, """layer_norm(x, weight, bias, y, *, mean=None, rstd=None, eps=1e-5,
+codes=None, scales=None, stream=0): y = (x - mean) rstd weight + bias along the last axis.  weight and bias may be
+None; mean, rstd (float32) and the normalised rows in 8 bits (codes, scales) are written where given.""")
+layer_norm_grad = Operator("ewf_layer_norm_grad", _layer_norm_grad, True, """layer_norm_grad(dy, weight, rstd, dx, *, dweight=None,
+dbias=None, x=None, mean=None, codes=None, scales=None, workspace=None, stream=0): the backward pass, from x and mean or from the
+normalised rows in 8 bits.""")
+activation = Operator("ewf_activation", _activation, False, """activation(act, x, y=None, *, codes=None, scales=None, stream=0): y = act(x),
+and x in 8 bits for the backward pass.  act: one of ACTIVATIONS.""")
+activation_grad = Operator("ewf_activation_grad", _activation_grad, False, """activation_grad(act, dy, dx, *, codes, scales, stream=0):
+dx = dy act'(x), x as its 8 bits have it.""")
+keep8 = Operator("ewf_activation", _keep8, False, """keep8(x, codes, scales, stream=0): x in 8 bits (int8 or float8_e4m3fn codes, a byte
+for the power of two of each 32 elements along the last axis).""")
+read8 = Operator("ewf_read8", _read8, False, """read8(codes, scales, x, stream=0): writes what 8 bits stand for into x.""")
+recurrence = Operator("ewf_recurrence", _recurrence, True, """recurrence(u, v, h, *, w=None, h0=None, last=None, lengths=None,
+workspace=None, stream=0): h_t = f_t h_(t-1) + i_t v_t over axis 1 of [batch, steps, channels], f = sigmoid(u), i = sigmoid(w) or
+1 - f; h0 and last are the float32 states before the first step and behind the last.""")
+recurrence_grad = Operator("ewf_recurrence_grad", _recurrence_grad, True, """recurrence_grad(u, v, h, dh, du, dv, *, w=None, dw=None,
+h0=None, dh0=None, dlast=None, lengths=None, workspace=None, stream=0): the backward pass of recurrence, which stored h.""")

@@ -1,0 +1,516 @@
+"""The operators of sequence models on the GPU against the formulas in 64 bits (tests/operators_ref.py, which also
+derives the bounds): sizes around every row shape and tile, strides, masks of lengths, values that are not finite, calls in
+place, on other streams and in captured graphs."""
+import pytest
+import torch
+
+import tests.operators_ref as ref
+from paper_1605_02688_amd import ewf
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+CODES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def say(*words):
+    print("[case]", *words, flush=True)
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape, mean=0.0, std=1.0, dtype=torch.float32):
+    return (torch.randn(shape, generator=g, device="cuda") * std + mean).to(dtype)
+
+
+def work_for(op, *args, **kw):
+    n = op.workspace_bytes(*args, **kw)
+    return torch.full((n,), 0xAB, dtype=torch.uint8, device="cuda") if n else None
+
+
+def run(op, *args, **kw):
+    op(*args, workspace=work_for(op, *args, **kw), stream=stream(), **kw)
+
+
+# ------------------------------------------------------------------ layer normalisation
+
+# each side of: one vector, the threads of a row with one, two and four vectors, whole and cut vectors
+NORM_COLS = (1, 2, 3, 7, 8, 9, 31, 32, 33, 64, 100, 128, 129, 256, 257, 300, 512, 513, 1000, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8199,
+             16384, 16390, 32768, 32771, 40005)
+
+
+def norm_case(g, rows, cols, dtype, params):
+    x = randn(g, rows, cols, mean=0.3, std=1.7, dtype=dtype)
+    pt = dtype if params == "own" else torch.float32
+    w, b = (None, None) if params == "none" else (randn(g, cols, mean=1, std=0.3, dtype=pt), randn(g, cols, std=0.3, dtype=pt))
+    return x, w, b, pt
+
+
+def check_norm(x, w, b, y, mean, rstd, eps=1e-5):
+    want = ref.layer_norm(x, w, b, eps, y.dtype)
+    ref.close("y", y, want["y"], want["e_y"])
+    if mean is not None:
+        ref.close("mean", mean, want["mean"], want["e_mean"])
+        ref.close("rstd", rstd, want["rstd"], want["e_rstd"])
+    return want
+
+
+def check_norm_grad(dy, x, w, mean, rstd, dx, dw, db, pt, n=None):
+    if n is None:
+        n = (x.double() - mean.double().unsqueeze(-1)) * rstd.double().unsqueeze(-1)
+        e_n = 2 * ref.U * n.abs()
+    else:
+        e_n = 0.0
+    want = ref.layer_norm_grad(dy, w, n, rstd, e_n, dx.dtype, pt)
+    ref.close("dx", dx.reshape(want["dx"].shape), want["dx"], want["e_dx"])
+    if dw is not None:
+        ref.close("dweight", dw, want["dw"], want["e_dw"])
+        ref.close("dbias", db, want["db"], want["e_db"])
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("cols", NORM_COLS)
+def test_layer_norm_and_its_gradient(dtype, cols):
+    dt = DT[dtype]
+    for rows, params in ((1, "own"), (5, "f32"), (67, "none") if cols < 9000 else (3, "none")):
+        say("layer norm", dtype, rows, cols, params)
+        g = gen(cols * 7 + rows)
+        x, w, b, pt = norm_case(g, rows, cols, dt, params)
+        y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        run(ewf.layer_norm, x, w, b, y, mean=mean, rstd=rstd)
+        check_norm(x, w, b, y, mean, rstd)
+        dy = randn(g, rows, cols, dtype=dt)
+        dx, dw, db = torch.empty_like(x), torch.empty(cols, dtype=pt, device="cuda"), torch.empty(cols, dtype=pt, device="cuda")
+        run(ewf.layer_norm_grad, dy, w, rstd, dx, x=x, mean=mean, dweight=dw, dbias=db)
+        check_norm_grad(dy, x, w, mean, rstd, dx, dw, db, pt)
+
+
+@pytest.mark.parametrize("dtype,rows,cols", (("bf16", 4099, 1001), ("f16", 20011, 72), ("f32", 3001, 260), ("bf16", 1500, 4096), ("f32", 66000, 8),
+                                             ("f16", 700, 16392)))
+def test_layer_norm_gradient_over_many_rows(dtype, rows, cols):
+    say("layer norm gradient", dtype, rows, cols)
+    dt, g = DT[dtype], gen(3)
+    x, w, b, pt = norm_case(g, rows, cols, dt, "f32")
+    dy, dx = randn(g, rows, cols, dtype=dt), torch.empty_like(x)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    run(ewf.layer_norm, x, w, b, y, mean=mean, rstd=rstd)
+    check_norm(x, w, b, y, mean, rstd)
+    dw, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    run(ewf.layer_norm_grad, dy, w, rstd, dx, x=x, mean=mean, dweight=dw, dbias=db)
+    check_norm_grad(dy, x, w, mean, rstd, dx, dw, db, pt)
+    again = [torch.empty_like(t) for t in (dx, dw, db)]
+    run(ewf.layer_norm_grad, dy, w, rstd, again[0], x=x, mean=mean, dweight=again[1], dbias=again[2])
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dw, db)))
+    only = torch.empty(cols, device="cuda")
+    run(ewf.layer_norm_grad, dy, w, rstd, dx, x=x, mean=mean, dbias=only)
+    assert torch.equal(only, db)
+
+
+def test_layer_norm_far_from_zero_and_without_spread():
+    # a mean a thousand deviations away, one element that dwarfs its row, rows of one value
+    g = gen(5)
+    for cols in (33, 1000, 4096, 20000):
+        x = randn(g, 6, cols, mean=1000.0)
+        x[1] = 3.0
+        x[2, cols // 2] = 1e6
+        x[3] = 0.0
+        y, mean, rstd = torch.empty_like(x), torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+        run(ewf.layer_norm, x, None, None, y, mean=mean, rstd=rstd)
+        check_norm(x, None, None, y, mean, rstd)
+
+
+def test_layer_norm_of_rows_that_are_not_finite():
+    x = torch.randn(4, 1000, device="cuda")
+    x[1, 7] = float("nan")
+    x[2, 999] = float("inf")
+    y = torch.empty_like(x)
+    run(ewf.layer_norm, x, None, None, y)
+    assert torch.isnan(y[1]).all() and torch.isnan(y[2, 999]) and torch.isfinite(y[0]).all() and torch.isfinite(y[3]).all()
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_layer_norm_strides_and_in_place(dtype):
+    dt, g = DT[dtype], gen(6)
+    for cols in (40, 129, 1000):
+        say("strides", dtype, cols)
+        wide = randn(g, 5, 6, 2 * cols + 3, dtype=dt)
+        x = wide[:, :, 1:cols + 1]                                   # rows that begin at odd elements
+        xt = x.transpose(0, 1)                                       # [6, 5, cols]: two axes
+        w, b = randn(g, cols), randn(g, cols)
+        out = torch.full((6, 5, cols + 5), 7.0, dtype=dt, device="cuda")
+        y = out[:, :, 2:cols + 2]
+        stats = torch.full((6, 10), 7.0, device="cuda")
+        mean, rstd = stats[:, :5], stats[:, 5:]
+        run(ewf.layer_norm, xt, w, b, y, mean=mean, rstd=rstd)
+        check_norm(xt, w, b, y, mean, rstd)
+        assert (out[:, :, :2] == 7).all() and (out[:, :, cols + 2:] == 7).all()
+        dy, dx = randn(g, 6, 5, cols, dtype=dt), torch.empty(6, 5, cols, dtype=dt, device="cuda")
+        dw, db = torch.empty_like(w), torch.empty_like(b)
+        run(ewf.layer_norm_grad, dy, w, rstd, dx, x=xt, mean=mean, dweight=dw, dbias=db)
+        check_norm_grad(dy, xt, w, mean.contiguous(), rstd.contiguous(), dx, dw, db, torch.float32)
+        # a gradient that is the same for every row; over dy, over x; y over x; one row alone
+        same = randn(g, cols, dtype=dt).expand(6, 5, cols)
+        run(ewf.layer_norm_grad, same, w, rstd, dx, x=xt, mean=mean, dweight=dw, dbias=db)
+        check_norm_grad(same, xt, w, mean.contiguous(), rstd.contiguous(), dx, dw, db, torch.float32)
+        for over in ("dy", "x"):
+            d, xx = dy.clone(), xt.contiguous()
+            run(ewf.layer_norm_grad, dy, w, rstd, dx, x=xx, mean=mean, dweight=dw, dbias=db)
+            target = d if over == "dy" else xx
+            ow, ob = torch.empty_like(w), torch.empty_like(b)
+            run(ewf.layer_norm_grad, d, w, rstd, target, x=xx, mean=mean, dweight=ow, dbias=ob)
+            assert torch.equal(target, dx) and torch.equal(ow, dw) and torch.equal(ob, db)
+        xx, yy = xt.contiguous(), torch.empty(6, 5, cols, dtype=dt, device="cuda")
+        run(ewf.layer_norm, xx, w, b, yy)
+        run(ewf.layer_norm, xx, w, b, xx)
+        assert torch.equal(xx, yy)
+        one = x[0, 0]
+        y1, m1, r1 = torch.empty(cols, dtype=dt, device="cuda"), torch.empty((), device="cuda"), torch.empty((), device="cuda")
+        run(ewf.layer_norm, one, w, b, y1, mean=m1, rstd=r1)
+        check_norm(one, w, b, y1, m1, r1)
+
+
+def test_layer_norm_gradient_in_place_on_long_rows():
+    g = gen(8)
+    x, dy = randn(g, 3, 40005), randn(g, 3, 40005)
+    mean, rstd = x.mean(1), torch.rsqrt(x.var(1, correction=0) + 1e-5)
+    dx, dw, db = torch.empty_like(x), torch.empty(40005, device="cuda"), torch.empty(40005, device="cuda")
+    run(ewf.layer_norm_grad, dy, None, rstd, dx, x=x, mean=mean, dweight=dw, dbias=db)
+    ow, ob = torch.empty_like(dw), torch.empty_like(db)
+    run(ewf.layer_norm_grad, dy, None, rstd, x, x=x, mean=mean, dweight=ow, dbias=ob)
+    assert torch.equal(x, dx) and torch.equal(ow, dw) and torch.equal(ob, db)
+
+
+def test_layer_norm_of_no_rows():
+    x = torch.empty(0, 40, device="cuda")
+    dw, db = torch.full((40,), 3.0, device="cuda"), torch.full((40,), 3.0, device="cuda")
+    run(ewf.layer_norm, x, None, None, x)
+    run(ewf.layer_norm_grad, x, None, torch.empty(0, device="cuda"), torch.empty_like(x), x=torch.empty_like(x),
+        mean=torch.empty(0, device="cuda"), dweight=dw, dbias=db)
+    assert (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("kind", sorted(CODES))
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_layer_norm_kept_in_8_bits(dtype, kind):
+    dt = DT[dtype]
+    for rows, cols in ((1, 1), (3, 7), (5, 33), (130, 64), (9, 1001), (6, 2048), (3, 4097), (2, 16400), (2, 40005)):
+        say("kept", dtype, kind, rows, cols)
+        g = gen(cols + rows)
+        x, w, b, pt = norm_case(g, rows, cols, dt, "own")
+        y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        codes = torch.empty((rows, cols), dtype=CODES[kind], device="cuda")
+        scales = torch.full((rows, (cols + 31) // 32), 99, dtype=torch.uint8, device="cuda")
+        run(ewf.layer_norm, x, w, b, y, mean=mean, rstd=rstd, codes=codes, scales=scales)
+        want = check_norm(x, w, b, y, mean, rstd)
+        n8 = torch.empty((rows, cols), device="cuda")
+        run(ewf.read8, codes, scales, n8)
+        # within half a step of the grid at n, and what n itself is off by.  The block's unit may be the next power where its
+        # largest element is within that of the border; the grid's steps are then twice as wide
+        _, byte, _, unit = ref.keep8(want["n"], kind)
+        step = unit if kind == "i8" else unit * ref.e4m3_step(want["n"] / unit)
+        exact_unit = (byte == scales).all()
+        ref.close("n", n8, want["n"], (0.5 if exact_unit else 1.0) * step * (1 + 1e-6) + 2 * want["e_n"] + (step if kind == "e4m3" else 0) * 1e-3)
+        assert ((scales.int() - byte.int()).abs() <= 1).all()
+        dy, dx = randn(g, rows, cols, dtype=dt), torch.empty_like(x)
+        dw, db = torch.empty(cols, dtype=pt, device="cuda"), torch.empty(cols, dtype=pt, device="cuda")
+        run(ewf.layer_norm_grad, dy, w, rstd, dx, codes=codes, scales=scales, dweight=dw, dbias=db)
+        check_norm_grad(dy, None, w, None, rstd, dx, dw, db, pt, n=n8)
+
+
+# ------------------------------------------------------------------ activations in 8 bits
+
+def special_values(dt):
+    if dt == torch.float32:
+        x = torch.tensor([0.0, -0.0, 1e-45, -1e-40, 2.0 ** -126, 3.4e38, -3.4e38, 1.0, 127.0, 127.0000076, 448.0, 449.0, 1e-30])
+        return x.cuda()
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
+    x = bits.view(dt).cuda()
+    return x[torch.isfinite(x)]
+
+
+@pytest.mark.parametrize("kind", sorted(CODES))
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_codes_to_the_bit(dtype, kind):
+    dt, g = DT[dtype], gen(11)
+    v = special_values(dt)
+    cases = {"values": v[: v.numel() // 32 * 32].reshape(-1, 32) if v.numel() >= 64 else v[None],
+             # every value alone beside a magnitude that sets the block's power
+             "random": randn(g, 200, 1003, std=3, dtype=dt), "wide": (randn(g, 64, 96) * torch.exp2(randn(g, 64, 96, std=12 if dtype != "f16" else 3))).to(dt),
+             "one": randn(g, 3, 1, dtype=dt), "short": randn(g, 70, 31, dtype=dt), "ties": (torch.arange(-508, 509, device="cuda") / 4).to(dt)[None].repeat(3, 1),
+             "grid": torch.cat((torch.arange(-1792, 1793, device="cuda") / 4, torch.arange(-64, 65, device="cuda") / 2048)).to(dt)[None]}
+    for name, x in cases.items():
+        say("codes", dtype, kind, name, tuple(x.shape))
+        rows, cols = x.shape
+        codes = torch.empty((rows, cols), dtype=CODES[kind], device="cuda")
+        scales = torch.full((rows, (cols + 31) // 32), 99, dtype=torch.uint8, device="cuda")
+        ewf.keep8(x, codes, scales, stream=stream())
+        code, byte, value, _ = ref.keep8(x, kind)
+        assert torch.equal(scales, byte)
+        assert torch.equal(codes.float().double(), code)
+        back = torch.empty((rows, cols), device="cuda")
+        ewf.read8(codes, scales, back, stream=stream())
+        assert torch.equal(back, value.float())              # (2^128, which the largest floats round to, is an infinity)
+        own = torch.empty_like(x)
+        ewf.read8(codes, scales, own, stream=stream())
+        assert torch.equal(own, back.to(dt))
+
+
+@pytest.mark.parametrize("kind", sorted(CODES))
+def test_blocks_that_are_not_finite(kind):
+    x = torch.randn(4, 100, device="cuda")
+    x[0, 40] = float("nan")
+    x[1, 0] = float("inf")
+    x[3, 99] = -float("inf")
+    codes = torch.empty((4, 100), dtype=CODES[kind], device="cuda")
+    scales = torch.empty((4, 4), dtype=torch.uint8, device="cuda")
+    ewf.keep8(x, codes, scales, stream=stream())
+    code, byte, value, _ = ref.keep8(x, kind)
+    assert torch.equal(scales, byte) and torch.equal(codes.float().double(), code)
+    back = torch.empty_like(x)
+    ewf.read8(codes, scales, back, stream=stream())
+    assert torch.equal(torch.isnan(back), torch.isnan(value)) and int(torch.isnan(back).sum()) == 32 + 32 + 4
+    for act in ewf.ACTIVATIONS:
+        dx = torch.empty_like(x)
+        ewf.activation_grad(act, torch.ones_like(x), dx, codes=codes, scales=scales, stream=stream())
+        assert torch.equal(torch.isnan(dx), torch.isnan(value)), act
+
+
+@pytest.mark.parametrize("act", sorted(ewf.ACTIVATIONS))
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_activation_and_its_gradient(dtype, act):
+    dt, g = DT[dtype], gen(13)
+    value, slope = ref.ACTS[act]
+    for kind, rows, cols in (("i8", 1, 1), ("e4m3", 1, 8), ("i8", 65, 33), ("e4m3", 7, 1000), ("i8", 129, 1003), ("e4m3", 64, 4096), ("i8", 2, 100001)):
+        say("activation", act, dtype, kind, rows, cols)
+        x, dy = randn(g, rows, cols, std=3, dtype=dt), randn(g, rows, cols, dtype=dt)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        codes = torch.empty((rows, cols), dtype=CODES[kind], device="cuda")
+        scales = torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device="cuda")
+        ewf.activation(act, x, y, codes=codes, scales=scales, stream=stream())
+        ev, _ = ref.act_bounds(act, x.double())
+        want = value(x.double())
+        ref.close("y", y, want, ref.stored(ev, want, dt))
+        _, byte, x8, _ = ref.keep8(x, kind)
+        assert torch.equal(scales, byte)
+        ewf.activation_grad(act, dy, dx, codes=codes, scales=scales, stream=stream())
+        _, es = ref.act_bounds(act, x8)
+        want = dy.double() * slope(x8)
+        ref.close("dx", dx, want, ref.stored(dy.double().abs() * es + ref.U * want.abs(), want, dt))
+        only = torch.empty_like(x)
+        ewf.activation(act, x, only, stream=stream())
+        assert torch.equal(only, y)
+        ewf.activation(act, x, x, stream=stream())                  # in place
+        assert torch.equal(x, y)
+        ewf.activation_grad(act, dy, dy, codes=codes, scales=scales, stream=stream())
+        assert torch.equal(dy, dx)
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_activation_strides(dtype):
+    dt, g = DT[dtype], gen(14)
+    x = randn(g, 5, 6, 150, dtype=dt)[:, :, 3:104].transpose(0, 1)   # [6, 5, 101], rows at odd elements
+    out = torch.full((6, 5, 110), 7.0, dtype=dt, device="cuda")
+    box = torch.zeros((6, 5, 107), dtype=torch.int8, device="cuda")
+    y, codes = out[:, :, 4:105], box[:, :, 1:102]
+    scales = torch.zeros((5, 6, 4), dtype=torch.uint8, device="cuda").transpose(0, 1)
+    ewf.activation("silu", x, y, codes=codes, scales=scales, stream=stream())
+    code, byte, x8, _ = ref.keep8(x, "i8")
+    assert torch.equal(scales, byte) and torch.equal(codes.double(), code)
+    assert (out[:, :, :4] == 7).all() and (out[:, :, 105:] == 7).all() and (box[:, :, 0] == 0).all() and (box[:, :, 102:] == 0).all()
+    dx = torch.empty(6, 5, 101, dtype=dt, device="cuda")
+    dy = randn(g, 101, dtype=dt).expand(6, 5, 101)
+    ewf.activation_grad("silu", dy, dx, codes=codes, scales=scales, stream=stream())
+    _, es = ref.act_bounds("silu", x8)
+    want = dy.double() * ref.ACTS["silu"][1](x8)
+    ref.close("dx", dx, want, ref.stored(dy.double().abs() * es + ref.U * want.abs(), want, dt))
+
+
+# ------------------------------------------------------------------ recurrence
+
+def rec_case(g, B, T, D, dt, tied, lengths):
+    c = dict(u=randn(g, B, T, D, mean=1.0, std=2.0, dtype=dt), v=randn(g, B, T, D, dtype=dt), w=None if tied else randn(g, B, T, D, dtype=dt),
+             h0=randn(g, B, D), lengths=None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    return c
+
+
+def rec_forward(c, h=None, last=None):
+    h = torch.full_like(c["u"], 7.0) if h is None else h
+    last = torch.full((c["u"].shape[0], c["u"].shape[2]), 7.0, device="cuda") if last is None else last
+    run(ewf.recurrence, c["u"], c["v"], h, w=c["w"], h0=c["h0"], last=last, lengths=c["lengths"])
+    return h, last
+
+
+def check_rec(c, h, last):
+    want = ref.recurrence(c["u"], c["v"], c["w"], c["h0"], c["lengths"], c["u"].dtype)
+    on = want["valid"]
+    ref.close("h", torch.where(on, h.double(), 0.0), torch.where(on, want["h"], 0.0), want["e_h"])
+    ref.close("last", last, want["last"], want["e_last"])
+    return on
+
+
+def rec_backward(c, h, dh, dlast, dh0=None):
+    d = {k: torch.full_like(c["u"], 7.0) for k in ("du", "dv", "dw")}
+    if c["w"] is None:
+        d["dw"] = None
+    d["dh0"] = torch.full((c["u"].shape[0], c["u"].shape[2]), 7.0, device="cuda")
+    run(ewf.recurrence_grad, c["u"], c["v"], h, dh, d["du"], d["dv"], w=c["w"], dw=d["dw"], h0=c["h0"], dh0=d["dh0"], dlast=dlast,
+        lengths=c["lengths"])
+    return d
+
+
+def check_rec_grad(c, h, dh, dlast, d):
+    want = ref.recurrence_grad(c["u"], c["v"], c["w"], h, c["h0"], dh, dlast, c["lengths"], c["u"].dtype)
+    on = want["valid"]
+    for k in ("du", "dv", "dw"):
+        if d[k] is not None:
+            ref.close(k, torch.where(on, d[k].double(), 0.0), torch.where(on, want[k], 0.0), want["e_" + k])
+            assert (d[k][~on] == 7).all(), k
+    ref.close("dh0", d["dh0"], want["dh0"], want["e_dh0"])
+
+
+REC_SHAPES = ((1, 1, 1), (3, 1, 2), (2, 2, 3), (64, 1, 300), (2, 16, 65), (3, 17, 1), (2, 17, 2), (1, 63, 64), (2, 64, 63), (1, 65, 130), (3, 127, 5),
+              (2, 128, 64), (1, 129, 66), (2, 200, 129), (1, 256, 7), (1, 257, 128), (5, 300, 40), (1, 1500, 67), (2, 2049, 192))
+
+
+@pytest.mark.parametrize("tied", (True, False))
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("B,T,D", REC_SHAPES)
+def test_recurrence_and_its_gradient(B, T, D, dtype, tied):
+    dt, g = DT[dtype], gen(B + T + D)
+    lens = [None]
+    if B > 1:
+        lens.append([(T * k) // (B - 1) for k in range(B)])          # from none to all
+    for lengths in lens:
+        say("recurrence", B, T, D, dtype, "tied" if tied else "gated", lengths)
+        c = rec_case(g, B, T, D, dt, tied, lengths)
+        h, last = rec_forward(c)
+        on = check_rec(c, h, last)
+        assert (h[~on] == 7).all()
+        dh, dlast = randn(g, B, T, D, dtype=dt), randn(g, B, D)
+        check_rec_grad(c, h, dh, dlast, rec_backward(c, h, dh, dlast))
+        # nothing given that may be absent
+        c["h0"] = None
+        h, last = rec_forward(c)
+        check_rec(c, h, last)
+        d = rec_backward(c, h, dh, None)
+        check_rec_grad(c, h, dh, None, d)
+
+
+@pytest.mark.parametrize("T", (3, 40, 700))
+def test_recurrence_lengths_out_of_range_and_what_lies_behind(T):
+    g = gen(T)
+    c = rec_case(g, 5, T, 70, torch.bfloat16, False, [-3, T + 9, 0, T // 2, 1])
+    clean = dict(c)
+    h, last = rec_forward(c)
+    on = check_rec(c, h, last)
+    dh, dlast = randn(g, 5, T, 70, dtype=torch.bfloat16), randn(g, 5, 70)
+    d = rec_backward(c, h, dh, dlast)
+    check_rec_grad(c, h, dh, dlast, d)
+    # what the inputs hold behind a sequence has no effect
+    for bad in (float("nan"), float("inf"), -float("inf"), torch.finfo(torch.bfloat16).min):
+        for k in ("u", "v", "w"):
+            clean[k] = torch.where(on, c[k], torch.full_like(c[k], bad))
+        h2, last2 = rec_forward(clean)
+        assert torch.equal(h2, h) and torch.equal(last2, last)
+        d2 = rec_backward(clean, torch.where(on, h, bad), torch.where(on, dh, bad), dlast)
+        assert all(torch.equal(d2[k], d[k]) for k in d), bad
+
+
+def test_recurrence_gates_at_their_ends():
+    # a shut gate forgets, an open one keeps, through hundreds of steps
+    B, T, D = 1, 400, 64
+    u = torch.full((B, T, D), 200.0, device="cuda")
+    u[0, 100] = -200.0
+    u[0, 300] = -float("inf")
+    v = torch.randn(B, T, D, device="cuda")
+    h, last = torch.empty_like(u), torch.empty(B, D, device="cuda")
+    h0 = torch.randn(B, D, device="cuda")
+    run(ewf.recurrence, u, v, h, h0=h0, last=last)
+    assert torch.equal(h[0, 0:100], h0.expand(100, D))
+    assert torch.equal(h[0, 100:300], v[0, 100].expand(200, D)) and torch.equal(h[0, 300:], v[0, 300].expand(100, D))
+    assert torch.equal(last[0], v[0, 300])
+
+
+@pytest.mark.parametrize("T", (5, 333))
+def test_recurrence_keeps_what_is_not_finite_in_its_channel(T):
+    g = gen(20 + T)
+    c = rec_case(g, 2, T, 66, torch.float32, True, None)
+    h, last = rec_forward(c)
+    c["v"][1, T // 2, 65] = float("nan")
+    c["v"][0, 1, 3] = float("inf")
+    h2, last2 = rec_forward(c)
+    touched = torch.zeros_like(h, dtype=torch.bool)
+    touched[1, T // 2:, 65] = True
+    touched[0, 1:, 3] = True
+    assert torch.equal(h2[~touched], h[~touched]) and not torch.isfinite(h2[touched]).any()
+    assert torch.isnan(last2[1, 65]) and not torch.isfinite(last2[0, 3])
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("T", (1, 7, 150))
+def test_recurrence_strides_and_in_place(dtype, T):
+    dt, g = DT[dtype], gen(30 + T)
+    for D in (1, 33, 64, 130):
+        say("strides", dtype, T, D)
+        B = 3
+        # time-major column blocks of one projection, each beginning at any element
+        p = randn(g, T, B, 3 * D + 1, dtype=dt)
+        blocks = [p[:, :, 1 + k * D:1 + (k + 1) * D].transpose(0, 1) for k in range(3)]
+        state = randn(g, B, D + 3)
+        c = dict(u=blocks[0], v=blocks[1], w=blocks[2], h0=state[:, 2:D + 2], lengths=torch.tensor([[T, 9], [T // 2, 9], [T, 9]], dtype=torch.int32, device="cuda")[:, 0])
+        keep = p.clone()
+        out = torch.full((T, B, D + 2), 7.0, dtype=dt, device="cuda")
+        h = out[:, :, 1:D + 1].transpose(0, 1)
+        h, last = rec_forward(c, h=h)
+        on = check_rec(c, h, last)
+        assert torch.equal(p, keep) and (out[:, :, 0] == 7).all() and (out[:, :, D + 1] == 7).all() and (h[~on] == 7).all()
+        dh, dlast = randn(g, B, T, D, dtype=dt), randn(g, B, D)
+        d = rec_backward(c, h, dh, dlast)
+        check_rec_grad(c, h, dh, dlast, d)
+        # gradients as column blocks over the operands themselves
+        dlast2 = dlast.clone()
+        saved = [b.clone() for b in blocks]
+        run(ewf.recurrence_grad, blocks[0], blocks[1], h, dh, blocks[0], blocks[1], w=blocks[2], dw=blocks[2], h0=c["h0"], dh0=dlast2, dlast=dlast2,
+            lengths=c["lengths"])
+        for k, b, s in zip(("du", "dv", "dw"), blocks, saved):
+            assert torch.equal(b[on], d[k][on]) and torch.equal(b[~on], s[~on])
+        assert torch.equal(dlast2, d["dh0"])
+        # forward over each operand, the state in place
+        p.copy_(keep)
+        for k in ("u", "v", "w"):
+            p.copy_(keep)
+            s = state[:, 2:D + 2].clone()
+            c2 = dict(c, h0=s)
+            rec_forward(c2, h=c2[k], last=s)
+            assert torch.equal(c2[k][on], h[on]) and torch.equal(s, last)
+        p.copy_(keep)
+
+
+def test_recurrence_step_by_step_is_the_whole():
+    g = gen(41)
+    c = rec_case(g, 4, 30, 100, torch.float32, False, None)
+    h, last = rec_forward(c)
+    s = c["h0"].clone()
+    steps = torch.empty_like(h)
+    for t in range(30):
+        sl = lambda x: x[:, t:t + 1]
+        run(ewf.recurrence, sl(c["u"]), sl(c["v"]), sl(steps), w=sl(c["w"]), h0=s, last=s)
+    want = ref.recurrence(c["u"], c["v"], c["w"], c["h0"], None, torch.float32)
+    ref.close("h", steps, want["h"], want["e_h"])
+    ref.close("last", s, want["last"], want["e_last"])
+
+
+def test_recurrence_of_no_steps():
+    u = torch.empty(2, 0, 5, device="cuda")
+    h0, last = torch.randn(2, 5, device="cuda"), torch.empty(2, 5, device="cuda")
+    run(ewf.recurrence, u, torch.empty_like(u), torch.empty_like(u), h0=h0, last=last)
+    assert torch.equal(last, h0)
+    dh0 = torch.empty(2, 5, device="cuda")
+    run(ewf.recurrence_grad, u, torch.empty_like(u), torch.empty_like(u), torch.empty_like(u), torch.empty_like(u), torch.empty_like(u),
+        dlast=h0, dh0=dh0)
+    assert torch.equal(dh0, h0)

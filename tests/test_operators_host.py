@@ -1,0 +1,237 @@
+"""The operators of sequence models without a GPU: their formulas against differences, and what the library refuses.
+Checks come before any launch; a workspace query makes them all and launches nothing, and calls that must be refused are
+made on made-up addresses."""
+import pytest
+import torch
+
+import tests.operators_ref as ref
+from paper_1605_02688_amd import ewf
+
+F32, F16, BF16, I8, E4M3, I32 = ewf.F32, ewf.F16, ewf.BF16, ewf.I8, ewf.E4M3, ewf.I32
+_next = [0x7E0000000000]
+
+
+def contig(shape):
+    st, acc = [], 1
+    for e in reversed(shape):
+        st.append(acc)
+        acc *= e
+    return tuple(reversed(st))
+
+
+def T(shape, dtype=BF16, strides=None, at=None, off=0):
+    """A tensor at an address of its own, 64 GiB from any other."""
+    if at is None:
+        _next[0] += 1 << 36
+        at = _next[0]
+    return ewf.TensorRef(at + off, tuple(shape), tuple(strides) if strides is not None else contig(shape), dtype)
+
+
+def refused(status, words, fn, *args, **kw):
+    with pytest.raises(ewf.EwfError) as e:
+        fn(*args, **kw)
+    assert e.value.status == status, e.value
+    assert words in e.value.message, e.value
+
+
+# ------------------------------------------------------------------ the formulas against differences
+
+def _differences(f, x, h=1e-6):
+    g = torch.zeros_like(x)
+    for k in range(x.numel()):
+        lo, hi = x.clone(), x.clone()
+        lo.view(-1)[k] -= h
+        hi.view(-1)[k] += h
+        g.view(-1)[k] = (f(hi) - f(lo)) / (2 * h)
+    return g
+
+
+def test_layer_norm_formula_is_the_gradient():
+    g = torch.Generator().manual_seed(1)
+    x, dy = torch.randn(3, 7, generator=g, dtype=torch.float64), torch.randn(3, 7, generator=g, dtype=torch.float64)
+    w, b = torch.randn(7, generator=g, dtype=torch.float64), torch.randn(7, generator=g, dtype=torch.float64)
+    out = ref.layer_norm(x, w, b, 1e-5, torch.float32)
+    got = ref.layer_norm_grad(dy, w, out["n"], out["rstd"], 0.0, torch.float32, torch.float32)
+    value = lambda x, w, b: float((ref.layer_norm(x, w, b, 1e-5, torch.float32)["y"] * dy).sum())
+    for name, d in (("dx", _differences(lambda t: value(t, w, b), x)), ("dw", _differences(lambda t: value(x, t, b), w)),
+                    ("db", _differences(lambda t: value(x, w, t), b))):
+        assert torch.allclose(got[name], d, rtol=1e-6, atol=1e-7), name
+
+
+@pytest.mark.parametrize("tied", (True, False))
+@pytest.mark.parametrize("lengths", (None, (4, 0, 2)))
+def test_recurrence_formula_is_the_gradient(tied, lengths):
+    g = torch.Generator().manual_seed(2)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)
+    u, v, w, h0, dh, dlast = r(3, 4, 2), r(3, 4, 2), None if tied else r(3, 4, 2), r(3, 2), r(3, 4, 2), r(3, 2)
+    n = None if lengths is None else torch.tensor(lengths)
+    def value(u, v, w, h0):
+        o = ref.recurrence(u, v, w, h0, n, torch.float32)
+        return float((torch.where(o["valid"], o["h"], 0.0) * dh).sum() + (o["last"] * dlast).sum())
+    h = ref.recurrence(u, v, w, h0, n, torch.float32)["h"]
+    got = ref.recurrence_grad(u, v, w, h, h0, dh, dlast, n, torch.float32)
+    live = got["valid"]
+    checks = [("du", _differences(lambda t: value(t, v, w, h0), u)), ("dv", _differences(lambda t: value(u, t, w, h0), v))]
+    if not tied:
+        checks.append(("dw", _differences(lambda t: value(u, v, t, h0), w)))
+    for name, d in checks:
+        assert torch.allclose(torch.where(live, got[name], 0.0), d, rtol=1e-6, atol=1e-7), name
+    assert torch.allclose(got["dh0"], _differences(lambda t: value(u, v, w, t), h0), rtol=1e-6, atol=1e-7)
+
+
+@pytest.mark.parametrize("act", sorted(ref.ACTS))
+def test_slopes_are_the_gradients(act):
+    x = torch.linspace(-6, 6, 41, dtype=torch.float64) + 0.01
+    value, slope = ref.ACTS[act]
+    assert torch.allclose(slope(x), (value(x + 1e-6) - value(x - 1e-6)) / 2e-6, rtol=1e-6, atol=1e-8)
+
+
+def test_codes_of_known_blocks():
+    x = torch.zeros(1, 64)
+    x[0, :4] = torch.tensor([127.0, 0.5, 1.5, -2.5])          # unit 1: ties go to even
+    x[0, 32:36] = torch.tensor([127.01, 1.0, -3.0, 5.0])      # unit 2
+    code, byte, value, _ = ref.keep8(x, "i8")
+    assert byte.tolist() == [[127, 128]]
+    assert code[0, :4].tolist() == [127, 0, 2, -2] and code[0, 32:36].tolist() == [64, 0, -2, 2]
+    assert value[0, 32].item() == 128
+    code, byte, value, _ = ref.keep8(torch.tensor([[448.0, 17.0, 2.0 ** -10, 19.0]]), "e4m3")
+    assert byte.tolist() == [[127]] and code.tolist() == [[448, 16, 0, 20]]
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_graphs_refuse_the_operators_types():
+    for storage in (BF16, I8, E4M3):
+        g = ewf.graph_create(1)
+        refused(ewf.ETYPE, "storage", ewf.input, g, storage, [0])
+        x = ewf.input(g, F32, [0])
+        refused(ewf.ETYPE, "storage", ewf.output, g, x, storage)
+        ewf.graph_destroy(g)
+
+
+def test_layer_norm_refusals():
+    x, y, w, st = T((6, 40)), T((6, 40)), T((40,), F32), T((6,), F32)
+    ln = ewf.layer_norm
+    refused(ewf.EINVAL, "y is needed", ln, x, w, w, None)
+    refused(ewf.ESHAPE, "extent", ln, x, T((41,), F32), None, y)
+    refused(ewf.ESHAPE, "rank", ln, x, T((1, 40), F32), None, y)
+    refused(ewf.ETYPE, "bfloat16", ln, x, None, None, T((6, 40), F16))
+    refused(ewf.ETYPE, "parameters", ln, x, T((40,), F16), None, y)          # parameters: the tensors' type or float32
+    refused(ewf.ETYPE, "float32", ln, x, None, None, y, mean=T((6,), F16))
+    refused(ewf.ETYPE, "float32", ln, T((6, 40), I32), None, None, T((6, 40), I32))
+    refused(ewf.EUNSUPPORTED, "contiguous", ln, T((6, 40), strides=(1, 6)), None, None, y)
+    refused(ewf.EUNSUPPORTED, "contiguous", ln, x, T((40,), F32, strides=(0,)), None, y)
+    refused(ewf.EINVAL, "eps", ln, x, None, None, y, eps=-1.0)
+    refused(ewf.EINVAL, "eps", ln, x, None, None, y, eps=float("nan"))
+    refused(ewf.EINVAL, "null pointer", ln, T((6, 40), at=0), None, None, y)
+    refused(ewf.EINVAL, "aligned", ln, T((6, 40), off=1), None, None, y)
+    refused(ewf.EINVAL, "come together", ln, x, None, None, y, codes=T((6, 40), I8))
+    refused(ewf.ETYPE, "codes", ln, x, None, None, y, codes=T((6, 40), F16), scales=T((6, 2), I8))
+    refused(ewf.ESHAPE, "scales", ln, x, None, None, y, codes=T((6, 40), I8), scales=T((6, 1), I8))
+    refused(ewf.ESHAPE, "1 to 2^24", ln, T((6, 0)), None, None, T((6, 0)))
+    refused(ewf.EINVAL, "rank", ln, T(()), None, None, T(()))
+    # results over operands
+    refused(ewf.EALIAS, "y overlaps x", ln, x, None, None, ewf.TensorRef(x.ptr + 2, x.shape, x.strides, BF16))
+    refused(ewf.EALIAS, "overlaps", ln, x, w, None, y, mean=T((6,), F32, at=w.ptr))
+    refused(ewf.EALIAS, "share memory", ln, x, None, None, T((6, 40), strides=(0, 1)))
+    # three axes that no two replace
+    a, b = T((3, 4, 5, 8)), T((3, 4, 5, 8), strides=(4000, 8, 400, 1))
+    refused(ewf.EUNSUPPORTED, "merge", ln, a, None, None, b)
+    assert ewf.layer_norm.workspace_bytes(x, w, w, y, mean=st) == 0
+
+
+def test_layer_norm_grad_refusals_and_workspace():
+    dy, dx, x, w, st, dw = T((6, 40)), T((6, 40)), T((6, 40)), T((40,), F32), T((6,), F32), T((40,), F32)
+    codes, scales = T((6, 40), I8), T((6, 2), I8)
+    q = ewf.layer_norm_grad.workspace_bytes
+    assert q(dy, w, st, dx, x=x, mean=st) == 0                              # dx alone
+    n = q(dy, w, st, dx, x=x, mean=st, dweight=dw)
+    assert n > 0 and n == q(dy, w, st, dx, codes=codes, scales=scales, dweight=dw, dbias=T((40,), F32))
+    refused(ewf.EINVAL, "either", q, dy, w, st, dx)
+    refused(ewf.EINVAL, "either", q, dy, w, st, dx, x=x, mean=st, codes=codes, scales=scales)
+    refused(ewf.EINVAL, "mean is needed", q, dy, w, st, dx, x=x)
+    refused(ewf.EINVAL, "rstd is needed", q, dy, w, None, dx, x=x, mean=st)
+    refused(ewf.EINVAL, "come together", q, dy, w, st, dx, codes=codes)
+    refused(ewf.EALIAS, "dweight overlaps weight", q, dy, w, st, dx, x=x, mean=st, dweight=w)
+    refused(ewf.EALIAS, "dbias overlaps dweight", q, dy, w, st, dx, x=x, mean=st, dweight=dw, dbias=dw)
+    q(dy, w, st, dy, x=x, mean=st), q(dy, w, st, x, x=x, mean=st)           # dx over dy, or over x
+    # the workspace is asked for
+    refused(ewf.ENOMEM, "needed", ewf.layer_norm_grad, dy, w, st, dx, x=x, mean=st, dweight=dw)
+    class Small:
+        def data_ptr(self): return 0x7D0000000000
+        def numel(self): return 16
+        def element_size(self): return 1
+    refused(ewf.ENOMEM, "needed", ewf.layer_norm_grad, dy, w, st, dx, x=x, mean=st, dweight=dw, workspace=Small())
+    class Odd(Small):
+        def data_ptr(self): return 0x7D0000000008
+        def numel(self): return 1 << 30
+    refused(ewf.EINVAL, "16-byte", ewf.layer_norm_grad, dy, w, st, dx, x=x, mean=st, dweight=dw, workspace=Odd())
+
+
+def test_activation_refusals():
+    x, y, codes, scales = T((6, 40)), T((6, 40)), T((6, 40), E4M3), T((6, 2), I8)
+    refused(ewf.EINVAL, "unknown activation", ewf.activation, "swish", x, y)
+    refused(ewf.EINVAL, "are needed", ewf.activation, "relu", x)
+    refused(ewf.EINVAL, "come together", ewf.activation, "relu", x, y, codes=codes)
+    refused(ewf.EINVAL, "codes is needed", ewf.activation_grad, "relu", x, y, codes=None, scales=None)
+    refused(ewf.ETYPE, "expected", ewf.activation, "relu", x, T((6, 40), F32))
+    refused(ewf.EALIAS, "codes overlaps x", ewf.keep8, x, T((6, 40), E4M3, at=x.ptr), scales)
+    refused(ewf.EALIAS, "x overlaps codes", ewf.read8, codes, scales, T((6, 40), at=codes.ptr))
+    refused(ewf.EALIAS, "scales overlaps codes", ewf.keep8, x, codes, T((6, 2), I8, at=codes.ptr))
+    refused(ewf.EUNSUPPORTED, "contiguous", ewf.keep8, x, T((6, 40), E4M3, strides=(1, 6)), scales)
+    refused(ewf.ESHAPE, "extent", ewf.read8, codes, scales, T((6, 41)))
+
+
+def test_recurrence_refusals_and_shapes():
+    u, v, h, w = T((3, 50, 10)), T((3, 50, 10)), T((3, 50, 10)), T((3, 50, 10))
+    s0, s1 = T((3, 10), F32), T((3, 10), F32)
+    q = ewf.recurrence.workspace_bytes
+    refused(ewf.EINVAL, "v is needed", q, u, None, h)
+    refused(ewf.ESHAPE, "rank", q, T((50, 10)), v, h)
+    refused(ewf.ESHAPE, "extent", q, u, T((3, 49, 10)), h)
+    refused(ewf.ETYPE, "bfloat16", q, u, T((3, 50, 10), F32), h)
+    refused(ewf.ETYPE, "float32", q, u, v, h, h0=T((3, 10)))
+    refused(ewf.ETYPE, "int32", q, u, v, h, lengths=T((3,), F32))
+    refused(ewf.EUNSUPPORTED, "contiguous", q, T((3, 50, 10), strides=(500, 1, 50)), v, h)
+    refused(ewf.EALIAS, "last overlaps u", q, u, v, h, last=T((3, 10), F32, at=u.ptr))
+    refused(ewf.EALIAS, "h overlaps u", q, u, v, T((3, 50, 10), at=u.ptr, off=2))
+    refused(ewf.EINVAL, "null pointer", q, u, v, h, lengths=T((3,), I32, at=0))
+    q(u, v, v), q(u, v, u), q(u, v, h, h0=s0, last=s0)                         # in place
+    # column blocks of one projection, time-major
+    p = T((50, 3, 30))
+    blocks = [ewf.TensorRef(p.ptr + 20 * k, (3, 50, 10), (30, 90, 1), BF16) for k in range(3)]
+    q(blocks[0], blocks[1], blocks[2])
+    refused(ewf.EALIAS, "h overlaps v", q, blocks[0], blocks[1], ewf.TensorRef(p.ptr + 30, (3, 50, 10), (30, 90, 1), BF16))
+    g = ewf.recurrence_grad.workspace_bytes
+    du, dv, dh = T((3, 50, 10)), T((3, 50, 10)), T((3, 50, 10))
+    refused(ewf.EINVAL, "dh is needed", g, u, v, h, None, du, dv)
+    refused(ewf.EINVAL, "dw comes with w", g, u, v, h, dh, du, dv, w=w)
+    refused(ewf.EINVAL, "dw comes with w", g, u, v, h, dh, du, dv, dw=w)
+    refused(ewf.EALIAS, "du overlaps h", g, u, v, h, dh, h, dv)
+    refused(ewf.EALIAS, "dv overlaps du", g, u, v, h, dh, du, du)
+    refused(ewf.EALIAS, "dh0 overlaps h0", g, u, v, h, dh, du, dv, h0=s0, dh0=s0)
+    g(u, v, h, dh, u, dh, dh0=s1, dlast=s1)                                    # in place
+    # nothing to do is no error
+    assert q(T((0, 50, 10)), T((0, 50, 10)), T((0, 50, 10))) == 0
+    ewf.recurrence(T((0, 50, 10)), T((0, 50, 10)), T((0, 50, 10)))
+    ewf.layer_norm(T((0, 40)), None, None, T((0, 40)))
+    ewf.keep8(T((0, 40)), T((0, 40), I8), T((0, 2), I8))
+
+
+def test_tensors_outside_device_memory_are_refused():
+    x = torch.zeros(2, 8)
+    refused(ewf.EINVAL, "device memory", ewf.layer_norm, x, None, None, x)
+
+
+def test_reserved_words_and_unknown_types_are_refused():
+    f = ewf._layer_norm(T((2, 8)), None, None, T((2, 8)))
+    f.args.reserved = 1
+    assert ewf._lib.ewf_layer_norm(ewf.ctypes.byref(f.args), None) == ewf.EINVAL
+    f.args.reserved, f.args.dtype = 0, 77
+    assert ewf._lib.ewf_layer_norm(ewf.ctypes.byref(f.args), None) == ewf.ETYPE
+    assert ewf._lib.ewf_layer_norm(None, None) == ewf.EINVAL
+    assert ewf._lib.ewf_recurrence(None, None, 0, None) == ewf.EINVAL
+    assert ewf._lib.ewf_read8(None, None) == ewf.EINVAL
+    f = ewf._activation("relu", T((2, 8)), T((2, 8)))
+    f.args.act = 99
+    assert ewf._lib.ewf_activation(ewf.ctypes.byref(f.args), None) == ewf.EINVAL
