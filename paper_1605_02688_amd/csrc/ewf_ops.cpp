@@ -16,6 +16,7 @@ namespace {
 constexpr int64_t kMaxCols = (int64_t)1 << 30;
 constexpr int64_t kMaxNormCols = (int64_t)1 << 24;      // what one workgroup's sums are accurate for
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxStepBytes = (int64_t)32 << 20;
 // Operands that a launch touches once, and far more than the caches hold: accesses that leave nothing behind.
 constexpr int64_t kStreamBytes = (int64_t)64 << 20;
 
@@ -331,8 +332,9 @@ ewf_status rec_layout(const ewf_recurrence_args *a, bool grad, RecLaunch &n)
     int64_t s[kMaxDims];
     ewf_status st = base_shape("u", a->u, 3, s);
     if (st != EWF_OK) return st;
-    if ((double)s[0] * (double)s[2] > (double)kMaxRows || s[1] > kMaxRows) {
-        set_error("fewer than 2^31 steps, and sequences times channels, are supported");
+    // (steps and channels are counted in 32 bits, to the end of the last tile)
+    if ((double)s[0] * (double)s[2] > (double)kMaxRows - 64 || s[1] > ((int64_t)1 << 30)) {
+        set_error("at most 2^30 steps, and fewer than 2^31 sequences times channels, are supported");
         return EWF_ESHAPE;
     }
     const int isz = float_size(a->dtype);
@@ -345,6 +347,11 @@ ewf_status rec_layout(const ewf_recurrence_args *a, bool grad, RecLaunch &n)
         to.p = t.ptr;
         to.batch = s[0] > 1 ? t.strides[0] : 0;
         to.step = s[1] > 1 ? t.strides[1] : 0;
+        // (the kernels reach 32 steps with offsets of 31 bits)
+        if (to.step > kMaxStepBytes / isz) {
+            set_error("%s: steps that are %lld elements apart: at most 32 MiB are supported", name, (long long)to.step);
+            c.fail(EWF_EUNSUPPORTED);
+        }
     };
     auto state = [&](const char *name, const ewf_tensor &t, bool out, RecTensor &to) {
         if (!c.add(name, t, 4, {s[0], s[2]}, out, false)) return;
@@ -376,7 +383,6 @@ ewf_status rec_layout(const ewf_recurrence_args *a, bool grad, RecLaunch &n)
                          {"dw", "u"}, {"dw", "v"}, {"dw", "w"}, {"dw", "dh"}, {"dh0", "dlast"}});
     }
     if (c.status != EWF_OK) return c.status;
-    n.nt = (double)n.batch * (double)n.steps * (double)n.channels * isz >= (double)kStreamBytes;
     return EWF_OK;
 }
 

@@ -58,7 +58,6 @@ struct RecLaunch {
     const int32_t *lengths;
     int64_t lengths_stride;
     void *workspace;
-    bool nt;
 };
 
 // ---- kernels' launchers (device translation units).  They launch on `stream` and report nothing: the caller asks the runtime.

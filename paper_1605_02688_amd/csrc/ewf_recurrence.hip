@@ -8,12 +8,11 @@
 
 namespace ewf {
 
+void aux_fill_zero(void *ptr, size_t nbytes, hipStream_t stream);
+
 namespace {
 
 constexpr float kLog2E = 1.44269504f;
-constexpr int kStrip = 64;               // channels of a workgroup: two a lane, 32 lanes
-
-struct Pair { float x, y; };
 
 // f = sigmoid(u) and 1 - f, both to within a few units in the last place: e = 2^(-u log2 e), f = 1 / (1 + e),
 // 1 - f = e f.  e is kept finite (a gate of less than 2^-126 counts as that); a NaN stays one.
@@ -25,395 +24,683 @@ EWF_OPS_DEV void gate(float u, float &f, float &g)
     g = e * f;
 }
 
-// Two neighbouring channels as they are stored: one word of halves, or two floats.
-template <typename T> struct Two;
-template <> struct Two<F32> {
-    u32x2 w;
-    EWF_OPS_DEV float x() const { return bits_to_float(w[0]); }
-    EWF_OPS_DEV float y() const { return bits_to_float(w[1]); }
-};
-template <> struct Two<F16> {
-    uint32_t w;
-    EWF_OPS_DEV float x() const { return half_lo<F16>(w); }
-    EWF_OPS_DEV float y() const { return half_hi<F16>(w); }
-};
-template <> struct Two<BF16> {
-    uint32_t w;
-    EWF_OPS_DEV float x() const { return half_lo<BF16>(w); }
-    EWF_OPS_DEV float y() const { return half_hi<BF16>(w); }
-};
+// ------------------------------------------------------------------ a lane's channels
+//
+// A lane takes C neighbouring channels, 8 bytes of them.  Where fewer are left it reads the last C of the row and drops
+// what is not its own; lanes behind the end read those too, and write nothing.
 
-template <typename T>
-EWF_OPS_DEV Two<T> load_two(const typename T::raw *p)
-{
-    if constexpr (sizeof(typename T::raw) == 4) return {*reinterpret_cast<const u32x2_a4 *>(p)};
-    else return {*reinterpret_cast<const u32_a2 *>(p)};
-}
+template <typename T> constexpr int kWidth = 8 / (int)sizeof(typename T::raw);
 
-template <typename T>
-EWF_OPS_DEV void store_two(typename T::raw *p, float x, float y)
-{
-    if constexpr (sizeof(typename T::raw) == 4) *reinterpret_cast<u32x2_a4 *>(p) = u32x2{float_to_bits(x), float_to_bits(y)};
-    else *reinterpret_cast<u32_a2 *>(p) = pack_halves<T>(x, y);
-}
-
-// A lane's channels c and c + 1 of `channels`.  At the last channels a lane reads the pair that ends there, and drops
-// what is not its own; lanes behind the end read it too and write nothing.
 struct Lane {
-    int64_t from;        // channel that a load begins at
-    int have;            // channels that are the lane's own: 0, 1 or 2
-    bool second;         // the lane's one channel is the second of the pair it reads
-    bool single;         // there is one channel in all: element loads
+    int from;            // channel that a load begins at
+    int have;            // channels that are the lane's own
 };
 
-EWF_OPS_DEV Lane lane_at(int64_t c, int64_t channels)
+template <typename T>
+EWF_OPS_DEV Lane lane_at(int c, int channels)
 {
+    constexpr int C = kWidth<T>;
     Lane l;
-    l.have = c + 1 < channels ? 2 : c < channels ? 1 : 0;
-    l.single = channels == 1;
-    l.from = l.have == 2 ? c : l.single ? 0 : channels - 2;
-    l.second = l.have == 1 && !l.single;
+    l.have = channels - c;
+    l.have = l.have < 0 ? 0 : l.have > C ? C : l.have;
+    l.from = c + C <= channels ? c : channels >= C ? channels - C : 0;
     return l;
 }
 
-template <typename T>
-EWF_OPS_DEV Two<T> load_edge(const typename T::raw *p, const Lane &l)
-{
-    Two<T> r;
-    if (l.single) {
-        if constexpr (sizeof(typename T::raw) == 4) r.w = u32x2{float_to_bits(*p), 0u};
-        else r.w = *p;
-    } else {
-        r = load_two<T>(p);
-        if constexpr (sizeof(typename T::raw) == 4) r.w[0] = l.second ? r.w[1] : r.w[0];
-        else r.w = l.second ? r.w >> 16 : r.w;
+template <typename T> struct Eight {
+    u32x2 w;
+    EWF_OPS_DEV float operator[](int e) const
+    {
+        if constexpr (sizeof(typename T::raw) == 4) return bits_to_float(w[e]);
+        else return (e & 1) ? half_hi<T>(w[e >> 1]) : half_lo<T>(w[e >> 1]);
     }
-    return r;
+    // Drops the first n elements; zeros move in behind.
+    EWF_OPS_DEV void move_down(int n)
+    {
+        const uint64_t x = __builtin_bit_cast(uint64_t, w);
+        w = __builtin_bit_cast(u32x2, n < kWidth<T> ? x >> (n * (64 / kWidth<T>)) : (uint64_t)0);
+    }
+};
+
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+template <typename T> struct EightAt { typedef u32x2_a2 at; };
+template <> struct EightAt<F32> { typedef u32x2_a4 at; };
+
+template <typename T>
+EWF_OPS_DEV Eight<T> load_eight(const typename T::raw *p) { return {*reinterpret_cast<const typename EightAt<T>::at *>(p)}; }
+
+// A row's edge: p is where the lane's load begins, c the channel that is its first.
+template <typename T>
+EWF_OPS_DEV Eight<T> load_edge(const typename T::raw *p, const Lane &l, int c, int channels)
+{
+    constexpr int C = kWidth<T>, bits = 64 / C;
+    if (channels >= C) {
+        Eight<T> x = load_eight<T>(p);
+        x.move_down(c - l.from);
+        return x;
+    }
+    uint64_t w = 0;
+#pragma unroll
+    for (int e = 0; e < C - 1; e++)
+        if (e < l.have) {
+            if constexpr (sizeof(typename T::raw) == 4) w |= (uint64_t)float_to_bits(p[e]) << (e * bits);
+            else w |= (uint64_t)p[e] << (e * bits);
+        }
+    return {__builtin_bit_cast(u32x2, w)};
 }
 
 template <typename T>
-EWF_OPS_DEV void store_edge(typename T::raw *p, int have, float x, float y)
+EWF_OPS_DEV void store_eight(typename T::raw *p, const float *f)
 {
-    if (have == 2) store_two<T>(p, x, y);
-    else if (have == 1) store1<T>(p, x);
-}
-
-EWF_OPS_DEV Pair load_state(const RecTensor &t, int64_t b, const Lane &l)
-{
-    Pair s = {0.f, 0.f};
-    if (!t.p) return s;
-    const Two<F32> v = load_edge<F32>((const float *)t.p + b * t.batch + l.from, l);
-    return {v.x(), v.y()};
-}
-
-EWF_OPS_DEV void store_state(const RecTensor &t, int64_t b, int64_t c, int have, Pair s)
-{
-    if (t.p) store_edge<F32>((float *)t.p + b * t.batch + c, have, s.x, s.y);
+    u32x2 w;
+    if constexpr (sizeof(typename T::raw) == 4) w = u32x2{float_to_bits(f[0]), float_to_bits(f[1])};
+    else w = u32x2{pack_halves<T>(f[0], f[1]), pack_halves<T>(f[2], f[3])};
+    *reinterpret_cast<typename EightAt<T>::at *>(p) = w;
 }
 
 template <typename T>
-EWF_OPS_DEV typename T::raw *at(const RecTensor &t, int64_t b, int64_t step, int64_t c)
+EWF_OPS_DEV void store_edge(typename T::raw *p, int have, const float *f)
 {
-    return (typename T::raw *)t.p + b * t.batch + step * t.step + c;
+    if (have == kWidth<T>) { store_eight<T>(p, f); return; }
+#pragma unroll
+    for (int e = 0; e < kWidth<T>; e++)
+        if (e < have) store1<T>(p + e, f[e]);
 }
 
-EWF_OPS_DEV int64_t sequence_length(const RecLaunch &a, int64_t b)
+EWF_OPS_DEV float load_state(const RecTensor &t, int64_t b, int c) { return t.p ? ((const float *)t.p)[b * t.batch + c] : 0.f; }
+EWF_OPS_DEV void store_state(const RecTensor &t, int64_t b, int c, float s)
 {
-    if (!a.lengths) return a.steps;
-    const int64_t n = a.lengths[b * a.lengths_stride];
-    return n < 0 ? 0 : n > a.steps ? a.steps : n;
+    if (t.p) ((float *)t.p)[b * t.batch + c] = s;
 }
 
-// The gradients of one element.
+EWF_OPS_DEV int sequence_length(const RecLaunch &a, int64_t b)
+{
+    if (!a.lengths) return (int)a.steps;
+    const int n = a.lengths[b * a.lengths_stride];
+    return n < 0 ? 0 : n > a.steps ? (int)a.steps : n;
+}
+
+// One element's gradients from G, the gradient of its state; `f` and `before` are its gate and the state before it.  Returns what the
+// step hands to the one before.
 template <bool TIED>
-EWF_OPS_DEV void gradients(float G, float f, float one_less_f, float i, float one_less_i, float before, float v, float &du, float &dv, float &dw)
+EWF_OPS_DEV float gradients(float G, float u, float w, float v, float before, float &du, float &dv, float &dw)
 {
-    dv = G * i;
-    if constexpr (TIED) du = G * (before - v) * (f * one_less_f);
-    else {
-        du = G * before * (f * one_less_f);
-        dw = dv * v * one_less_i;
+    float f, g;
+    gate(u, f, g);
+    if constexpr (TIED) {
+        dv = G * g;
+        du = dv * (before - v) * f;
+    } else {
+        float i, j;
+        gate(w, i, j);
+        dv = G * i;
+        dw = dv * v * j;
+        du = G * before * (f * g);
     }
+    return f * G;
 }
 
 // ------------------------------------------------------------------ few steps: a lane walks through time
 
-template <typename T, bool TIED>
+template <typename T, bool TIED, bool BACK>
 __global__ void __launch_bounds__(64) k_rec_walk(RecLaunch a)
 {
-    const uint32_t pairs = (uint32_t)((a.channels + 1) / 2), all = pairs * (uint32_t)a.batch;
-    const uint32_t id = blockIdx.x * 64 + threadIdx.x;
-    if (id >= all) return;
-    const int64_t b = id / pairs, c = (int64_t)(id - (uint32_t)b * pairs) * 2;
-    const Lane l = lane_at(c, a.channels);
-    const int64_t len = sequence_length(a, b);
-    Pair s = load_state(a.h0, b, l);
-    for (int64_t t = 0; t < len; t++) {
-        const Two<T> u = load_edge<T>(at<T>(a.u, b, t, l.from), l), v = load_edge<T>(at<T>(a.v, b, t, l.from), l);
-        float f0, g0, f1, g1;
-        gate(u.x(), f0, g0);
-        gate(u.y(), f1, g1);
-        if constexpr (!TIED) {
-            const Two<T> w = load_edge<T>(at<T>(a.w, b, t, l.from), l);
-            float less;
-            gate(w.x(), g0, less);
-            gate(w.y(), g1, less);
+    constexpr int C = kWidth<T>;
+    typedef typename T::raw raw;
+    const int channels = (int)a.channels;
+    const uint32_t lanes = (uint32_t)(channels + C - 1) / C, id = blockIdx.x * 64 + threadIdx.x;
+    if (id >= lanes * (uint32_t)a.batch) return;
+    const int64_t b = id / lanes;
+    const int c = (int)(id - (uint32_t)b * lanes) * C;
+    const Lane l = lane_at<T>(c, channels);
+    const int len = sequence_length(a, b);
+    auto load = [&](const RecTensor &x, int64_t t) {
+        const raw *p = (const raw *)x.p + b * x.batch + t * x.step + l.from;
+        return l.have == C ? load_eight<T>(p) : load_edge<T>(p, l, c, channels);
+    };
+    auto store = [&](const RecTensor &x, int64_t t, const float *f) { store_edge<T>((raw *)x.p + b * x.batch + t * x.step + c, l.have, f); };
+    float s[C];
+#pragma unroll
+    for (int e = 0; e < C; e++) s[e] = e < l.have ? load_state(BACK ? a.dlast : a.h0, b, c + e) : 0.f;
+    if constexpr (!BACK) {
+        for (int t = 0; t < len; t++) {
+            const Eight<T> u = load(a.u, t), v = load(a.v, t);
+            Eight<T> w = u;
+            if constexpr (!TIED) w = load(a.w, t);
+#pragma unroll
+            for (int e = 0; e < C; e++) {
+                float f, i, less;
+                gate(u[e], f, i);
+                if constexpr (!TIED) gate(w[e], i, less);
+                s[e] = fmaf(f, s[e], i * v[e]);
+            }
+            store(a.h, t, s);
         }
-        s = {fmaf(f0, s.x, g0 * v.x()), fmaf(f1, s.y, g1 * v.y())};
-        store_edge<T>(at<T>(a.h, b, t, c), l.have, s.x, s.y);
+    } else {
+        for (int t = len - 1; t >= 0; t--) {
+            const Eight<T> u = load(a.u, t), v = load(a.v, t), dh = load(a.dh, t);
+            Eight<T> w = u, h = u;
+            if constexpr (!TIED) w = load(a.w, t);
+            if (t > 0) h = load(a.h, t - 1);
+            float du[C], dv[C], dw[C];
+#pragma unroll
+            for (int e = 0; e < C; e++) {
+                float before = h[e];
+                if (t == 0) before = e < l.have ? load_state(a.h0, b, c + e) : 0.f;
+                s[e] = gradients<TIED>(dh[e] + s[e], u[e], w[e], v[e], before, du[e], dv[e], dw[e]);
+            }
+            store(a.du, t, du);
+            store(a.dv, t, dv);
+            if constexpr (!TIED) store(a.dw, t, dw);
+        }
     }
-    store_state(a.last, b, c, l.have, s);
-}
-
-template <typename T, bool TIED>
-__global__ void __launch_bounds__(64) k_rec_walk_grad(RecLaunch a)
-{
-    const uint32_t pairs = (uint32_t)((a.channels + 1) / 2), all = pairs * (uint32_t)a.batch;
-    const uint32_t id = blockIdx.x * 64 + threadIdx.x;
-    if (id >= all) return;
-    const int64_t b = id / pairs, c = (int64_t)(id - (uint32_t)b * pairs) * 2;
-    const Lane l = lane_at(c, a.channels);
-    const int64_t len = sequence_length(a, b);
-    const Pair h0 = load_state(a.h0, b, l);
-    Pair s = load_state(a.dlast, b, l);
-    for (int64_t t = len - 1; t >= 0; t--) {
-        const Two<T> u = load_edge<T>(at<T>(a.u, b, t, l.from), l), v = load_edge<T>(at<T>(a.v, b, t, l.from), l);
-        const Two<T> dh = load_edge<T>(at<T>(a.dh, b, t, l.from), l);
-        Pair before = h0;
-        if (t > 0) {
-            const Two<T> h = load_edge<T>(at<T>(a.h, b, t - 1, l.from), l);
-            before = {h.x(), h.y()};
-        }
-        float f0, g0, f1, g1, i0, j0, i1, j1;
-        gate(u.x(), f0, g0);
-        gate(u.y(), f1, g1);
-        i0 = g0; j0 = f0; i1 = g1; j1 = f1;
-        if constexpr (!TIED) {
-            const Two<T> w = load_edge<T>(at<T>(a.w, b, t, l.from), l);
-            gate(w.x(), i0, j0);
-            gate(w.y(), i1, j1);
-        }
-        const Pair G = {dh.x() + s.x, dh.y() + s.y};
-        float du0, dv0, dw0, du1, dv1, dw1;
-        gradients<TIED>(G.x, f0, g0, i0, j0, before.x, v.x(), du0, dv0, dw0);
-        gradients<TIED>(G.y, f1, g1, i1, j1, before.y, v.y(), du1, dv1, dw1);
-        store_edge<T>(at<T>(a.du, b, t, c), l.have, du0, du1);
-        store_edge<T>(at<T>(a.dv, b, t, c), l.have, dv0, dv1);
-        if constexpr (!TIED) store_edge<T>(at<T>(a.dw, b, t, c), l.have, dw0, dw1);
-        s = {f0 * G.x, f1 * G.y};
-    }
-    store_state(a.dh0, b, c, l.have, s);
+#pragma unroll
+    for (int e = 0; e < C; e++)
+        if (e < l.have) store_state(BACK ? a.dh0 : a.last, b, c + e, s[e]);
 }
 
 // ------------------------------------------------------------------ tiles of steps
 //
-// A workgroup of W wavefronts takes kStrip channels of a sequence and W x 2 x R steps at a time.  A lane holds two
-// channels and R consecutive steps in registers, the two halves of a wavefront one run of R steps after the
-// other.  A lane composes its steps (the map of all of them, and the state at each of them if the tile began at zero),
-// the maps are composed across halves by a lane exchange and across wavefronts through LDS, and with the state that
-// its run begins at a lane finishes its results: F_r s + (state from zero).
+// A workgroup of W wavefronts takes a strip of L x C channels of a sequence and W x G x R steps at a time, G = 64 / L.
+// A lane holds R consecutive steps in registers, the G groups of a wavefront one run of R steps after the other.  A
+// lane composes its steps to one map; the maps are composed across groups by lane exchanges and across wavefronts
+// through LDS, by one thread for each channel, which also keeps the channel's state; and from the state that its run
+// begins at a lane walks its steps a second time.
+
+struct Map { float F, B; };
+EWF_OPS_DEV Map after(const Map &m, const Map &n) { return {m.F * n.F, fmaf(m.F, n.B, m.B)}; }     // m after n
+EWF_OPS_DEV float apply(const Map &m, float s) { return fmaf(m.F, s, m.B); }
 
 template <typename T, bool BACK> struct Raw;            // a lane's operands at one step, as stored
-template <typename T> struct Raw<T, false> { Two<T> u, v, w; };
-template <typename T> struct Raw<T, true> { Two<T> u, v, w, h, dh; };
+template <typename T> struct Raw<T, false> { Eight<T> u, v, w; };
+template <typename T> struct Raw<T, true> { Eight<T> u, v, w, h, dh; };
 
-template <typename T, bool TIED, bool BACK, int R, int W>
-struct Tile {
-    static constexpr int kSteps = W * 2 * R;
-    const RecLaunch &a;
-    int64_t b, c, len;
-    Lane l;
-    bool whole_strip;
-    int first;                                          // of this lane's steps within a tile
-    Pair h0;                                            // BACK: the state before the first step
+// The rows of one tensor that a lane reads or writes, one after the other: an address that all lanes of a wavefront share, and
+// offsets of 32 bits to it (the host refuses steps that are further apart).  Reads stay between the first and the last
+// step that exists: steps that do not are read from there, and composing leaves them out.
+template <typename T, bool BACK>
+struct Rows {
+    char *base;
+    int at, step, lowest, highest;                      // bytes
 
-    EWF_OPS_DEV Tile(const RecLaunch &a_, int64_t strip, int64_t b_) : a(a_), b(b_)
+    EWF_OPS_DEV Eight<T> load() const
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        c = strip * kStrip + (lane & 31) * 2;
-        len = sequence_length(a, b);
-        l = lane_at(c, a.channels);
-        whole_strip = strip * kStrip + kStrip <= a.channels;
-        first = (wave * 2 + (lane >> 5)) * R;
-        if constexpr (BACK) h0 = load_state(a.h0, b, l);
+        const int off = BACK ? (at > lowest ? at : lowest) : (at < highest ? at : highest);
+        return load_eight<T>((const typename T::raw *)(base + (uint32_t)off));
+    }
+    EWF_OPS_DEV typename T::raw *pointer() const { return (typename T::raw *)(base + (uint32_t)at); }
+    EWF_OPS_DEV void next() { at += BACK ? -step : step; }
+};
+
+template <typename T, bool TIED, bool BACK, int L, int R, int W>
+struct Tile {
+    static constexpr int C = kWidth<T>, G = 64 / L, kSteps = W * G * R, kStrip = L * C, size = sizeof(typename T::raw);
+    static_assert(kStrip <= W * 64, "one thread for each channel of a strip");
+    static_assert(G * R <= 32, "a wavefront's steps span less than 2^31 bytes");
+    const RecLaunch &a;
+    int b, c0, len, channels;                           // sequence, first channel
+    int place, group, wave;                             // of the lane in its row; of its run in the wavefront
+    bool whole_strip;
+    Lane l;
+
+    EWF_OPS_DEV Tile(const RecLaunch &a_, int strip, int b_) : a(a_), b(b_), c0(strip * kStrip)
+    {
+        channels = (int)a.channels;
+        place = threadIdx.x % L;
+        group = threadIdx.x % 64 / L;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        len = __builtin_amdgcn_readfirstlane(sequence_length(a, b));
+        l = lane_at<T>(channel(), channels);
+        whole_strip = c0 + kStrip <= channels;
     }
 
+    EWF_OPS_DEV int channel() const { return c0 + C * place; }
     // The time of the k-th step of the walk: backwards it begins at the sequence's end.
-    EWF_OPS_DEV int64_t time(int64_t k) const { return BACK ? len - 1 - k : k; }
-
-    // Every step of the tile from k0 on exists, and so does the state before it in memory.
-    EWF_OPS_DEV bool whole(int64_t k0) const { return whole_strip && k0 + kSteps <= len - (BACK ? 1 : 0); }
-
-    EWF_OPS_DEV void load(int64_t k0, Raw<T, BACK> (&raw)[R]) const
+    EWF_OPS_DEV int time(int k) const { return BACK ? len - 1 - k : k; }
+    // The first step of a lane's R in the tile that begins at step k0.
+    EWF_OPS_DEV int first(int k0) const { return k0 + (wave * G + group) * R; }
+    // The earliest time of the wavefront's steps that exist (a wavefront without any reads the last that does).
+    EWF_OPS_DEV int earliest(int k0) const
     {
-        if (whole(k0)) {
-            const int64_t t = time(k0 + first), s = BACK ? -1 : 1;
-            const typename T::raw *pu = at<T>(a.u, b, t, c), *pv = at<T>(a.v, b, t, c), *pw = nullptr, *ph = nullptr, *pd = nullptr;
-            if constexpr (!TIED) pw = at<T>(a.w, b, t, c);
-            if constexpr (BACK) { ph = at<T>(a.h, b, t - 1, c); pd = at<T>(a.dh, b, t, c); }
+        const int k = k0 + wave * G * R + (BACK ? G * R - 1 : 0);
+        return time(k < len ? k : len - 1);
+    }
+
+    // `before` of the tensor: its rows one step earlier.
+    EWF_OPS_DEV Rows<T, BACK> rows(const RecTensor &x, int k0, bool read, bool before = false) const
+    {
+        const int t0 = earliest(k0), shift = before ? 1 : 0;
+        const int base = t0 >= shift ? t0 - shift : 0;                                  // (uniform)
+        int rel = BACK ? len - 1 - first(k0) - shift - base : group * R;               // of the lane's first step
+        if (BACK && rel < 0) rel = 0;                                                   // (all its rows are read at the earliest)
+        const int more = len - 1 - base;
+        const int edge = channels - C < c0 ? channels - C : c0;                         // (uniform: reads of the last channels begin there)
+        const int from = read ? edge : c0, c = (read ? l.from - edge : C * place) * size;
+        Rows<T, BACK> r;
+        r.base = (char *)x.p + (b * x.batch + base * x.step + from) * size;
+        r.step = (int)(x.step * size);
+        r.at = rel * r.step + c;
+        r.lowest = c;
+        r.highest = (more < G * R - 1 ? more : G * R - 1) * r.step + c;
+        return r;
+    }
+
+    EWF_OPS_DEV void load(int k0, Raw<T, BACK> (&raw)[R]) const
+    {
+        auto fetch = [&](const RecTensor &x, bool before, Eight<T> Raw<T, BACK>::*to) {
+            auto p = rows(x, k0, true, before);
+#pragma unroll
+            for (int r = 0; r < R; r++) { raw[r].*to = p.load(); p.next(); }
+        };
+        fetch(a.u, false, &Raw<T, BACK>::u);
+        fetch(a.v, false, &Raw<T, BACK>::v);
+        if constexpr (!TIED) fetch(a.w, false, &Raw<T, BACK>::w);
+        if constexpr (BACK) {
+            fetch(a.dh, false, &Raw<T, BACK>::dh);
+            fetch(a.h, true, &Raw<T, BACK>::h);
+        }
+        if (!whole_strip) {
+            const int drop = channel() - l.from;
 #pragma unroll
             for (int r = 0; r < R; r++) {
-                raw[r].u = load_two<T>(pu + r * s * a.u.step);
-                raw[r].v = load_two<T>(pv + r * s * a.v.step);
-                if constexpr (!TIED) raw[r].w = load_two<T>(pw + r * s * a.w.step);
-                if constexpr (BACK) {
-                    raw[r].h = load_two<T>(ph + r * s * a.h.step);
-                    raw[r].dh = load_two<T>(pd + r * s * a.dh.step);
-                }
+                raw[r].u.move_down(drop);
+                raw[r].v.move_down(drop);
+                if constexpr (!TIED) raw[r].w.move_down(drop);
+                if constexpr (BACK) { raw[r].h.move_down(drop); raw[r].dh.move_down(drop); }
             }
-            return;
         }
+    }
+
+    // What a lane keeps of its steps between the two walks: forward the steps' maps; backward the operands, from which
+    // the gates are computed a second time (bfloat16 [8, 4096, 2048] 176 us; with the gates kept, 218.  Forward the second
+    // computation costs more than the registers it saves: 108 and 100).
+    static constexpr bool kMaps = !BACK;
+    struct Maps { float f[R][C], b[R][C]; };
+
+    EWF_OPS_DEV void step_map(const Raw<T, BACK> &x, int e, float &f, float &b) const
+    {
+        float i, less;
+        gate(x.u[e], f, i);
+        if constexpr (BACK) b = f * x.dh[e];
+        else {
+            if constexpr (!TIED) gate(x.w[e], i, less);
+            b = i * x.v[e];
+        }
+    }
+
+    // Composes a lane's steps to one map a channel.
+    EWF_OPS_DEV void compose(int k0, const Raw<T, BACK> (&raw)[R], Maps &maps, Map (&m)[C]) const
+    {
+        const bool all = len - k0 >= kSteps;
+        const int from = first(k0);
+#pragma unroll
+        for (int e = 0; e < C; e++) m[e] = {1.f, 0.f};
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            // (steps that do not exist read one that does; compose() leaves them out)
-            int64_t k = k0 + first + r;
-            k = k < len ? k : len - 1;
-            const int64_t t = time(k);
-            raw[r].u = load_edge<T>(at<T>(a.u, b, t, l.from), l);
-            raw[r].v = load_edge<T>(at<T>(a.v, b, t, l.from), l);
-            if constexpr (!TIED) raw[r].w = load_edge<T>(at<T>(a.w, b, t, l.from), l);
-            if constexpr (BACK) {
-                raw[r].h = load_edge<T>(at<T>(a.h, b, t > 0 ? t - 1 : 0, l.from), l);
-                raw[r].dh = load_edge<T>(at<T>(a.dh, b, t, l.from), l);
+#pragma unroll
+            for (int e = 0; e < C; e++) {
+                float f, x;
+                step_map(raw[r], e, f, x);
+                if (!all && from + r >= len) { f = 1.f; x = 0.f; }
+                m[e] = after({f, x}, m[e]);
+                if constexpr (kMaps) { maps.f[r][e] = f; maps.b[r][e] = x; }
+            }
+        }
+    }
+
+    // The maps of the groups before a lane's own, composed; m becomes the map of the wavefront in its last group.
+    EWF_OPS_DEV void across_groups(Map (&m)[C], Map (&before)[C]) const
+    {
+#pragma unroll
+        for (int e = 0; e < C; e++) {
+            Map own = m[e];
+#pragma unroll
+            for (int d = 1; d < G; d *= 2) {
+                const Map prev = {__shfl_up(own.F, d * L), __shfl_up(own.B, d * L)};
+                if (group >= d) own = after(own, prev);
+            }
+            before[e] = {1.f, 0.f};
+            if constexpr (G > 1) {
+                const Map prev = {__shfl_up(own.F, L), __shfl_up(own.B, L)};
+                if (group > 0) before[e] = prev;
+            }
+            m[e] = own;
+        }
+    }
+
+    // Walks a lane's steps from the states s that they begin at, and writes its results.
+    EWF_OPS_DEV void finish(int k0, const Raw<T, BACK> (&raw)[R], const Maps &maps, float (&s)[C]) const
+    {
+        const int from = first(k0);
+        auto put = [&](Rows<T, BACK> &p, int r, const float *f) {
+            if (from + r < len) {
+                if (whole_strip) store_eight<T>(p.pointer(), f);
+                else store_edge<T>(p.pointer(), l.have, f);
+            }
+            p.next();
+        };
+        if constexpr (!BACK) {
+            auto ph = rows(a.h, k0, false);
+#pragma unroll
+            for (int r = 0; r < R; r++) {
+#pragma unroll
+                for (int e = 0; e < C; e++) {
+                    float f, b;
+                    if constexpr (kMaps) { f = maps.f[r][e]; b = maps.b[r][e]; }
+                    else step_map(raw[r], e, f, b);
+                    s[e] = fmaf(f, s[e], b);
+                }
+                put(ph, r, s);
+            }
+        } else {
+            auto pu = rows(a.du, k0, false), pv = rows(a.dv, k0, false), pw = rows(TIED ? a.du : a.dw, k0, false);
+#pragma unroll
+            for (int r = 0; r < R; r++) {
+                const Raw<T, true> &x = raw[r];
+                float du[C], dv[C], dw[C];
+#pragma unroll
+                for (int e = 0; e < C; e++) {
+                    float state = x.h[e];
+                    if (from + r == len - 1) state = e < l.have ? load_state(a.h0, b, channel() + e) : 0.f;
+                    s[e] = gradients<TIED>(x.dh[e] + s[e], x.u[e], TIED ? 0.f : x.w[e], x.v[e], state, du[e], dv[e], dw[e]);
+                }
+                put(pu, r, du);
+                put(pv, r, dv);
+                if constexpr (!TIED) put(pw, r, dw);
             }
         }
     }
 };
 
-struct Map { float F0, B0, F1, B1; };                   // of a lane's two channels
+// ------------------------------------------------------------------ one workgroup for a strip: tile after tile
 
-EWF_OPS_DEV Pair apply(const Map &m, const Pair &s) { return {fmaf(m.F0, s.x, m.B0), fmaf(m.F1, s.y, m.B1)}; }
-
-template <typename T, bool TIED, bool BACK, int R, int W>
+template <typename T, bool TIED, bool BACK, int L, int R, int W>
 __global__ void __launch_bounds__(W * 64) k_rec_march(RecLaunch a)
 {
-    typedef Tile<T, TIED, BACK, R, W> Tl;
-    __shared__ Map totals[2][W][32];
-    const uint32_t strips = (uint32_t)((a.channels + kStrip - 1) / kStrip), jobs = strips * (uint32_t)a.batch;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool later = lane >= 32;
+    typedef Tile<T, TIED, BACK, L, R, W> Tl;
+    constexpr int C = Tl::C;
+    __shared__ Map totals[W][Tl::kStrip];
+    __shared__ float states[W][Tl::kStrip];             // that a wavefront's steps begin at
+    const uint32_t strips = ((uint32_t)a.channels + Tl::kStrip - 1) / Tl::kStrip, jobs = strips * (uint32_t)a.batch;
     for (uint32_t job = blockIdx.x; job < jobs; job += gridDim.x) {
         const uint32_t b = job / strips;
-        Tl tile(a, job - b * strips, b);
-        __syncthreads();                                    // (the arrays of the job before are read)
-        Pair carry = load_state(BACK ? a.dlast : a.h0, b, tile.l);
+        const Tl tile(a, job - b * strips, b);
+        const int mine = tile.c0 + threadIdx.x;         // the channel whose state this thread keeps
+        const bool keeps = threadIdx.x < Tl::kStrip && mine < tile.channels;
+        float state = keeps ? load_state(BACK ? a.dlast : a.h0, b, mine) : 0.f;
         Raw<T, BACK> raw[R];
         if (tile.len > 0) tile.load(0, raw);
-        int buf = 0;
-        for (int64_t k0 = 0; k0 < tile.len; k0 += Tl::kSteps, buf ^= 1) {
-            const bool whole = k0 + Tl::kSteps <= tile.len;
-            float F[R][2], S[R][2];                         // the map's factor up to (BACK: before) a step; the state there from zero
-            float f[R][2], g[R][2], i[R][2], j[R][2], v[R][2], before[R][2];
-            float P0 = 1.f, P1 = 1.f, s0 = 0.f, s1 = 0.f;
-    #pragma unroll
-            for (int r = 0; r < R; r++) {
-                const int64_t k = k0 + tile.first + r;
-                const bool live = whole || k < tile.len;
-                gate(raw[r].u.x(), f[r][0], g[r][0]);
-                gate(raw[r].u.y(), f[r][1], g[r][1]);
-                if constexpr (!TIED) {
-                    gate(raw[r].w.x(), i[r][0], j[r][0]);
-                    gate(raw[r].w.y(), i[r][1], j[r][1]);
-                } else {
-                    i[r][0] = g[r][0]; i[r][1] = g[r][1]; j[r][0] = f[r][0]; j[r][1] = f[r][1];
-                }
-                v[r][0] = raw[r].v.x(); v[r][1] = raw[r].v.y();
-                if constexpr (!BACK) {
-                    if (live) {
-                        s0 = fmaf(f[r][0], s0, i[r][0] * v[r][0]);
-                        s1 = fmaf(f[r][1], s1, i[r][1] * v[r][1]);
-                        P0 *= f[r][0];
-                        P1 *= f[r][1];
-                    }
-                    F[r][0] = P0; F[r][1] = P1;
-                    S[r][0] = s0; S[r][1] = s1;
-                } else {
-                    before[r][0] = raw[r].h.x(); before[r][1] = raw[r].h.y();
-                    if (k == tile.len - 1) { before[r][0] = tile.h0.x; before[r][1] = tile.h0.y; }
-                    F[r][0] = P0; F[r][1] = P1;
-                    S[r][0] = s0 + raw[r].dh.x(); S[r][1] = s1 + raw[r].dh.y();
-                    if (live) {
-                        s0 = f[r][0] * S[r][0];
-                        s1 = f[r][1] * S[r][1];
-                        P0 *= f[r][0];
-                        P1 *= f[r][1];
-                    }
-                }
-            }
-            // the next tile's operands are in flight during the rest
-            if (k0 + Tl::kSteps < tile.len) tile.load(k0 + Tl::kSteps, raw);
-            // across the halves of the wavefront
-            const Map own = {P0, s0, P1, s1};
-            const Map other = {__shfl_xor(P0, 32), __shfl_xor(s0, 32), __shfl_xor(P1, 32), __shfl_xor(s1, 32)};
-            if (later)
-                totals[buf][wave][lane - 32] = Map{own.F0 * other.F0, fmaf(own.F0, other.B0, own.B0), own.F1 * other.F1, fmaf(own.F1, other.B1, own.B1)};
+        for (int k0 = 0; k0 < tile.len; k0 += Tl::kSteps) {
+            typename Tl::Maps maps;
+            Map m[C], before[C];
+            Raw<T, BACK> now[R];
+#pragma unroll
+            for (int r = 0; r < R; r++) now[r] = raw[r];
+            // the next tile's operands are in flight during all of this one
+            if (tile.len - k0 > Tl::kSteps) tile.load(k0 + Tl::kSteps, raw);
+            tile.compose(k0, now, maps, m);
+            tile.across_groups(m, before);
+            if (tile.group == Tl::G - 1)
+#pragma unroll
+                for (int e = 0; e < C; e++) totals[tile.wave][tile.place * C + e] = m[e];
             __syncthreads();
-            // across the wavefronts, in every one of them (two arrays in turn: one barrier a tile)
-            Pair at_wave = carry;
-    #pragma unroll
-            for (int q = 0; q < W; q++) {
-                if (q == wave) at_wave = carry;
-                carry = apply(totals[buf][q][lane & 31], carry);
-            }
-            const Pair from = later ? apply(other, at_wave) : at_wave;
-    #pragma unroll
-            for (int r = 0; r < R; r++) {
-                const int64_t k = k0 + tile.first + r;
-                if (!(whole || k < tile.len)) continue;
-                const int64_t t = tile.time(k);
-                const float G0 = fmaf(F[r][0], from.x, S[r][0]), G1 = fmaf(F[r][1], from.y, S[r][1]);
-                if constexpr (!BACK) store_edge<T>(at<T>(a.h, b, t, tile.c), tile.l.have, G0, G1);
-                else {
-                    float du0, dv0, dw0, du1, dv1, dw1;
-                    gradients<TIED>(G0, f[r][0], g[r][0], i[r][0], j[r][0], before[r][0], v[r][0], du0, dv0, dw0);
-                    gradients<TIED>(G1, f[r][1], g[r][1], i[r][1], j[r][1], before[r][1], v[r][1], du1, dv1, dw1);
-                    store_edge<T>(at<T>(a.du, b, t, tile.c), tile.l.have, du0, du1);
-                    store_edge<T>(at<T>(a.dv, b, t, tile.c), tile.l.have, dv0, dv1);
-                    if constexpr (!TIED) store_edge<T>(at<T>(a.dw, b, t, tile.c), tile.l.have, dw0, dw1);
+            if (threadIdx.x < Tl::kStrip) {
+#pragma unroll
+                for (int q = 0; q < W; q++) {
+                    states[q][threadIdx.x] = state;
+                    state = apply(totals[q][threadIdx.x], state);
                 }
             }
+            __syncthreads();
+            float s[C];
+#pragma unroll
+            for (int e = 0; e < C; e++) s[e] = apply(before[e], states[tile.wave][tile.place * C + e]);
+            tile.finish(k0, now, maps, s);
         }
-        if (wave == 0 && !later) store_state(BACK ? a.dh0 : a.last, b, tile.c, tile.l.have, carry);
+        if (keeps) store_state(BACK ? a.dh0 : a.last, b, mine, state);
+    }
+}
+
+// ------------------------------------------------------------------ chains of tiles
+//
+// Many steps: a workgroup takes one tile, and the tiles of a strip of channels form a chain.  Every tile's map is published
+// as soon as it is known, and the state behind it as soon as that is: a tile finds the state that it begins at by
+// composing the maps of the tiles before it, back to the nearest whose state is known.  The operands are read once and no
+// tile waits for another's loads.
+//
+// A channel's record in the workspace is one 64-bit word, written and read by single atomic accesses that need no order among
+// each other: the map's B or the state in the upper half, the map's F below, whose two upper bits are
+// free (F lies in [0, 1]) and say what the word holds.  The words are zero when the kernel begins.
+//
+// The wait ends: a workgroup draws its place in the chain when it runs, so that all tiles before it belong to workgroups
+// that run or are done, and it publishes its own map before it waits; the first tile waits for none, and each next one
+// only for words that workgroups publish without waiting, or after a wait that has ended.
+
+constexpr uint32_t kMapBit = 1u << 30, kStateBit = 1u << 31;
+
+// (a factor that is NaN becomes a map that yields NaN)
+EWF_OPS_DEV uint64_t map_word(const Map &m)
+{
+    const bool sound = m.F == m.F;
+    return (uint64_t)float_to_bits(sound ? m.B : m.F) << 32 | (sound ? float_to_bits(m.F) : 0u) | kMapBit;
+}
+EWF_OPS_DEV uint64_t state_word(float s) { return (uint64_t)float_to_bits(s) << 32 | kStateBit; }
+EWF_OPS_DEV bool is_empty(uint64_t w) { return (uint32_t)w < kMapBit; }
+
+EWF_OPS_DEV void publish(uint64_t *p, uint64_t w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+EWF_OPS_DEV uint64_t look(const uint64_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// The state that the tile at `place` (not the first) of a channel begins at; `record` is the tile's own, `back` what two
+// neighbouring tiles' records are apart.  Back to the nearest known state, then from it through the maps in the order of
+// the tiles: the operations are those by which the tiles in between find their own states, so that the result has the same
+// bits wherever the search ends.  Four records are looked at together: their loads overlap (eight and sixteen cost
+// more traffic than they save).
+constexpr int kLook = 4;
+
+EWF_OPS_DEV float search(const uint64_t *record, int64_t back, int place)
+{
+    uint64_t w[kLook];
+    int from = place - 1;
+    for (bool known = false; ; from -= kLook) {
+#pragma unroll
+        for (int q = 0; q < kLook; q++) w[q] = from >= q ? look(record - (place - from + q) * back) : 0;
+#pragma unroll
+        for (int q = 0; q < kLook; q++) {
+            if (known) break;
+            while (is_empty(w[q])) {                    // (never before the first tile, which publishes a state)
+                __builtin_amdgcn_s_sleep(1);
+                w[q] = look(record - (place - from + q) * back);
+            }
+            known = (uint32_t)w[q] & kStateBit;
+        }
+        if (known) break;
+    }
+    float s = 0.f;
+    for (;;) {
+#pragma unroll
+        for (int q = kLook - 1; q >= 0; q--) {          // (what precedes the nearest known state is replaced by it)
+            const float value = bits_to_float((uint32_t)(w[q] >> 32));
+            s = (uint32_t)w[q] & kStateBit ? value : fmaf(bits_to_float((uint32_t)w[q] & ~kMapBit), s, value);
+        }
+        from += kLook;
+        if (from > place - 1) return s;
+#pragma unroll
+        for (int q = 0; q < kLook; q++) w[q] = look(record - (place - from + q) * back);
+    }
+}
+
+template <typename T, bool TIED, bool BACK, int L, int R, int W>
+__global__ void __launch_bounds__(W * 64) k_rec_chain(RecLaunch a, uint32_t chains, uint32_t tiles)
+{
+    typedef Tile<T, TIED, BACK, L, R, W> Tl;
+    constexpr int C = Tl::C;
+    __shared__ Map totals[W][Tl::kStrip];
+    __shared__ float states[W][Tl::kStrip];
+    __shared__ uint32_t drawn;
+    const uint32_t strips = ((uint32_t)a.channels + Tl::kStrip - 1) / Tl::kStrip, jobs = chains * tiles;
+    uint64_t *records = (uint64_t *)a.workspace;
+    uint32_t *counters = (uint32_t *)(records + (uint64_t)chains * tiles * Tl::kStrip);
+    const int64_t back = (int64_t)chains * Tl::kStrip;
+    for (uint32_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const uint32_t chain = job % chains, b = chain / strips;
+        uint32_t place = 0;
+        __syncthreads();                                // (the arrays of the job before are read)
+        if (tiles > 1) {
+            if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(counters + chain, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            place = __builtin_amdgcn_readfirstlane(drawn);
+        }
+        const Tl tile(a, chain - b * strips, b);
+        const int k0 = (int)place * Tl::kSteps;
+        if (k0 >= tile.len && place) continue;          // (no step: nobody looks for this tile)
+        Raw<T, BACK> raw[R];
+        typename Tl::Maps maps;
+        Map m[C], before[C];
+        if (tile.len > 0) {
+            tile.load(k0, raw);
+            tile.compose(k0, raw, maps, m);
+            tile.across_groups(m, before);
+            if (tile.group == Tl::G - 1)
+#pragma unroll
+                for (int e = 0; e < C; e++) totals[tile.wave][tile.place * C + e] = m[e];
+        }
+        __syncthreads();
+        if (threadIdx.x < Tl::kStrip) {
+            const int mine = tile.c0 + threadIdx.x;
+            const bool exists = mine < tile.channels;
+            Map part[W], all = {1.f, 0.f};
+            if (tile.len > 0)
+#pragma unroll
+                for (int q = 0; q < W; q++) {
+                    part[q] = totals[q][threadIdx.x];
+                    all = after(part[q], all);
+                }
+            uint64_t *record = records + (uint64_t)place * back + chain * Tl::kStrip + threadIdx.x;
+            float state;
+            if (place) {
+                publish(record, map_word(all));
+                state = search(record, back, (int)place);
+            } else state = exists ? load_state(BACK ? a.dlast : a.h0, b, mine) : 0.f;
+            const float end = apply(all, state);
+            if (tile.len - k0 > Tl::kSteps) publish(record, state_word(end));
+            else if (exists) store_state(BACK ? a.dh0 : a.last, b, mine, end);
+            if (tile.len > 0)
+#pragma unroll
+                for (int q = 0; q < W; q++) {
+                    states[q][threadIdx.x] = state;
+                    state = apply(part[q], state);
+                }
+        }
+        __syncthreads();
+        if (tile.len == 0) continue;
+        float s[C];
+#pragma unroll
+        for (int e = 0; e < C; e++) s[e] = apply(before[e], states[tile.wave][tile.place * C + e]);
+        tile.finish(k0, raw, maps, s);
     }
 }
 
 // ------------------------------------------------------------------ which kernel
 
-constexpr uint32_t kMostJobs = 1 << 20;  // workgroups of a launch; further strips are taken in turn
+constexpr uint32_t kMostJobs = 1 << 20;  // workgroups of a launch; further jobs are taken in turn
 constexpr int kWalkSteps = 16;           // up to here a lane walks through time by itself
 
-template <typename T, bool TIED>
-void run(const RecLaunch &a, bool backward, hipStream_t stream)
+// Lanes a row, steps a lane, wavefronts.
+template <int L_, int R_, int W_> struct Shape { static constexpr int L = L_, R = R_, W = W_, steps = W_ * (64 / L_) * R_; };
+typedef Shape<16, 4, 8> Narrow;          // 128 bytes of a row, 128 steps
+typedef Shape<32, 16, 8> Long;           // 256 bytes, 256 steps
+typedef Shape<64, 8, 8> Wide;            // 512 bytes, 64 steps
+
+enum class How { Walk, March, Small, Large };
+
+struct Plan {
+    How how = How::Walk;
+    uint64_t chains = 0, tiles = 1;
+    size_t bytes = 0;
+};
+
+template <typename S>
+void cut(const RecLaunch &a, How how, Plan &p)
 {
-    if (a.steps <= kWalkSteps) {
+    const int64_t strip = S::L * (a.dtype == EWF_F32 ? 2 : 4);
+    p.how = how;
+    p.chains = (uint64_t)((a.channels + strip - 1) / strip) * a.batch;
+    p.tiles = how == How::March ? 1 : (uint64_t)((a.steps + S::steps - 1) / S::steps);
+    p.bytes = p.tiles > 1 ? (p.chains * p.tiles * strip * 8 + p.chains * 4 + 15) / 16 * 16 : 0;
+}
+
+// Forward, us, march / chains of long tiles / chains of narrow tiles, bfloat16 [8, 4096, 2048] (256 strips of 64 channels)
+// 91 / 105 / 121, [16, 512, 1024] (256) 13.0 / 15.3 / -, [3, 4096, 2048] (96) 73 / 44 / 48, [1, 65536, 1024] (16) 1047 / 103 / -: a
+// workgroup for a strip where there is one for nearly each unit, tiles where there are fewer.  Long tiles, of which fewer
+// search, where there is one for each unit ([4, 2048, 1024], 256 of them, 16.6 / 18.2; [2, 512, 2048], 64, 11.8 / 10.8).
+// Backward, wide tiles / narrow ones: [8, 4096, 2048] 176 / 206, [3, 4096, 2048] (1536 wide tiles) 77 / 82, [4, 2048, 1024] (512)
+// 34.1 / 32.8, float16 [5, 1237, 1000] (400) 30.9 / 23.0; sequences that one wide tile holds ([32, 64, 2048]) 14.5 / 19.0.
+Plan plan_of(const RecLaunch &a, bool backward, int units)
+{
+    Plan p;
+    if (a.steps <= kWalkSteps || a.channels < (a.dtype == EWF_F32 ? 2 : 4)) return p;
+    if (!backward) {
+        cut<Narrow>(a, How::March, p);
+        if (p.chains * 8 >= (uint64_t)units * 7) return p;
+        cut<Long>(a, How::Large, p);
+        if (p.chains * p.tiles >= (uint64_t)units) return p;
+    } else {
+        cut<Wide>(a, How::Large, p);
+        if (p.chains * p.tiles >= 4 * (uint64_t)units || p.tiles == 1) return p;
+    }
+    cut<Narrow>(a, How::Small, p);
+    return p;
+}
+
+template <typename T, bool TIED, bool BACK, typename S>
+void run_chain(const RecLaunch &a, const Plan &p, hipStream_t stream)
+{
+    if (p.bytes) aux_fill_zero(a.workspace, p.bytes, stream);
+    const uint64_t jobs = p.chains * p.tiles;
+    hipLaunchKernelGGL((k_rec_chain<T, TIED, BACK, S::L, S::R, S::W>), dim3((uint32_t)(jobs < kMostJobs ? jobs : kMostJobs)), dim3(S::W * 64), 0, stream, a,
+                       (uint32_t)p.chains, (uint32_t)p.tiles);
+}
+
+template <typename T, bool TIED, bool BACK>
+void run(const RecLaunch &a, const Plan &p, hipStream_t stream)
+{
+    constexpr int C = kWidth<T>;
+    switch (p.how) {
+    case How::Walk: {
         // (fewer than 2^31 lanes: batch x channels is)
-        const dim3 grid((uint32_t)(((uint64_t)((a.channels + 1) / 2) * a.batch + 63) / 64));
-        if (backward) hipLaunchKernelGGL((k_rec_walk_grad<T, TIED>), grid, dim3(64), 0, stream, a);
-        else hipLaunchKernelGGL((k_rec_walk<T, TIED>), grid, dim3(64), 0, stream, a);
+        const dim3 grid((uint32_t)(((uint64_t)((a.channels + C - 1) / C) * a.batch + 63) / 64));
+        hipLaunchKernelGGL((k_rec_walk<T, TIED, BACK>), grid, dim3(64), 0, stream, a);
         return;
     }
-    const uint64_t jobs = (uint64_t)((a.channels + kStrip - 1) / kStrip) * a.batch;
-    const dim3 grid((uint32_t)(jobs < kMostJobs ? jobs : kMostJobs));
-    if (backward) hipLaunchKernelGGL((k_rec_march<T, TIED, true, 4, 8>), grid, dim3(512), 0, stream, a);
-    else hipLaunchKernelGGL((k_rec_march<T, TIED, false, 8, 8>), grid, dim3(512), 0, stream, a);
+    case How::March:
+        if constexpr (!BACK)
+            hipLaunchKernelGGL((k_rec_march<T, TIED, false, Narrow::L, Narrow::R, Narrow::W>), dim3((uint32_t)(p.chains < kMostJobs ? p.chains : kMostJobs)),
+                               dim3(Narrow::W * 64), 0, stream, a);
+        return;
+    case How::Small: return run_chain<T, TIED, BACK, Narrow>(a, p, stream);
+    case How::Large:
+        if constexpr (BACK) return run_chain<T, TIED, true, Wide>(a, p, stream);
+        else return run_chain<T, TIED, false, Long>(a, p, stream);
+    }
 }
 
 template <typename T>
-void run_type(const RecLaunch &a, bool backward, hipStream_t stream)
+void run_type(const RecLaunch &a, bool backward, const Plan &p, hipStream_t stream)
 {
-    if (a.w.p) run<T, false>(a, backward, stream);
-    else run<T, true>(a, backward, stream);
+    if (a.w.p) { if (backward) run<T, false, true>(a, p, stream); else run<T, false, false>(a, p, stream); }
+    else { if (backward) run<T, true, true>(a, p, stream); else run<T, true, false>(a, p, stream); }
 }
 
 }  // namespace
 
-size_t recurrence_workspace(const RecLaunch &, bool, int) { return 0; }
+size_t recurrence_workspace(const RecLaunch &a, bool backward, int units) { return plan_of(a, backward, units).bytes; }
 
-void launch_recurrence(const RecLaunch &a, bool backward, int, hipStream_t stream)
+void launch_recurrence(const RecLaunch &a, bool backward, int units, hipStream_t stream)
 {
-    if (a.dtype == EWF_F32) run_type<F32>(a, backward, stream);
-    else if (a.dtype == EWF_F16) run_type<F16>(a, backward, stream);
-    else run_type<BF16>(a, backward, stream);
+    const Plan p = plan_of(a, backward, units);
+    if (a.dtype == EWF_F32) run_type<F32>(a, backward, p, stream);
+    else if (a.dtype == EWF_F16) run_type<F16>(a, backward, p, stream);
+    else run_type<BF16>(a, backward, p, stream);
 }
 
 }  // namespace ewf

@@ -401,6 +401,26 @@ def test_recurrence_and_its_gradient(B, T, D, dtype, tied):
         check_rec_grad(c, h, dh, None, d)
 
 
+@pytest.mark.parametrize("B,T,D,dtype,tied", (
+    (8, 2100, 1000, "bf16", True), (8, 2100, 1000, "f16", False), (8, 2100, 500, "f32", True),      # chains of long and of wide tiles
+    (8, 150, 2000, "bf16", False), (16, 300, 600, "f32", True),                                    # a workgroup for a strip
+    (1, 9000, 9, "f32", True), (2, 5000, 70, "bf16", False)))                                      # few chains of many tiles
+def test_recurrence_of_many_tiles(B, T, D, dtype, tied):
+    say("recurrence", B, T, D, dtype, tied)
+    g = gen(B + T + D)
+    for lengths in (None, [T - (T * k) // (2 * B) for k in range(B)]):
+        c = rec_case(g, B, T, D, DT[dtype], tied, lengths)
+        h, last = rec_forward(c)
+        on = check_rec(c, h, last)
+        assert (h[~on] == 7).all()
+        dh, dlast = randn(g, B, T, D, dtype=DT[dtype]), randn(g, B, D)
+        d = rec_backward(c, h, dh, dlast)
+        check_rec_grad(c, h, dh, dlast, d)
+        again = rec_forward(c), rec_backward(c, h, dh, dlast)
+        assert torch.equal(again[0][0], h) and torch.equal(again[0][1], last)
+        assert all(torch.equal(again[1][k], d[k]) for k in d if d[k] is not None)
+
+
 @pytest.mark.parametrize("T", (3, 40, 700))
 def test_recurrence_lengths_out_of_range_and_what_lies_behind(T):
     g = gen(T)
