@@ -6,9 +6,10 @@ namespace ewf {
 namespace {
 
 // A row is held by TPR threads, NV vectors of 16 bytes each: vector j of thread t begins at element
-// (j TPR + t) V.  Workgroups of 256 threads (1024 where a row needs them) hold G = threads / TPR rows at once.
-template <int TPR> struct Shape {
-    static constexpr int threads = TPR > 256 ? TPR : 256;
+// (j TPR + t) V.  A workgroup holds G = threads / TPR rows at once.
+constexpr int kThreads = 512;
+template <int TPR> struct Held {
+    static constexpr int threads = TPR > kThreads ? TPR : kThreads;
     static constexpr int groups = threads / TPR;
     static constexpr int waves = threads / 64;
 };
@@ -34,12 +35,12 @@ EWF_OPS_DEV float row_sum(float x, float *lds)
 
 // ------------------------------------------------------------------ forward
 
-template <typename T, int TPR, int NV>
-__global__ void __launch_bounds__(Shape<TPR>::threads) k_norm(NormLaunch a)
+template <typename T, int TPR, int NV, bool CUT, bool KEPT>
+__global__ void __launch_bounds__(Held<TPR>::threads) k_norm(NormLaunch a)
 {
-    constexpr int V = Vec16<T>::V, G = Shape<TPR>::groups;
+    constexpr int V = Vec16<T>::V, G = Held<TPR>::groups;
     typedef typename T::raw raw;
-    __shared__ float red[2][Shape<TPR>::waves];
+    __shared__ float red[2][Held<TPR>::waves];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.r.cols;
     const bool pf32 = a.param_dtype == EWF_F32, e4m3 = a.code_dtype == EWF_E4M3;
     float w[NV][V], b[NV][V];
@@ -48,61 +49,63 @@ __global__ void __launch_bounds__(Shape<TPR>::threads) k_norm(NormLaunch a)
         const int c = (j * TPR + t) * V;
 #pragma unroll
         for (int e = 0; e < V; e++) { w[j][e] = 1.f; b[j][e] = 0.f; }
-        if (a.weight) load_params<T>(a.weight, pf32, c, cols, w[j]);
-        if (a.bias) load_params<T>(a.bias, pf32, c, cols, b[j]);
+        if (a.weight) load_params<T, CUT>(a.weight, pf32, c, cols, w[j]);
+        if (a.bias) load_params<T, CUT>(a.bias, pf32, c, cols, b[j]);
     }
-    u32x4 x[NV];
+    u32x4 next[NV];
     auto fetch = [&](uint32_t row) {
         const raw *p = (const raw *)a.x + row_offset(a.r, row, a.sx);
 #pragma unroll
-        for (int j = 0; j < NV; j++) x[j] = load_part<T>(p, (j * TPR + t) * V, cols, a.nt);
+        for (int j = 0; j < NV; j++) next[j] = load_part<T, CUT>(p, (j * TPR + t) * V, cols, a.nt);
     };
+#pragma unroll
+    for (int j = 0; j < NV; j++) next[j] = u32x4{0u, 0u, 0u, 0u};
     uint32_t base = blockIdx.x * G;
     if (base + g < a.r.rows) fetch(base + g);
     // (the same number of trips in every thread of a workgroup: row_sum synchronises it)
     for (; base < a.r.rows; base += gridDim.x * G) {
         const uint32_t row = base + g;
         const bool live = row < a.r.rows;
-        float s = 0.f;
-        u32x4 now[NV];
+        float f[NV][V], s = 0.f;                         // the elements; less the mean
 #pragma unroll
-        for (int j = 0; j < NV; j++) {
-            now[j] = live ? x[j] : u32x4{0u, 0u, 0u, 0u};
+        for (int j = 0; j < NV; j++)
 #pragma unroll
-            for (int e = 0; e < V; e++) s += element<T>(now[j], e);
-        }
-        const uint64_t next = (uint64_t)row + (uint64_t)gridDim.x * G;
-        if (next < a.r.rows) fetch((uint32_t)next);      // in flight during this row's sums
+            for (int e = 0; e < V; e++) { f[j][e] = element<T>(next[j], e); s += f[j][e]; }   // (zeros behind the row's end)
+        const uint64_t then = (uint64_t)row + (uint64_t)gridDim.x * G;
+        if (then < a.r.rows) fetch((uint32_t)then);      // in flight during this row
         const float mean = row_sum<TPR>(s, red[0]) / (float)cols;
         float q = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int c = (j * TPR + t) * V;
+            float part = 0.f;
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const float d = element<T>(now[j], e) - mean;
-                if (c + e < cols) q = fmaf(d, d, q);
+                f[j][e] -= mean;
+                if (!CUT || c + e < cols) part = fmaf(f[j][e], f[j][e], part);
             }
+            if (!CUT && c >= cols) part = 0.f;
+            q += part;
         }
         const float rstd = 1.f / sqrtf(row_sum<TPR>(q, red[1]) / (float)cols + a.eps);
-        raw *y = (raw *)a.y + (live ? row_offset(a.r, row, a.sy) : 0);
-        uint8_t *codes = a.codes + (live ? row_offset(a.r, row, a.scodes) : 0);
-        uint8_t *scales = a.scales + (live ? row_offset(a.r, row, a.sscales) : 0);
         const int end = live ? cols : 0;
+        const uint32_t at = live ? row : 0;
+        raw *y = (raw *)a.y + row_offset(a.r, at, a.sy);
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int c = (j * TPR + t) * V;
             float n[V], o[V];
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                n[e] = (element<T>(now[j], e) - mean) * rstd;
+                n[e] = f[j][e] * rstd;
                 o[e] = fmaf(n[e], w[j][e], b[j][e]);
             }
-            if (c < end) store_part<T>(y, c, end, pack16<T>(o), a.nt);
-            if (a.codes) {
+            if (c < end) store_part<T, CUT>(y, c, end, pack16<T>(o), a.nt);
+            if constexpr (KEPT) {
+                if (CUT || c >= end)
 #pragma unroll
-                for (int e = 0; e < V; e++) n[e] = c + e < end ? n[e] : 0.f;
-                keep_part<V>(codes, scales, c, end, n, e4m3);
+                    for (int e = 0; e < V; e++) n[e] = c + e < end ? n[e] : 0.f;
+                keep_part<V, CUT>(a.codes + row_offset(a.r, at, a.scodes), a.scales + row_offset(a.r, at, a.sscales), c, end, n, e4m3);
             }
         }
         if (live && t == 0) {
@@ -192,12 +195,12 @@ EWF_OPS_DEV void normalised(const NormLaunch &a, u32x4 x, float mean, float rstd
 
 // One sweep over dy and x: a workgroup takes rows in turn and its threads keep their columns' sums for dweight and
 // dbias in registers; what remains across workgroups is one partial per workgroup, folded by k_norm_finish.
-template <typename T, int TPR, int NV>
-__global__ void __launch_bounds__(Shape<TPR>::threads) k_norm_grad(NormLaunch a)
+template <typename T, int TPR, int NV, bool CUT, bool KEPT>
+__global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
 {
-    constexpr int V = Vec16<T>::V, G = Shape<TPR>::groups;
+    constexpr int V = Vec16<T>::V, G = Held<TPR>::groups;
     typedef typename T::raw raw;
-    __shared__ float red[2][Shape<TPR>::waves];
+    __shared__ float red[2][Held<TPR>::waves];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.r.cols;
     const bool sums = a.partials != nullptr;
     float w[NV][V], dw[NV][V], db[NV][V];
@@ -205,63 +208,88 @@ __global__ void __launch_bounds__(Shape<TPR>::threads) k_norm_grad(NormLaunch a)
     for (int j = 0; j < NV; j++) {
 #pragma unroll
         for (int e = 0; e < V; e++) { w[j][e] = 1.f; dw[j][e] = 0.f; db[j][e] = 0.f; }
-        if (a.weight) load_params<T>(a.weight, a.param_dtype == EWF_F32, (j * TPR + t) * V, cols, w[j]);
+        if (a.weight) load_params<T, CUT>(a.weight, a.param_dtype == EWF_F32, (j * TPR + t) * V, cols, w[j]);
     }
-    u32x4 dy[NV], x[NV];
-    u32x2 code[NV];
-    uint32_t byte[NV];
-    float mean = 0.f, rstd = 0.f;
+    // (workgroups of 1024 threads have 128 registers a thread, which do not hold a second row)
+    constexpr bool kAhead = TPR < 1024;
+    struct Row {
+        u32x4 dy[NV], x[NV];
+        u32x2 code[NV];
+        uint32_t byte[NV];
+        float mean, rstd;
+    } next;
     auto fetch = [&](uint32_t row) {
         const raw *pd = (const raw *)a.dy + row_offset(a.r, row, a.sdy);
-#pragma unroll
-        for (int j = 0; j < NV; j++) dy[j] = load_part<T>(pd, (j * TPR + t) * V, cols, a.nt);
-        if (a.codes) {
+        next.rstd = a.rstd[row_offset(a.r, row, a.srstd)];
+        next.mean = 0.f;
+        if constexpr (KEPT) {
             const uint8_t *pc = a.codes + row_offset(a.r, row, a.scodes), *ps = a.scales + row_offset(a.r, row, a.sscales);
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int c = (j * TPR + t) * V;
-                code[j] = load_codes<V>(pc, c, cols);
-                byte[j] = c < cols ? ps[c / kKeepBlock] : 0;
+                next.dy[j] = load_part<T, CUT>(pd, c, cols, a.nt);
+                next.code[j] = load_codes<V, CUT>(pc, c, cols);
+                next.byte[j] = c < cols ? ps[c / kKeepBlock] : 0;
             }
         } else {
             const raw *px = (const raw *)a.x + row_offset(a.r, row, a.sx);
+            next.mean = a.mean[row_offset(a.r, row, a.smean)];
 #pragma unroll
-            for (int j = 0; j < NV; j++) x[j] = load_part<T>(px, (j * TPR + t) * V, cols, a.nt);
-            mean = a.mean[row_offset(a.r, row, a.smean)];
+            for (int j = 0; j < NV; j++) {
+                next.dy[j] = load_part<T, CUT>(pd, (j * TPR + t) * V, cols, a.nt);
+                next.x[j] = load_part<T, CUT>(px, (j * TPR + t) * V, cols, a.nt);
+            }
         }
-        rstd = a.rstd[row_offset(a.r, row, a.srstd)];
     };
-    for (uint32_t base = blockIdx.x * G; base < a.r.rows; base += gridDim.x * G) {
+    uint32_t base = blockIdx.x * G;
+    if (kAhead && base + g < a.r.rows) fetch(base + g);
+    for (; base < a.r.rows; base += gridDim.x * G) {
         const uint32_t row = base + g;
         const bool live = row < a.r.rows;
-        if (live) fetch(row);
-        const int end = live ? cols : 0;
-        float n[NV][V], s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int j = 0; j < NV; j++) {
-            const int c = (j * TPR + t) * V;
-            normalised<T>(a, x[j], mean, rstd, code[j], byte[j], n[j]);
+        if (!kAhead && live) fetch(row);
+        const Row now = next;
+        const uint64_t then = (uint64_t)row + (uint64_t)gridDim.x * G;
+        if (kAhead && then < a.r.rows) fetch((uint32_t)then);   // in flight during this row
+        const float rstd = now.rstd;
+        // n, and g = dy weight: kept for the second half, or, where rows are cut, computed again (kernels of rows that are cut need the
+        // registers: float16 [20011, 1001] 40 us and 58, where two workgroups share a unit and where they do not; bfloat16
+        // [16384, 4096], kept, 77, computed again, 80)
+        float gr[NV][V], n[NV][V], s1 = 0.f, s2 = 0.f;
+        auto elements = [&](int j) {
+            if constexpr (KEPT) decode_part<V>(now.code[j], now.byte[j], a.code_dtype == EWF_E4M3, n[j]);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const bool in = c + e < end;
-                const float d = in ? element<T>(dy[j], e) : 0.f, ne = in ? n[j][e] : 0.f, gr = d * w[j][e];
-                n[j][e] = ne;
-                s1 += gr;
-                s2 = fmaf(gr, ne, s2);
-                dw[j][e] = fmaf(d, ne, dw[j][e]);
-                db[j][e] += d;
+                if constexpr (!KEPT) n[j][e] = (element<T>(now.x[j], e) - now.mean) * rstd;
+                gr[j][e] = element<T>(now.dy[j], e) * w[j][e];
+            }
+        };
+        if (live) {
+            // (behind the row's end dy is zero, and n is finite wherever the row's own are)
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                elements(j);
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const float d = element<T>(now.dy[j], e);
+                    s1 += gr[j][e];
+                    s2 = fmaf(gr[j][e], n[j][e], s2);
+                    dw[j][e] = fmaf(d, n[j][e], dw[j][e]);
+                    db[j][e] += d;
+                }
             }
         }
         const float m1 = row_sum<TPR>(s1, red[0]) / (float)cols;
         const float m2 = row_sum<TPR>(s2, red[1]) / (float)cols;
-        raw *dx = (raw *)a.dx + (live ? row_offset(a.r, row, a.sdx) : 0);
+        if (!live) continue;
+        raw *dx = (raw *)a.dx + row_offset(a.r, row, a.sdx);
 #pragma unroll
         for (int j = 0; j < NV; j++) {
             const int c = (j * TPR + t) * V;
             float o[V];
+            if constexpr (CUT) elements(j);
 #pragma unroll
-            for (int e = 0; e < V; e++) o[e] = rstd * (fmaf(-n[j][e], m2, element<T>(dy[j], e) * w[j][e] - m1));
-            if (c < end) store_part<T>(dx, c, end, pack16<T>(o), a.nt);
+            for (int e = 0; e < V; e++) o[e] = rstd * fmaf(-n[j][e], m2, gr[j][e] - m1);
+            if (c < cols) store_part<T, CUT>(dx, c, cols, pack16<T>(o), a.nt);
         }
     }
     if (!sums) return;
@@ -288,7 +316,7 @@ __global__ void __launch_bounds__(Shape<TPR>::threads) k_norm_grad(NormLaunch a)
         }
     } else {
         constexpr int L = TPR < 64 ? TPR : 64;                      // lanes of a wavefront with columns of their own
-        constexpr int groups = TPR <= 64 ? Shape<TPR>::waves : G;   // rows left
+        constexpr int groups = TPR <= 64 ? Held<TPR>::waves : G;   // rows left
         __shared__ float sum[NV * TPR * V];
         const int who = TPR <= 64 ? (int)(threadIdx.x >> 6) : g;
         const bool holds = (int)(threadIdx.x & 63) < L;
@@ -307,7 +335,7 @@ __global__ void __launch_bounds__(Shape<TPR>::threads) k_norm_grad(NormLaunch a)
                 }
             }
             __syncthreads();
-            for (int c = threadIdx.x; c < a.padded; c += Shape<TPR>::threads) mine[part * a.padded + c] = sum[c];
+            for (int c = threadIdx.x; c < a.padded; c += Held<TPR>::threads) mine[part * a.padded + c] = sum[c];
         }
     }
 }
@@ -446,36 +474,30 @@ __global__ void __launch_bounds__(kFinishWaves * 64) k_norm_finish(NormLaunch a)
 
 // ------------------------------------------------------------------ which kernel
 
-// The threads of a row: the fewest that hold it in four vectors each (0: none do).  At least the 32 / V lanes
-// that share a scale.
-int row_threads(int cols, int V, int most)
+constexpr int kVectors = 2;
+
+// The threads of a row: the fewest that hold it in two vectors each (0: none do), and at least the 32 / V lanes that
+// share a scale.
+int row_threads(int cols, int V)
 {
     const int need = (cols + V - 1) / V;
-    for (int tpr : {kKeepBlock / V, 16, 64, 256}) if (need <= 4 * tpr) return tpr;
-    return need <= most * 1024 ? 1024 : 0;
+    for (int tpr = 8; tpr <= 1024; tpr *= 2) if (need <= kVectors * tpr) return tpr;
+    return 0;
 }
 
-template <typename F, typename T, int TPR>
-bool with_vectors(F &&f, int need, int most)
-{
-    if (need <= TPR) return f.template operator()<T, TPR, 1>(), true;
-    if (need <= 2 * TPR) return f.template operator()<T, TPR, 2>(), true;
-    if (need <= 4 * TPR && most >= 4) return f.template operator()<T, TPR, 4>(), true;
-    return false;
-}
-
-// Calls f<T, TPR, NV>() for the row's shape; false where no workgroup holds it.
+// Calls f<T, TPR, 2>() for the row's shape; false where no workgroup holds it.
 template <typename T, typename F>
-bool with_shape(F &&f, int cols, int most)
+bool with_shape(F &&f, int cols)
 {
-    constexpr int V = Vec16<T>::V;
-    const int need = (cols + V - 1) / V;
-    switch (row_threads(cols, V, most)) {
-    case kKeepBlock / V: return with_vectors<F, T, kKeepBlock / V>(f, need, 4);
-    case 16: return with_vectors<F, T, 16>(f, need, 4);
-    case 64: return with_vectors<F, T, 64>(f, need, 4);
-    case 256: return with_vectors<F, T, 256>(f, need, 4);
-    case 1024: return with_vectors<F, T, 1024>(f, need, most);
+    switch (row_threads(cols, Vec16<T>::V)) {
+    case 8: return f.template operator()<T, 8, kVectors>(), true;
+    case 16: return f.template operator()<T, 16, kVectors>(), true;
+    case 32: return f.template operator()<T, 32, kVectors>(), true;
+    case 64: return f.template operator()<T, 64, kVectors>(), true;
+    case 128: return f.template operator()<T, 128, kVectors>(), true;
+    case 256: return f.template operator()<T, 256, kVectors>(), true;
+    case 512: return f.template operator()<T, 512, kVectors>(), true;
+    case 1024: return f.template operator()<T, 1024, kVectors>(), true;
     }
     return false;
 }
@@ -488,38 +510,40 @@ void with_type(F &&f, int dtype)
     else f.template operator()<BF16>();
 }
 
-// Workgroups of 1024 threads have 128 registers a thread: what they hold of a row in the backward pass (the
-// elements, the parameters and two sums each) must fit those.
-int grad_vectors(int dtype) { return dtype == EWF_F32 ? 4 : 2; }
-
 uint32_t at_most(uint64_t n, uint32_t cap) { return (uint32_t)(n < cap ? n : cap); }
 
+template <bool CUT>
 struct Forward {
     const NormLaunch &a;
+    int units;
     hipStream_t stream;
     template <typename T, int TPR, int NV> void operator()() const
     {
-        constexpr int G = Shape<TPR>::groups;
-        const uint32_t blocks = at_most(((uint64_t)a.r.rows + G - 1) / G, 2048);
-        hipLaunchKernelGGL((k_norm<T, TPR, NV>), dim3(blocks), dim3(Shape<TPR>::threads), 0, stream, a);
+        constexpr int G = Held<TPR>::groups;
+        const dim3 grid(at_most(((uint64_t)a.r.rows + G - 1) / G, 2 * (uint32_t)units)), block(Held<TPR>::threads);
+        if (a.codes) hipLaunchKernelGGL((k_norm<T, TPR, NV, CUT, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_norm<T, TPR, NV, CUT, false>), grid, block, 0, stream, a);
     }
     template <typename T> void operator()() const
     {
-        if (with_shape<T>(*this, a.r.cols, 4)) return;
+        if (with_shape<T>(*this, a.r.cols)) return;
         hipLaunchKernelGGL(k_norm_long<T>, dim3(at_most(a.r.rows, 4096)), dim3(kLongThreads), 0, stream, a);
     }
 };
 
+template <bool CUT>
 struct Backward {
     const NormLaunch &a;
     hipStream_t stream;
     template <typename T, int TPR, int NV> void operator()() const
     {
-        hipLaunchKernelGGL((k_norm_grad<T, TPR, NV>), dim3(a.blocks), dim3(Shape<TPR>::threads), 0, stream, a);
+        const dim3 grid(a.blocks), block(Held<TPR>::threads);
+        if (a.codes) hipLaunchKernelGGL((k_norm_grad<T, TPR, NV, CUT, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_norm_grad<T, TPR, NV, CUT, false>), grid, block, 0, stream, a);
     }
     template <typename T> void operator()() const
     {
-        if (a.r.rows && !with_shape<T>(*this, a.r.cols, grad_vectors(a.dtype))) {
+        if (a.r.rows && !with_shape<T>(*this, a.r.cols)) {
             // (the sums first: dx may lie over dy or x)
             const int per = 256 * Vec16<T>::V;
             if (a.partials)
@@ -531,20 +555,33 @@ struct Backward {
     }
 };
 
+// Rows that end inside a vector of 16 bytes have kernels of their own.
+bool is_cut(const NormLaunch &a) { return a.r.cols % (a.dtype == EWF_F32 ? 4 : 8) != 0; }
+
 }  // namespace
 
-void launch_layer_norm(const NormLaunch &a, hipStream_t stream) { with_type(Forward{a, stream}, a.dtype); }
+void launch_layer_norm(const NormLaunch &a, int units, hipStream_t stream) 
+{
+    if (is_cut(a)) with_type(Forward<true>{a, units, stream}, a.dtype);
+    else with_type(Forward<false>{a, units, stream}, a.dtype);
+}
 
 void plan_layer_norm_grad(NormLaunch &a, int units)
 {
     const int V = a.dtype == EWF_F32 ? 4 : 8;
     a.padded = (a.r.cols + 7) / 8 * 8;
-    const int tpr = row_threads(a.r.cols, V, grad_vectors(a.dtype));
-    const int groups = tpr == 0 ? 1 : tpr > 256 ? 1 : 256 / tpr;
+    const int tpr = row_threads(a.r.cols, V);
+    const int groups = tpr == 0 || tpr > kThreads ? 1 : kThreads / tpr;
     const uint64_t trips = ((uint64_t)a.r.rows + groups - 1) / groups;
-    a.blocks = (int)at_most(trips, (uint32_t)(tpr == 0 ? 64 : tpr > 256 ? units : 4 * units));
+    // One workgroup of 512 threads for each unit, two where rows are cut (its kernels have the registers for two): bfloat16
+    // [16384, 4096] 77 and 83 us, [16384, 1024] 26.6 and 28.7; float16 [20011, 1001] 53 and 40.  More leave more partials.
+    a.blocks = (int)at_most(trips, (uint32_t)(tpr == 0 ? 64 : tpr <= kThreads && is_cut(a) ? 2 * units : units));
 }
 
-void launch_layer_norm_grad(const NormLaunch &a, hipStream_t stream) { with_type(Backward{a, stream}, a.dtype); }
+void launch_layer_norm_grad(const NormLaunch &a, hipStream_t stream) 
+{
+    if (is_cut(a)) with_type(Backward<true>{a, stream}, a.dtype);
+    else with_type(Backward<false>{a, stream}, a.dtype);
+}
 
 }  // namespace ewf

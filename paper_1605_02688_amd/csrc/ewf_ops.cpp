@@ -420,7 +420,7 @@ ewf_status ewf_layer_norm(const ewf_layer_norm_args *a, void *hip_stream)
         ewf_status st = norm_layout(a, false, n);
         if (st != EWF_OK) return st;
         if (n.r.rows == 0) return EWF_OK;
-        launch_layer_norm(n, (hipStream_t)hip_stream);
+        launch_layer_norm(n, device_cu_count(), (hipStream_t)hip_stream);
         return launched("layer normalisation");
     });
 }

@@ -61,7 +61,7 @@ struct RecLaunch {
 };
 
 // ---- kernels' launchers (device translation units).  They launch on `stream` and report nothing: the caller asks the runtime.
-void launch_layer_norm(const NormLaunch &a, ihipStream_t *stream);
+void launch_layer_norm(const NormLaunch &a, int units, ihipStream_t *stream);
 // Chooses the backward pass's workgroups: fills blocks and padded.
 void plan_layer_norm_grad(NormLaunch &a, int units);
 void launch_layer_norm_grad(const NormLaunch &a, ihipStream_t *stream);

@@ -122,21 +122,18 @@ EWF_OPS_DEV u32x4 move_down(u32x4 v, int s)
 }
 
 // Elements c .. c + V - 1 of a row of `cols` elements, zeros behind its end.  Rows of whole vectors: one
-// access or none.  Others: every lane reads a whole vector inside the row -- no lane branches around a
-// load, so a row's accesses are in flight together -- and moves it down by what it began too early.
-template <typename T>
+// access or none.  Rows that a vector is CUT by the end of: every lane reads a whole vector inside the row -- no lane
+// branches around a load, so a row's accesses are in flight together -- and moves it down by what it began too early.
+template <typename T, bool CUT = true>
 EWF_OPS_DEV u32x4 load_part(const typename T::raw *row, int c, int cols, bool nt)
 {
     constexpr int V = Vec16<T>::V;
-    if (cols % V == 0) {
-        u32x4 z = {0u, 0u, 0u, 0u};
-        return c < cols ? load16<T>(row + c, nt) : z;
-    }
+    u32x4 r = {0u, 0u, 0u, 0u};
+    if (!CUT || cols % V == 0) return c < cols ? load16<T>(row + c, nt) : r;
     if (cols >= V) {
         const int from = c <= cols - V ? c : cols - V;
         return move_down<T>(load16<T>(row + from, nt), c - from < V ? c - from : V);
     }
-    u32x4 r = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int e = 0; e < V; e++)
         if (c + e < cols) {
@@ -146,12 +143,11 @@ EWF_OPS_DEV u32x4 load_part(const typename T::raw *row, int c, int cols, bool nt
     return r;
 }
 
-template <typename T>
+template <typename T, bool CUT = true>
 EWF_OPS_DEV void store_part(typename T::raw *row, int c, int cols, u32x4 v, bool nt)
 {
     constexpr int V = Vec16<T>::V;
-    if (c + V <= cols) { store16<T>(row + c, v, nt); return; }
-    if (cols % V == 0) return;
+    if (!CUT || c + V <= cols) { store16<T>(row + c, v, nt); return; }
 #pragma unroll
     for (int e = 0; e < V; e++)
         if (c + e < cols) {
@@ -161,19 +157,19 @@ EWF_OPS_DEV void store_part(typename T::raw *row, int c, int cols, u32x4 v, bool
 }
 
 // Parameters: the tensors' type, or float32.  Zeros behind the end.
-template <typename T>
+template <typename T, bool CUT = true>
 EWF_OPS_DEV void load_params(const void *p, bool f32, int c, int cols, float *out)
 {
     constexpr int V = Vec16<T>::V;
     if (f32) {
 #pragma unroll
         for (int q = 0; q < V; q += 4) {
-            u32x4 w = load_part<F32>((const float *)p, c + q, cols, false);
+            u32x4 w = load_part<F32, CUT>((const float *)p, c + q, cols, false);
 #pragma unroll
             for (int e = 0; e < 4; e++) out[q + e] = element<F32>(w, e);
         }
     } else {
-        u32x4 w = load_part<T>((const typename T::raw *)p, c, cols, false);
+        u32x4 w = load_part<T, CUT>((const typename T::raw *)p, c, cols, false);
 #pragma unroll
         for (int e = 0; e < V; e++) out[e] = element<T>(w, e);
     }
@@ -265,7 +261,7 @@ EWF_OPS_DEV float scale_unit(uint32_t byte) { return bits_to_float(byte << 23); 
 
 // Writes the V elements f (zeros behind the row's end) of a lane as codes, and once a block its scale.  A block of 32
 // is 32 / V neighbouring lanes, all of which take part; c is a multiple of V.
-template <int V>
+template <int V, bool CUT = true>
 EWF_OPS_DEV void keep_part(uint8_t *codes, uint8_t *scales, int c, int cols, const float *f, bool e4m3)
 {
     uint32_t top = 0;
@@ -286,7 +282,7 @@ EWF_OPS_DEV void keep_part(uint8_t *codes, uint8_t *scales, int c, int cols, con
     if (c + V <= cols) {
         if constexpr (V == 8) *reinterpret_cast<u32x2_a1 *>(codes + c) = u32x2{w[0], w[1]};
         else *reinterpret_cast<u32_a1 *>(codes + c) = w[0];
-    } else {
+    } else if constexpr (CUT) {
 #pragma unroll
         for (int e = 0; e < V; e++)
             if (c + e < cols) codes[c + e] = (uint8_t)(w[e >> 2] >> ((e & 3) * 8));
@@ -295,14 +291,14 @@ EWF_OPS_DEV void keep_part(uint8_t *codes, uint8_t *scales, int c, int cols, con
 }
 
 // The raw codes of a lane's V elements: zeros behind the row's end.
-template <int V>
+template <int V, bool CUT = true>
 EWF_OPS_DEV u32x2 load_codes(const uint8_t *codes, int c, int cols)
 {
     u32x2 w = {0u, 0u};
     if (c + V <= cols) {
         if constexpr (V == 8) w = *reinterpret_cast<const u32x2_a1 *>(codes + c);
         else w[0] = *reinterpret_cast<const u32_a1 *>(codes + c);
-    } else {
+    } else if constexpr (CUT) {
 #pragma unroll
         for (int e = 0; e < V; e++)
             if (c + e < cols) w[e >> 2] |= (uint32_t)codes[c + e] << ((e & 3) * 8);
