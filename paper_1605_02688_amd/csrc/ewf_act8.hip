@@ -5,8 +5,6 @@ namespace ewf {
 
 namespace {
 
-constexpr float kLog2E = 1.44269504f;
-
 // 1 / (1 + 2^(-x log2 e)) with native exp2 and reciprocal: relative error 2^-24 (2 + |x|) or so
 EWF_OPS_DEV float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2E)); }
 
@@ -27,8 +25,8 @@ EWF_OPS_DEV float act_slope(float x)
 {
     if constexpr (ACT == EWF_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
     else if constexpr (ACT == EWF_ACT_TANH) { const float t = tanhf(x); return fmaf(-t, t, 1.f); }
-    else if constexpr (ACT == EWF_ACT_SIGMOID) { const float p = sigmoid(x); return p * sigmoid(-x); }
-    else if constexpr (ACT == EWF_SILU) { const float p = sigmoid(x); return fmaf(x * p, sigmoid(-x), p); }
+    else if constexpr (ACT == EWF_ACT_SIGMOID) { float p, m; gate(x, p, m); return p * m; }
+    else if constexpr (ACT == EWF_SILU) { float p, m; gate(x, p, m); return fmaf(x * p, m, p); }
     else if constexpr (ACT == EWF_GELU) {
         const float density = 0.39894228f * __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2E));
         return fmaf(x, density, 0.5f + 0.5f * erff(x * 0.70710678f));
@@ -49,52 +47,75 @@ EWF_OPS_DEV Place place(uint32_t item, const Items &i, int V)
     return {i.row0 + row, (int)(item - row * i.per_row) * V};
 }
 
-template <typename T, int ACT>
+template <typename T, int ACT, int U>
 __global__ void __launch_bounds__(256) k_act(ActLaunch a, Items items)
 {
     constexpr int V = Vec16<T>::V;
     typedef typename T::raw raw;
-    const uint32_t item = blockIdx.x * 256 + threadIdx.x;
-    const bool live = item < items.count;                    // (all lanes of a scale's group or none)
-    const Place at = live ? place(item, items, V) : Place{0, 0};
-    const int cols = live ? a.r.cols : 0, c = at.c;
-    u32x4 x = {0u, 0u, 0u, 0u};
-    if (c < cols) x = load_part<T>((const raw *)a.x + row_offset(a.r, at.row, a.sx), c, cols, a.nt);
-    float f[V];
+    Place at[U];
+    u32x4 x[U];
+    const int cols = a.r.cols;
 #pragma unroll
-    for (int e = 0; e < V; e++) f[e] = element<T>(x, e);
-    if (a.codes)
-        keep_part<V>(a.codes + row_offset(a.r, at.row, a.scodes), a.scales + row_offset(a.r, at.row, a.sscales), c, cols, f,
-                     a.code_dtype == EWF_E4M3);
-    if (a.y && c < cols) {
+    for (int i = 0; i < U; i++) {
+        const uint32_t item = (blockIdx.x * U + i) * 256 + threadIdx.x;
+        at[i] = item < items.count ? place(item, items, V) : Place{items.row0, cols};    // (all lanes of a scale's group or none)
+        x[i] = u32x4{0u, 0u, 0u, 0u};
+        if (at[i].c < cols) x[i] = load_part<T>((const raw *)a.x + row_offset(a.r, at[i].row, a.sx), at[i].c, cols, a.nt);
+    }
 #pragma unroll
-        for (int e = 0; e < V; e++) f[e] = act_value<ACT>(f[e]);
-        store_part<T>((raw *)a.y + row_offset(a.r, at.row, a.sy), c, cols, pack16<T>(f), a.nt);
+    for (int i = 0; i < U; i++) {
+        const int c = at[i].c;
+        float f[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) f[e] = element<T>(x[i], e);
+        if (a.codes)
+            keep_part<V>(a.codes + row_offset(a.r, at[i].row, a.scodes), a.scales + row_offset(a.r, at[i].row, a.sscales), c, cols, f,
+                         a.code_dtype == EWF_E4M3);
+        if (a.y && c < cols) {
+#pragma unroll
+            for (int e = 0; e < V; e++) f[e] = act_value<ACT>(f[e]);
+            store_part<T>((raw *)a.y + row_offset(a.r, at[i].row, a.sy), c, cols, pack16<T>(f), a.nt);
+        }
     }
 }
 
 // dx = dy act'(x8); without dy: x8 itself.
-template <typename T, int ACT>
+template <typename T, int ACT, int U>
 __global__ void __launch_bounds__(256) k_act_grad(ActLaunch a, Items items)
 {
     constexpr int V = Vec16<T>::V;
     typedef typename T::raw raw;
-    const uint32_t item = blockIdx.x * 256 + threadIdx.x;
-    if (item >= items.count) return;
-    const Place at = place(item, items, V);
-    const int cols = a.r.cols, c = at.c;
-    if (c >= cols) return;
-    u32x4 dy = {0u, 0u, 0u, 0u};
-    if (a.dy) dy = load_part<T>((const raw *)a.dy + row_offset(a.r, at.row, a.sdy), c, cols, a.nt);
-    const u32x2 code = load_codes<V>(a.codes + row_offset(a.r, at.row, a.scodes), c, cols);
-    const uint32_t byte = a.scales[row_offset(a.r, at.row, a.sscales) + c / kKeepBlock];
-    float f[V];
-    decode_part<V>(code, byte, a.code_dtype == EWF_E4M3, f);
-    if (a.dy) {
+    Place at[U];
+    u32x4 dy[U];
+    u32x2 code[U];
+    uint32_t byte[U];
+    const int cols = a.r.cols;
 #pragma unroll
-        for (int e = 0; e < V; e++) f[e] = element<T>(dy, e) * act_slope<ACT>(f[e]);
+    for (int i = 0; i < U; i++) {
+        const uint32_t item = (blockIdx.x * U + i) * 256 + threadIdx.x;
+        at[i] = item < items.count ? place(item, items, V) : Place{items.row0, cols};
+        dy[i] = u32x4{0u, 0u, 0u, 0u};
+        code[i] = u32x2{0u, 0u};
+        byte[i] = 0;
+        const int c = at[i].c;
+        if (c < cols) {
+            if (a.dy) dy[i] = load_part<T>((const raw *)a.dy + row_offset(a.r, at[i].row, a.sdy), c, cols, a.nt);
+            code[i] = load_codes<V>(a.codes + row_offset(a.r, at[i].row, a.scodes), c, cols);
+            byte[i] = a.scales[row_offset(a.r, at[i].row, a.sscales) + c / kKeepBlock];
+        }
     }
-    store_part<T>((raw *)a.dx + row_offset(a.r, at.row, a.sdx), c, cols, pack16<T>(f), a.nt);
+#pragma unroll
+    for (int i = 0; i < U; i++) {
+        const int c = at[i].c;
+        if (c >= cols) continue;
+        float f[V];
+        decode_part<V>(code[i], byte[i], a.code_dtype == EWF_E4M3, f);
+        if (a.dy) {
+#pragma unroll
+            for (int e = 0; e < V; e++) f[e] = element<T>(dy[i], e) * act_slope<ACT>(f[e]);
+        }
+        store_part<T>((raw *)a.dx + row_offset(a.r, at[i].row, a.sdx), c, cols, pack16<T>(f), a.nt);
+    }
 }
 
 template <typename T, int ACT, bool GRAD>
@@ -108,13 +129,14 @@ void run(const ActLaunch &a, hipStream_t stream)
     i.shift = 31 + s;
     i.mul = (uint32_t)((((uint64_t)1 << i.shift) + i.per_row - 1) / i.per_row);
     // launches of fewer than 2^31 items each
-    const uint32_t most = 0x7fffff00u / i.per_row;
+    const uint32_t most = 0x7ffff000u / i.per_row;
     for (uint32_t row = 0; row < a.r.rows; row += i.count / i.per_row) {
         i.row0 = row;
         i.count = (a.r.rows - row < most ? a.r.rows - row : most) * i.per_row;
-        const dim3 grid((i.count + 255) / 256);
-        if constexpr (GRAD) hipLaunchKernelGGL((k_act_grad<T, ACT>), grid, dim3(256), 0, stream, a, i);
-        else hipLaunchKernelGGL((k_act<T, ACT>), grid, dim3(256), 0, stream, a, i);
+        constexpr uint32_t U = 1, per = 256 * U;
+        const dim3 grid((i.count + per - 1) / per);
+        if constexpr (GRAD) hipLaunchKernelGGL((k_act_grad<T, ACT, U>), grid, dim3(256), 0, stream, a, i);
+        else hipLaunchKernelGGL((k_act<T, ACT, U>), grid, dim3(256), 0, stream, a, i);
     }
 }
 

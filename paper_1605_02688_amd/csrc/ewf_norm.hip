@@ -450,11 +450,11 @@ __global__ void __launch_bounds__(kFinishWaves * 64) k_norm_finish(NormLaunch a)
     if (at < wide) {
         const float *p = a.partials + at;
         int k = wave;
-        for (; k + 3 * kFinishWaves < a.blocks; k += 4 * kFinishWaves) {
-            float v[4];
+        for (; k + 7 * kFinishWaves < a.blocks; k += 8 * kFinishWaves) {
+            float v[8];
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = p[(int64_t)(k + i * kFinishWaves) * wide];
-            s += (v[0] + v[1]) + (v[2] + v[3]);
+            for (int i = 0; i < 8; i++) v[i] = p[(int64_t)(k + i * kFinishWaves) * wide];
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
         for (; k < a.blocks; k += kFinishWaves) s += p[(int64_t)k * wide];
     }
@@ -575,7 +575,10 @@ void plan_layer_norm_grad(NormLaunch &a, int units)
     const uint64_t trips = ((uint64_t)a.r.rows + groups - 1) / groups;
     // One workgroup of 512 threads for each unit, two where rows are cut (its kernels have the registers for two): bfloat16
     // [16384, 4096] 77 and 83 us, [16384, 1024] 26.6 and 28.7; float16 [20011, 1001] 53 and 40.  More leave more partials.
-    a.blocks = (int)at_most(trips, (uint32_t)(tpr == 0 ? 64 : tpr <= kThreads && is_cut(a) ? 2 * units : units));
+    const uint64_t most = tpr == 0 ? 64 : tpr <= kThreads && is_cut(a) ? 2 * units : units;
+    // the fewest that take no more rows each: 513 trips by 512 workgroups are two trips for the longest, and by 257 as well
+    const uint64_t each = (trips + most - 1) / most;
+    a.blocks = each ? (int)((trips + each - 1) / each) : 0;
 }
 
 void launch_layer_norm_grad(const NormLaunch &a, hipStream_t stream) 

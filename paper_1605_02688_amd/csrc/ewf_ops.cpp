@@ -3,7 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
+#include <cstring>
 #include <initializer_list>
 
 #include "ewf_internal.h"
@@ -34,7 +34,9 @@ struct Operand8 {
 
 // The tensors of one call, checked one by one as they are added.
 struct Call {
-    std::vector<Operand8> ops;
+    // (no heap: the checks are made on every call)
+    Operand8 ops[16];
+    size_t n = 0;
     ewf_status status = EWF_OK;
 
     ewf_status fail(ewf_status s) { return status = s; }
@@ -64,12 +66,12 @@ struct Call {
             o.view.str[d] = t.shape[d] > 1 ? t.strides[d] : 0;
             if (t.shape[d] > 1) span += (double)(t.shape[d] - 1) * (double)t.strides[d];
         }
-        if (empty) { ops.push_back(o); return true; }
+        if (empty) { ops[n++] = o; return true; }
         if (!t.ptr) { set_error("%s: null pointer", name); fail(EWF_EINVAL); return false; }
         if ((uintptr_t)t.ptr % (unsigned)isz) { set_error("%s: the pointer is not aligned to its element", name); fail(EWF_EINVAL); return false; }
         if (span * isz >= 0x1p62) { set_error("%s: its extents and strides reach beyond the address space", name); fail(EWF_ESHAPE); return false; }
         if (out && !self_disjoint(o.view)) { set_error("%s: two of its elements share memory", name); fail(EWF_EALIAS); return false; }
-        ops.push_back(o);
+        ops[n++] = o;
         return true;
     }
     bool add(const char *name, const ewf_tensor &t, int isz, std::initializer_list<int64_t> shape, bool out, bool required)
@@ -92,13 +94,13 @@ struct Call {
     ewf_status check_results(std::initializer_list<std::pair<const char *, const char *>> allowed)
     {
         if (status != EWF_OK) return status;
-        for (size_t o = 0; o < ops.size(); o++) {
+        for (size_t o = 0; o < n; o++) {
             if (!ops[o].out) continue;
-            for (size_t k = 0; k < ops.size(); k++) {
+            for (size_t k = 0; k < n; k++) {
                 if (k == o || (ops[k].out && k > o) || !views_overlap(ops[k].view, ops[o].view)) continue;
                 bool ok = false;
                 for (auto &p : allowed)
-                    ok = ok || (!ops[k].out && std::string(p.first) == ops[o].name && std::string(p.second) == ops[k].name &&
+                    ok = ok || (!ops[k].out && !strcmp(p.first, ops[o].name) && !strcmp(p.second, ops[k].name) &&
                                 ops[k].view.rank == ops[o].view.rank && same_view(ops[k].view, ops[o].view));
                 if (ok) continue;
                 set_error("%s overlaps %s", ops[o].name, ops[k].name);
@@ -111,9 +113,10 @@ struct Call {
 
 // The axes before the last of the row tensors, merged into at most two that all of them share.
 struct RowLayout {
-    struct Entry { const char *name; const ewf_tensor *t; RowStride *to; };
-    std::vector<Entry> e;
-    void add(const char *name, const ewf_tensor &t, RowStride *to) { if (present(t)) e.push_back({name, &t, to}); }
+    struct Entry { const ewf_tensor *t; RowStride *to; };
+    Entry e[8];
+    size_t n = 0;
+    void add(const ewf_tensor &t, RowStride *to) { if (present(t)) e[n++] = {&t, to}; }
 
     ewf_status merge(const int64_t *shape, int lead, Rows &r)
     {
@@ -121,25 +124,25 @@ struct RowLayout {
         for (int d = 0; d < lead; d++) total *= (double)shape[d];
         if (total > (double)kMaxRows) { set_error("%.0f rows: fewer than 2^31 are supported", total); return EWF_ESHAPE; }
         if (total == 0) { r.rows = 0; r.n1 = 1; return EWF_OK; }
-        struct Axis { int64_t ext; std::vector<int64_t> st; };
-        std::vector<Axis> axes;
+        struct Axis { int64_t ext, st[8]; } axes[kMaxDims];
+        int naxes = 0;
         for (int d = 0; d < lead; d++) {
             if (shape[d] == 1) continue;
-            Axis a{shape[d], {}};
-            for (auto &x : e) a.st.push_back(x.t->strides[d]);
-            if (!axes.empty()) {
-                bool ok = true;
-                for (size_t k = 0; k < e.size(); k++) ok = ok && axes.back().st[k] == a.st[k] * a.ext;
-                if (ok) { axes.back().ext *= a.ext; axes.back().st = a.st; continue; }
-            }
-            axes.push_back(a);
+            Axis &a = axes[naxes];
+            a.ext = shape[d];
+            for (size_t k = 0; k < n; k++) a.st[k] = e[k].t->strides[d];
+            bool ok = naxes > 0;
+            for (size_t k = 0; ok && k < n; k++) ok = axes[naxes - 1].st[k] == a.st[k] * a.ext;
+            if (!ok) { naxes++; continue; }
+            a.ext *= axes[naxes - 1].ext;
+            axes[naxes - 1] = a;
         }
-        if (axes.size() > 2) { set_error("the axes before the last do not merge into two that all tensors share"); return EWF_EUNSUPPORTED; }
+        if (naxes > 2) { set_error("the axes before the last do not merge into two that all tensors share"); return EWF_EUNSUPPORTED; }
         r.rows = (uint32_t)total;
-        r.n1 = axes.empty() ? 1 : (uint32_t)axes.back().ext;
-        for (size_t k = 0; k < e.size(); k++) {
-            e[k].to->inner = axes.empty() ? 0 : axes.back().st[k];
-            e[k].to->outer = axes.size() == 2 ? axes[0].st[k] : 0;
+        r.n1 = naxes ? (uint32_t)axes[naxes - 1].ext : 1;
+        for (size_t k = 0; k < n; k++) {
+            e[k].to->inner = naxes ? axes[naxes - 1].st[k] : 0;
+            e[k].to->outer = naxes == 2 ? axes[0].st[k] : 0;
         }
         return EWF_OK;
     }
@@ -188,8 +191,8 @@ ewf_status kept_pair(Call &c, RowLayout &l, const ewf_tensor &codes, const ewf_t
     c.add("scales", scales, 1, nd, ks, out, required);
     c.unit_last(codes, "codes", nd);
     c.unit_last(scales, "scales", nd);
-    l.add("codes", codes, sc);
-    l.add("scales", scales, ss);
+    l.add(codes, sc);
+    l.add(scales, ss);
     return c.status;
 }
 
@@ -217,10 +220,10 @@ ewf_status norm_layout(const ewf_layer_norm_args *a, bool grad, NormLaunch &n)
     auto full = [&](const char *name, const ewf_tensor &t, bool out, bool required, RowStride *to) {
         if (!c.add(name, t, isz, nd, shape, out, required)) return;
         c.unit_last(t, name, nd);
-        l.add(name, t, to);
+        l.add(t, to);
     };
     auto stat = [&](const char *name, const ewf_tensor &t, bool out, bool required, RowStride *to) {
-        if (c.add(name, t, 4, nd - 1, shape, out, required)) l.add(name, t, to);
+        if (c.add(name, t, 4, nd - 1, shape, out, required)) l.add(t, to);
     };
     auto param = [&](const char *name, const ewf_tensor &t, bool out) {
         if (c.add(name, t, psz, {cols}, out, false)) c.unit_last(t, name, 1);
@@ -291,7 +294,7 @@ ewf_status act_layout(const ewf_activation_args *a, ActCall call, ActLaunch &n)
     auto full = [&](const char *name, const ewf_tensor &t, bool out, bool required, RowStride *to) {
         if (!c.add(name, t, isz, nd, shape, out, required)) return;
         c.unit_last(t, name, nd);
-        l.add(name, t, to);
+        l.add(t, to);
     };
     if (call == ActCall::Forward) {
         if (!present(a->y) && !present(a->codes)) { set_error("y, or codes and scales, are needed"); return EWF_EINVAL; }

@@ -205,6 +205,20 @@ EWF_OPS_DEV float group_sum(float x)
     return x;
 }
 
+// ------------------------------------------------------------------ sigmoids
+
+constexpr float kLog2E = 1.44269504f;
+
+// f = sigmoid(u) and 1 - f, both to within a few units in the last place: e = 2^(-u log2 e), f = 1 / (1 + e),
+// 1 - f = e f.  e is kept finite (a gate of less than 2^-126 counts as that); a NaN stays one.
+EWF_OPS_DEV void gate(float u, float &f, float &g)
+{
+    float e = __builtin_amdgcn_exp2f(-u * kLog2E);
+    e = e > 0x1p126f ? 0x1p126f : e;
+    f = __builtin_amdgcn_rcpf(1.f + e);
+    g = e * f;
+}
+
 // ------------------------------------------------------------------ 8 bits
 
 // Magnitudes are compared as their bits, which rank NaN above infinity above every number.

@@ -12,18 +12,6 @@ void aux_fill_zero(void *ptr, size_t nbytes, hipStream_t stream);
 
 namespace {
 
-constexpr float kLog2E = 1.44269504f;
-
-// f = sigmoid(u) and 1 - f, both to within a few units in the last place: e = 2^(-u log2 e), f = 1 / (1 + e),
-// 1 - f = e f.  e is kept finite (a gate of less than 2^-126 counts as that); a NaN stays one.
-EWF_OPS_DEV void gate(float u, float &f, float &g)
-{
-    float e = __builtin_amdgcn_exp2f(-u * kLog2E);
-    e = e > 0x1p126f ? 0x1p126f : e;
-    f = __builtin_amdgcn_rcpf(1.f + e);
-    g = e * f;
-}
-
 // ------------------------------------------------------------------ a lane's channels
 //
 // A lane takes C neighbouring channels, 8 bytes of them.  Where fewer are left it reads the last C of the row and drops
