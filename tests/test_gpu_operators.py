@@ -534,3 +534,186 @@ def test_recurrence_of_no_steps():
     run(ewf.recurrence_grad, u, torch.empty_like(u), torch.empty_like(u), torch.empty_like(u), torch.empty_like(u), torch.empty_like(u),
         dlast=h0, dh0=dh0)
     assert torch.equal(dh0, h0)
+
+
+# ------------------------------------------------------------------ streams, graphs, several calls at once
+
+def small_calls(g):
+    """One bound call of every operator on tensors of its own: [(call, results)]."""
+    bf = torch.bfloat16
+    made = []
+
+    def bound(op, results, *args, **kw):
+        made.append((op.bind(*args, workspace=work_for(op, *args, **kw), **kw), results))
+
+    x, w, b = randn(g, 300, 1000, dtype=bf), randn(g, 1000), randn(g, 1000)
+    y, mean, rstd = torch.empty_like(x), torch.empty(300, device="cuda"), torch.empty(300, device="cuda")
+    codes, scales = torch.empty((300, 1000), dtype=torch.int8, device="cuda"), torch.empty((300, 32), dtype=torch.uint8, device="cuda")
+    bound(ewf.layer_norm, (y, mean, rstd, codes, scales), x, w, b, y, mean=mean, rstd=rstd, codes=codes, scales=scales)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    bound(ewf.layer_norm_grad, (dx, dw, db), y, w, rstd, dx, dweight=dw, dbias=db, codes=codes, scales=scales)
+    z, zc, zs = torch.empty_like(x), torch.empty((300, 1000), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((300, 32), dtype=torch.uint8, device="cuda")
+    bound(ewf.activation, (z, zc, zs), "gelu", y, z, codes=zc, scales=zs)
+    dz, back = torch.empty_like(x), torch.empty_like(x)
+    bound(ewf.activation_grad, (dz,), "gelu", dx, dz, codes=zc, scales=zs)
+    bound(ewf.read8, (back,), zc, zs, back)
+    c = rec_case(g, 3, 700, 130, bf, False, [700, 0, 123])
+    h, last, dh, dlast = torch.zeros_like(c["u"]), torch.empty(3, 130, device="cuda"), randn(g, 3, 700, 130, dtype=bf), randn(g, 3, 130)
+    bound(ewf.recurrence, (h, last), c["u"], c["v"], h, w=c["w"], h0=c["h0"], last=last, lengths=c["lengths"])
+    du, dv, dq = (torch.zeros_like(c["u"]) for _ in range(3))
+    dh0 = torch.empty(3, 130, device="cuda")
+    bound(ewf.recurrence_grad, (du, dv, dq, dh0), c["u"], c["v"], h, dh, du, dv, w=c["w"], dw=dq, h0=c["h0"], dh0=dh0, dlast=dlast, lengths=c["lengths"])
+    return made
+
+
+def clear(calls):
+    for _, results in calls:
+        for r in results:
+            r.view(torch.uint8).zero_()
+
+
+def test_all_operators_in_a_captured_graph():
+    calls = small_calls(gen(50))
+    for call, _ in calls:
+        call.launch(stream())
+    torch.cuda.synchronize()
+    eager = [[r.clone() for r in results] for _, results in calls]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            for call, _ in calls:
+                call.launch(side.cuda_stream)
+    torch.cuda.current_stream().wait_stream(side)
+    for replay in range(4):
+        clear(calls)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for (_, results), want in zip(calls, eager):
+            for r, e in zip(results, want):
+                assert torch.equal(r.view(torch.uint8), e.view(torch.uint8)), replay
+        # eager work and the same operators between the replays, the workspaces left dirty
+        assert torch.isfinite(torch.randn(1 << 16, device="cuda").sum())
+        for call, _ in calls:
+            call.launch(stream())
+        torch.cuda.synchronize()
+
+
+def test_calls_on_several_streams_at_once():
+    sets = [small_calls(gen(60 + k)) for k in range(3)]
+    for calls in sets:
+        for call, _ in calls:
+            call.launch(stream())
+    torch.cuda.synchronize()
+    want = [[[r.clone() for r in results] for _, results in calls] for calls in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for calls in sets:
+        clear(calls)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, calls in zip(streams, sets):
+            for call, _ in calls:
+                call.launch(s.cuda_stream)
+    torch.cuda.synchronize()
+    for calls, w in zip(sets, want):
+        for (_, results), e in zip(calls, w):
+            assert all(torch.equal(r.view(torch.uint8), x.view(torch.uint8)) for r, x in zip(results, e))
+
+
+def test_long_recurrences_on_two_streams_at_once():
+    # chains whose tiles wait for each other, twice, side by side
+    g = gen(70)
+    made = []
+    for k in range(2):
+        c = rec_case(g, 1, 20000, 300, torch.float32, True, None)
+        h, last = torch.empty_like(c["u"]), torch.empty(1, 300, device="cuda")
+        args, kw = (c["u"], c["v"], h), dict(h0=c["h0"], last=last)
+        made.append((ewf.recurrence.bind(*args, workspace=work_for(ewf.recurrence, *args, **kw), **kw), h, last))
+    want = []
+    for call, h, last in made:
+        call.launch(stream())
+        torch.cuda.synchronize()
+        want.append((h.clone(), last.clone()))
+        h.zero_()
+    streams = [torch.cuda.Stream() for _ in made]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for s, (call, _, _) in zip(streams, made):
+            call.launch(s.cuda_stream)
+    torch.cuda.synchronize()
+    for (call, h, last), (wh, wl) in zip(made, want):
+        assert torch.equal(h, wh) and torch.equal(last, wl)
+
+
+def test_workspace_of_the_wrong_size_is_refused():
+    g = gen(71)
+    c = rec_case(g, 1, 5000, 64, torch.bfloat16, True, None)
+    h = torch.empty_like(c["u"])
+    n = ewf.recurrence.workspace_bytes(c["u"], c["v"], h)
+    assert n > 16
+    with pytest.raises(ewf.EwfError) as e:
+        ewf.recurrence(c["u"], c["v"], h, workspace=torch.empty(n - 16, dtype=torch.uint8, device="cuda"), stream=stream())
+    assert e.value.status == ewf.ENOMEM
+
+
+# ------------------------------------------------------------------ all together
+
+def test_a_block_of_a_recurrent_language_model():
+    """Norm, gates, recurrence, activation, projection and the loss of the expressions, forward and backward, with 8 bits
+    kept of the norm's rows and of the activation's argument; each step against the formulas in 64 bits, on what the
+    step before it handed over."""
+    from workloads import configs as wl
+    import tests.harness as hn
+    g = gen(80)
+    B, T, D, H, V = 3, 90, 96, 80, 200
+    x = randn(g, B, T, D, mean=0.2)
+    lw, lb = randn(g, D, mean=1, std=0.2), randn(g, D, std=0.2)
+    wu, wv, wo = (randn(g, D, H, std=D ** -0.5), randn(g, D, H, std=D ** -0.5), randn(g, H, V, std=H ** -0.5))
+    target = torch.randint(0, V, (B * T,), generator=g, device="cuda", dtype=torch.int32)
+    dev = dict(device="cuda")
+    n8, ns = torch.empty(B, T, D, dtype=torch.int8, **dev), torch.empty(B, T, 3, dtype=torch.uint8, **dev)
+    y, rstd = torch.empty_like(x), torch.empty(B, T, **dev)
+    run(ewf.layer_norm, x, lw, lb, y, rstd=rstd, codes=n8, scales=ns)
+    p = torch.empty(B, T, 2 * H, **dev)                              # both gates' projections beside each other
+    torch.matmul(y.view(-1, D), torch.cat((wu, wv), 1), out=p.view(-1, 2 * H))
+    u, v = p[:, :, :H], p[:, :, H:]
+    h, last = torch.empty(B, T, H, **dev), torch.empty(B, H, **dev)
+    run(ewf.recurrence, u, v, h, last=last)
+    z, zc, zs = torch.empty_like(h), torch.empty(B, T, H, dtype=torch.int8, **dev), torch.empty(B, T, 3, dtype=torch.uint8, **dev)
+    run(ewf.activation, "silu", h, z, codes=zc, scales=zs)
+    logits = z.view(-1, H) @ wo
+    # the loss's gradient is one of the library's expressions: softmax minus one-hot, by ewf_grad
+    w = wl.layout_only(wl.c3_softmax_xent_backward, rows=B * T, vocab=V)
+    expr = ewf.Expression(w.spec)
+    ins = [logits, target.view(-1, 1)]
+    (dlogits,) = outs = hn.alloc_outputs(expr, w.spec, ins)
+    expr.run(ins, outs, w.scalars, hn.make_workspace(expr, ins, outs), stream())
+    dz = (dlogits @ wo.t()).view(B, T, H)
+    dh = torch.empty_like(h)
+    run(ewf.activation_grad, "silu", dz, dh, codes=zc, scales=zs)
+    dp = torch.empty_like(p)
+    run(ewf.recurrence_grad, u, v, h, dh, dp[:, :, :H], dp[:, :, H:])
+    dy = (dp.view(-1, 2 * H) @ torch.cat((wu, wv), 1).t()).view(B, T, D)
+    dx, dlw, dlb = torch.empty_like(x), torch.empty_like(lw), torch.empty_like(lb)
+    run(ewf.layer_norm_grad, dy, lw, rstd, dx, dweight=dlw, dbias=dlb, codes=n8, scales=ns)
+    # each step against the formulas on the values that the step before it handed over
+    want = check_norm(x, lw, lb, y, None, None)
+    check_rec(dict(u=u, v=v, w=None, h0=None, lengths=None), h, last)
+    ev, _ = ref.act_bounds("silu", h.double())
+    ref.close("z", z, ref.ACTS["silu"][0](h.double()), ref.stored(ev, z.double(), torch.float32))
+    _, zbyte, h8, _ = ref.keep8(h, "i8")
+    assert torch.equal(zs, zbyte)
+    _, es = ref.act_bounds("silu", h8)
+    wdh = dz.double() * ref.ACTS["silu"][1](h8)
+    ref.close("dh", dh, wdh, ref.stored(dz.double().abs() * es + ref.U * wdh.abs(), wdh, torch.float32))
+    check_rec_grad(dict(u=u, v=v, w=None, h0=None, lengths=None), h, dh, None,
+                   dict(du=dp[:, :, :H], dv=dp[:, :, H:], dw=None, dh0=ref.recurrence_grad(u, v, None, h, None, dh, None, None, torch.float32)["dh0"]))
+    n = torch.empty(B, T, D, **dev)
+    run(ewf.read8, n8, ns, n)
+    _, byte, _, unit = ref.keep8(want["n"], "i8")
+    ref.close("n", n, want["n"], (0.5 if torch.equal(byte, ns) else 1.0) * unit * (1 + 1e-6) + 2 * want["e_n"])
+    soft = torch.softmax(logits.double(), 1)
+    soft[torch.arange(B * T, device="cuda"), target.long()] -= 1
+    hn.compare("dlogits", dlogits.cpu().numpy(), (soft / (B * T)).float().cpu().numpy(), 1e-5, 1e-9)
+    check_norm_grad(dy, None, lw, None, rstd, dx, dlw, dlb, torch.float32, n=n)
