@@ -5,9 +5,6 @@ namespace ewf {
 
 namespace {
 
-// 1 / (1 + 2^(-x log2 e)) with native exp2 and reciprocal: relative error 2^-24 (2 + |x|) or so
-EWF_OPS_DEV float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2E)); }
-
 template <int ACT>
 EWF_OPS_DEV float act_value(float x)
 {

@@ -219,6 +219,9 @@ EWF_OPS_DEV void gate(float u, float &f, float &g)
     g = e * f;
 }
 
+// sigmoid alone: 1 / (1 + 2^(-x log2 e)); e may overflow, and the result is then zero
+EWF_OPS_DEV float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2E)); }
+
 // ------------------------------------------------------------------ 8 bits
 
 // Magnitudes are compared as their bits, which rank NaN above infinity above every number.

@@ -307,10 +307,12 @@ struct Tile {
 
     EWF_OPS_DEV void step_map(const Raw<T, BACK> &x, int e, float &f, float &b) const
     {
-        float i, less;
-        gate(x.u[e], f, i);
-        if constexpr (BACK) b = f * x.dh[e];
-        else {
+        if constexpr (BACK) {
+            f = sigmoid(x.u[e]);
+            b = f * x.dh[e];
+        } else {
+            float i, less;
+            gate(x.u[e], f, i);
             if constexpr (!TIED) gate(x.w[e], i, less);
             b = i * x.v[e];
         }
@@ -462,7 +464,9 @@ __global__ void __launch_bounds__(W * 64) k_rec_march(RecLaunch a)
 //
 // The wait ends: a workgroup draws its place in the chain when it runs, so that all tiles before it belong to workgroups
 // that run or are done, and it publishes its own map before it waits; the first tile waits for none, and each next one
-// only for words that workgroups publish without waiting, or after a wait that has ended.
+// only for words that workgroups publish without waiting, or after a wait that has ended.  Where a caller breaks the
+// rule that overlapping calls have workspaces of their own, words can be lost: a wait is given up after kMostLooks
+// looks (seconds; a tile takes microseconds), and the channel's states from there on are NaN.
 
 constexpr uint32_t kMapBit = 1u << 30, kStateBit = 1u << 31;
 
@@ -484,18 +488,21 @@ EWF_OPS_DEV uint64_t look(const uint64_t *p) { return __hip_atomic_load(p, __ATO
 // bits wherever the search ends.  Four records are looked at together: their loads overlap (eight and sixteen cost
 // more traffic than they save).
 constexpr int kLook = 4;
+constexpr int kMostLooks = 1 << 22;
 
 EWF_OPS_DEV float search(const uint64_t *record, int64_t back, int place)
 {
+    constexpr uint64_t kNone = (uint64_t)0x7fc00000u << 32 | kStateBit;    // before the first tile, which publishes a state: never reached
     uint64_t w[kLook];
-    int from = place - 1;
+    int from = place - 1, looks = 0;
     for (bool known = false; ; from -= kLook) {
 #pragma unroll
-        for (int q = 0; q < kLook; q++) w[q] = from >= q ? look(record - (place - from + q) * back) : 0;
+        for (int q = 0; q < kLook; q++) w[q] = from >= q ? look(record - (place - from + q) * back) : kNone;
 #pragma unroll
         for (int q = 0; q < kLook; q++) {
             if (known) break;
-            while (is_empty(w[q])) {                    // (never before the first tile, which publishes a state)
+            while (is_empty(w[q])) {
+                if (++looks > kMostLooks) return bits_to_float(0x7fc00000u);
                 __builtin_amdgcn_s_sleep(1);
                 w[q] = look(record - (place - from + q) * back);
             }

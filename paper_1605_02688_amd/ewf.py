@@ -790,6 +790,9 @@ class BoundOperator:
     tensors alive."""
 
     def __init__(self, operator: "Operator", filler: _Filler, workspace=None, stream: int = 0):
+        device = getattr(workspace, "device", None)
+        if device is not None and filler._device is not None and device != filler._device:
+            _refuse(EINVAL, f"workspace: on {device}, the tensors on {filler._device}")
         self._keep = (filler, workspace)
         self._ref = ctypes.byref(filler.args)
         self._fn = operator._fn
