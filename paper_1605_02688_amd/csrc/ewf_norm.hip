@@ -474,30 +474,36 @@ __global__ void __launch_bounds__(kFinishWaves * 64) k_norm_finish(NormLaunch a)
 
 // ------------------------------------------------------------------ which kernel
 
-constexpr int kVectors = 2;
+// Threads and vectors a thread of a row.
+struct RowShape { int threads, vectors; };
 
-// The threads of a row: the fewest that hold it in two vectors each (0: none do), and at least the 32 / V lanes that
-// share a scale.
-int row_threads(int cols, int V)
+// The fewest vectors that hold the row, by 8 (the lanes that share a scale, at most) to 1024 threads of two, or 32 to 512
+// threads of three (0: none do).  bfloat16 rows on T threads of three vectors and on 2 T of two, us: forward [16384, 4608] 61 and 66,
+// [16384, 1400] 18.9 and 21.1, [16384, 6144] 77.6 and 77.7.  Backward three vectors take registers for their sums: worth it where two
+// vectors of twice the threads would stand half empty ([16384, 4608] 86 and 98; [16384, 6144] 120 and 111, [16384, 1400] 35 and 33) and
+// where that would be 1024 threads, whose registers do not hold two ([8192, 12000] 120 and 206); rows that are cut have none left
+// over (float16 [20011, 1301] 82 and 67).
+RowShape row_shape(int cols, int V, bool backward)
 {
     const int need = (cols + V - 1) / V;
-    for (int tpr = 8; tpr <= 1024; tpr *= 2) if (need <= kVectors * tpr) return tpr;
-    return 0;
+    for (int tpr = 8; tpr <= 1024; tpr *= 2) {
+        if (need <= 2 * tpr) return {tpr, 2};
+        if (need > 3 * tpr || tpr < 32 || tpr > 512) continue;
+        if (!backward || tpr == 512 || (2 * need <= 5 * tpr && cols % V == 0)) return {tpr, 3};
+    }
+    return {0, 0};
 }
 
-// Calls f<T, TPR, 2>() for the row's shape; false where no workgroup holds it.
+// Calls f<T, threads, vectors>() for the row's shape; false where no workgroup holds it.
 template <typename T, typename F>
-bool with_shape(F &&f, int cols)
+bool with_shape(F &&f, int cols, bool backward)
 {
-    switch (row_threads(cols, Vec16<T>::V)) {
-    case 8: return f.template operator()<T, 8, kVectors>(), true;
-    case 16: return f.template operator()<T, 16, kVectors>(), true;
-    case 32: return f.template operator()<T, 32, kVectors>(), true;
-    case 64: return f.template operator()<T, 64, kVectors>(), true;
-    case 128: return f.template operator()<T, 128, kVectors>(), true;
-    case 256: return f.template operator()<T, 256, kVectors>(), true;
-    case 512: return f.template operator()<T, 512, kVectors>(), true;
-    case 1024: return f.template operator()<T, 1024, kVectors>(), true;
+    const RowShape s = row_shape(cols, Vec16<T>::V, backward);
+    switch (s.threads * 4 + s.vectors) {
+#define EWF_ROW(TPR, NV) case TPR * 4 + NV: return f.template operator()<T, TPR, NV>(), true;
+    EWF_ROW(8, 2) EWF_ROW(16, 2) EWF_ROW(32, 2) EWF_ROW(32, 3) EWF_ROW(64, 2) EWF_ROW(64, 3) EWF_ROW(128, 2) EWF_ROW(128, 3)
+    EWF_ROW(256, 2) EWF_ROW(256, 3) EWF_ROW(512, 2) EWF_ROW(512, 3) EWF_ROW(1024, 2)
+#undef EWF_ROW
     }
     return false;
 }
@@ -526,7 +532,7 @@ struct Forward {
     }
     template <typename T> void operator()() const
     {
-        if (with_shape<T>(*this, a.r.cols)) return;
+        if (with_shape<T>(*this, a.r.cols, false)) return;
         hipLaunchKernelGGL(k_norm_long<T>, dim3(at_most(a.r.rows, 4096)), dim3(kLongThreads), 0, stream, a);
     }
 };
@@ -543,7 +549,7 @@ struct Backward {
     }
     template <typename T> void operator()() const
     {
-        if (a.r.rows && !with_shape<T>(*this, a.r.cols)) {
+        if (a.r.rows && !with_shape<T>(*this, a.r.cols, true)) {
             // (the sums first: dx may lie over dy or x)
             const int per = 256 * Vec16<T>::V;
             if (a.partials)
@@ -570,7 +576,7 @@ void plan_layer_norm_grad(NormLaunch &a, int units)
 {
     const int V = a.dtype == EWF_F32 ? 4 : 8;
     a.padded = (a.r.cols + 7) / 8 * 8;
-    const int tpr = row_threads(a.r.cols, V);
+    const int tpr = row_shape(a.r.cols, V, true).threads;
     const int groups = tpr == 0 || tpr > kThreads ? 1 : kThreads / tpr;
     const uint64_t trips = ((uint64_t)a.r.rows + groups - 1) / groups;
     // One workgroup of 512 threads for each unit, two where rows are cut (its kernels have the registers for two): bfloat16

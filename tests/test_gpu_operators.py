@@ -40,8 +40,8 @@ def run(op, *args, **kw):
 # ------------------------------------------------------------------ layer normalisation
 
 # each side of: one vector, the threads of a row with one, two and four vectors, whole and cut vectors
-NORM_COLS = (1, 2, 3, 7, 8, 9, 31, 32, 33, 64, 100, 128, 129, 256, 257, 300, 512, 513, 1000, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8199,
-             16384, 16390, 32768, 32771, 40005)
+NORM_COLS = (1, 2, 3, 7, 8, 9, 31, 32, 33, 64, 100, 128, 129, 256, 257, 300, 512, 513, 600, 1000, 1024, 1025, 1152, 1300, 2048, 2049, 2304,
+             4096, 4097, 4608, 6144, 8192, 8199, 10000, 12001, 16384, 16390, 32768, 32771, 40005)
 
 
 def norm_case(g, rows, cols, dtype, params):
