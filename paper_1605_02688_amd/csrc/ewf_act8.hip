@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(256) k_act(ActLaunch a, Items items)
         const uint32_t item = (blockIdx.x * U + i) * 256 + threadIdx.x;
         at[i] = item < items.count ? place(item, items, V) : Place{items.row0, cols};    // (all lanes of a scale's group or none)
         x[i] = u32x4{0u, 0u, 0u, 0u};
-        if (at[i].c < cols) x[i] = load_part<T>((const raw *)a.x + row_offset(a.r, at[i].row, a.sx), at[i].c, cols, a.nt);
+        if (at[i].c < cols) x[i] = load_part<T>((const raw *)a.x + row_offset(a.r, at[i].row, a.sx), at[i].c, cols);
     }
 #pragma unroll
     for (int i = 0; i < U; i++) {
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256) k_act(ActLaunch a, Items items)
         if (a.y && c < cols) {
 #pragma unroll
             for (int e = 0; e < V; e++) f[e] = act_value<ACT>(f[e]);
-            store_part<T>((raw *)a.y + row_offset(a.r, at[i].row, a.sy), c, cols, pack16<T>(f), a.nt);
+            store_part<T>((raw *)a.y + row_offset(a.r, at[i].row, a.sy), c, cols, pack16<T>(f));
         }
     }
 }
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(256) k_act_grad(ActLaunch a, Items items)
         byte[i] = 0;
         const int c = at[i].c;
         if (c < cols) {
-            if (a.dy) dy[i] = load_part<T>((const raw *)a.dy + row_offset(a.r, at[i].row, a.sdy), c, cols, a.nt);
+            if (a.dy) dy[i] = load_part<T>((const raw *)a.dy + row_offset(a.r, at[i].row, a.sdy), c, cols);
             code[i] = load_codes<V>(a.codes + row_offset(a.r, at[i].row, a.scodes), c, cols);
             byte[i] = a.scales[row_offset(a.r, at[i].row, a.sscales) + c / kKeepBlock];
         }
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) k_act_grad(ActLaunch a, Items items)
 #pragma unroll
             for (int e = 0; e < V; e++) f[e] = element<T>(dy[i], e) * act_slope<ACT>(f[e]);
         }
-        store_part<T>((raw *)a.dx + row_offset(a.r, at[i].row, a.sdx), c, cols, pack16<T>(f), a.nt);
+        store_part<T>((raw *)a.dx + row_offset(a.r, at[i].row, a.sdx), c, cols, pack16<T>(f));
     }
 }
 

@@ -33,6 +33,14 @@ EWF_OPS_DEV float row_sum(float x, float *lds)
     }
 }
 
+// Vector j of thread t once its access is there; vectors that lie inside the row in all threads are whole.
+template <typename T, bool CUT, int TPR>
+EWF_OPS_DEV u32x4 settle(u32x4 v, int j, int t, int cols)
+{
+    if (CUT && (j + 1) * TPR * Vec16<T>::V > cols) v = settle_part<T, CUT>(v, (j * TPR + t) * Vec16<T>::V, cols);
+    return v;
+}
+
 // ------------------------------------------------------------------ forward
 
 template <typename T, int TPR, int NV, bool CUT, bool KEPT>
@@ -56,7 +64,7 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm(NormLaunch a)
     auto fetch = [&](uint32_t row) {
         const raw *p = (const raw *)a.x + row_offset(a.r, row, a.sx);
 #pragma unroll
-        for (int j = 0; j < NV; j++) next[j] = load_part<T, CUT>(p, (j * TPR + t) * V, cols, a.nt);
+        for (int j = 0; j < NV; j++) next[j] = fetch_part<T, CUT>(p, (j * TPR + t) * V, cols);
     };
 #pragma unroll
     for (int j = 0; j < NV; j++) next[j] = u32x4{0u, 0u, 0u, 0u};
@@ -68,9 +76,11 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm(NormLaunch a)
         const bool live = row < a.r.rows;
         float f[NV][V], s = 0.f;                         // the elements; less the mean
 #pragma unroll
-        for (int j = 0; j < NV; j++)
+        for (int j = 0; j < NV; j++) {
+            const u32x4 x = settle<T, CUT, TPR>(next[j], j, t, cols);
 #pragma unroll
-            for (int e = 0; e < V; e++) { f[j][e] = element<T>(next[j], e); s += f[j][e]; }   // (zeros behind the row's end)
+            for (int e = 0; e < V; e++) { f[j][e] = element<T>(x, e); s += f[j][e]; }        // (zeros behind the row's end)
+        }
         const uint64_t then = (uint64_t)row + (uint64_t)gridDim.x * G;
         if (then < a.r.rows) fetch((uint32_t)then);      // in flight during this row
         const float mean = row_sum<TPR>(s, red[0]) / (float)cols;
@@ -100,7 +110,7 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm(NormLaunch a)
                 n[e] = f[j][e] * rstd;
                 o[e] = fmaf(n[e], w[j][e], b[j][e]);
             }
-            if (c < end) store_part<T, CUT>(y, c, end, pack16<T>(o), a.nt);
+            if (c < end) store_part<T, CUT>(y, c, end, pack16<T>(o));
             if constexpr (KEPT) {
                 if (CUT || c >= end)
 #pragma unroll
@@ -133,7 +143,7 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(NormLaunch a)
         uint8_t *codes = a.codes + row_offset(a.r, row, a.scodes), *scales = a.scales + row_offset(a.r, row, a.sscales);
         float s = 0.f, q = 0.f;
         for (int64_t at = 0; at < cols; at += step) {
-            const u32x4 v = load_part<T>(x, (int)(at + threadIdx.x * V), cols, false);
+            const u32x4 v = load_part<T>(x, (int)(at + threadIdx.x * V), cols);
             float part = 0.f;
 #pragma unroll
             for (int e = 0; e < V; e++) part += element<T>(v, e);
@@ -142,7 +152,7 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(NormLaunch a)
         const float mean = row_sum<kLongThreads>(s, red[0]) / (float)cols;
         for (int64_t at = 0; at < cols; at += step) {
             const int c = (int)(at + threadIdx.x * V);
-            const u32x4 v = load_part<T>(x, c, cols, false);
+            const u32x4 v = load_part<T>(x, c, cols);
             float part = 0.f;
 #pragma unroll
             for (int e = 0; e < V; e++) {
@@ -154,7 +164,7 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(NormLaunch a)
         const float rstd = 1.f / sqrtf(row_sum<kLongThreads>(q, red[1]) / (float)cols + a.eps);
         for (int64_t at = 0; at < cols; at += step) {
             const int c = (int)(at + threadIdx.x * V);
-            const u32x4 v = load_part<T>(x, c, cols, false);
+            const u32x4 v = load_part<T>(x, c, cols);
             float n[V], o[V], w[V], b[V];
 #pragma unroll
             for (int e = 0; e < V; e++) { w[e] = 1.f; b[e] = 0.f; }
@@ -165,7 +175,7 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(NormLaunch a)
                 n[e] = (element<T>(v, e) - mean) * rstd;
                 o[e] = fmaf(n[e], w[e], b[e]);
             }
-            if (c < cols) store_part<T>(y, c, cols, pack16<T>(o), a.nt);
+            if (c < cols) store_part<T>(y, c, cols, pack16<T>(o));
             if (a.codes) {
 #pragma unroll
                 for (int e = 0; e < V; e++) n[e] = c + e < cols ? n[e] : 0.f;
@@ -227,7 +237,7 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int c = (j * TPR + t) * V;
-                next.dy[j] = load_part<T, CUT>(pd, c, cols, a.nt);
+                next.dy[j] = fetch_part<T, CUT>(pd, c, cols);
                 next.code[j] = load_codes<V, CUT>(pc, c, cols);
                 next.byte[j] = c < cols ? ps[c / kKeepBlock] : 0;
             }
@@ -236,8 +246,8 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
             next.mean = a.mean[row_offset(a.r, row, a.smean)];
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                next.dy[j] = load_part<T, CUT>(pd, (j * TPR + t) * V, cols, a.nt);
-                next.x[j] = load_part<T, CUT>(px, (j * TPR + t) * V, cols, a.nt);
+                next.dy[j] = fetch_part<T, CUT>(pd, (j * TPR + t) * V, cols);
+                next.x[j] = fetch_part<T, CUT>(px, (j * TPR + t) * V, cols);
             }
         }
     };
@@ -247,7 +257,13 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
         const uint32_t row = base + g;
         const bool live = row < a.r.rows;
         if (!kAhead && live) fetch(row);
-        const Row now = next;
+        Row now = next;
+        if constexpr (CUT)
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                now.dy[j] = settle<T, CUT, TPR>(now.dy[j], j, t, cols);
+                if constexpr (!KEPT) now.x[j] = settle<T, CUT, TPR>(now.x[j], j, t, cols);
+            }
         const uint64_t then = (uint64_t)row + (uint64_t)gridDim.x * G;
         if (kAhead && then < a.r.rows) fetch((uint32_t)then);   // in flight during this row
         const float rstd = now.rstd;
@@ -289,7 +305,7 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
             if constexpr (CUT) elements(j);
 #pragma unroll
             for (int e = 0; e < V; e++) o[e] = rstd * fmaf(-n[j][e], m2, gr[j][e] - m1);
-            if (c < cols) store_part<T, CUT>(dx, c, cols, pack16<T>(o), a.nt);
+            if (c < cols) store_part<T, CUT>(dx, c, cols, pack16<T>(o));
         }
     }
     if (!sums) return;
@@ -310,8 +326,8 @@ __global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
             if (c < a.padded)
 #pragma unroll
                 for (int e = 0; e < V; e += 4) {
-                    store16<F32>(mine + c + e, pack16<F32>(&dw[j][e]), false);
-                    store16<F32>(mine + a.padded + c + e, pack16<F32>(&db[j][e]), false);
+                    store16<F32>(mine + c + e, pack16<F32>(&dw[j][e]));
+                    store16<F32>(mine + a.padded + c + e, pack16<F32>(&db[j][e]));
                 }
         }
     } else {
@@ -358,11 +374,11 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_grad_long(NormLaunch a)
         float gr[V], n[V];
         auto part = [&](int64_t at) {
             const int c = (int)(at + threadIdx.x * V);
-            const u32x4 dy = load_part<T>(pd, c, cols, false);
+            const u32x4 dy = load_part<T>(pd, c, cols);
             u32x4 x = {0u, 0u, 0u, 0u};
             u32x2 code = {0u, 0u};
             uint32_t byte = 0;
-            if (!a.codes) x = load_part<T>(px, c, cols, false);
+            if (!a.codes) x = load_part<T>(px, c, cols);
             else if (c < cols) { code = load_codes<V>(pc, c, cols); byte = ps[c / kKeepBlock]; }
             float w[V];
 #pragma unroll
@@ -392,7 +408,7 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_grad_long(NormLaunch a)
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; e++) o[e] = rstd * fmaf(-n[e], m2, gr[e] - m1);
-            if (c < cols) store_part<T>(dx, c, cols, pack16<T>(o), a.nt);
+            if (c < cols) store_part<T>(dx, c, cols, pack16<T>(o));
         }
     }
 }
@@ -408,13 +424,13 @@ __global__ void __launch_bounds__(256) k_norm_grad_columns(NormLaunch a)
 #pragma unroll
     for (int e = 0; e < V; e++) dw[e] = db[e] = 0.f;
     for (uint32_t row = blockIdx.x; row < a.r.rows; row += gridDim.x) {
-        const u32x4 dy = load_part<T>((const raw *)a.dy + row_offset(a.r, row, a.sdy), c, cols, false);
+        const u32x4 dy = load_part<T>((const raw *)a.dy + row_offset(a.r, row, a.sdy), c, cols);
         u32x4 x = {0u, 0u, 0u, 0u};
         u32x2 code = {0u, 0u};
         uint32_t byte = 0;
         float mean = 0.f;
         if (!a.codes) {
-            x = load_part<T>((const raw *)a.x + row_offset(a.r, row, a.sx), c, cols, false);
+            x = load_part<T>((const raw *)a.x + row_offset(a.r, row, a.sx), c, cols);
             mean = a.mean[row_offset(a.r, row, a.smean)];
         } else if (c < cols) {
             code = load_codes<V>(a.codes + row_offset(a.r, row, a.scodes), c, cols);
@@ -432,8 +448,8 @@ __global__ void __launch_bounds__(256) k_norm_grad_columns(NormLaunch a)
     float *mine = a.partials + (size_t)blockIdx.x * 2 * a.padded;
 #pragma unroll
     for (int e = 0; e < V; e += 4) {
-        store16<F32>(mine + c + e, pack16<F32>(&dw[e]), false);
-        store16<F32>(mine + a.padded + c + e, pack16<F32>(&db[e]), false);
+        store16<F32>(mine + c + e, pack16<F32>(&dw[e]));
+        store16<F32>(mine + a.padded + c + e, pack16<F32>(&db[e]));
     }
 }
 
@@ -483,22 +499,23 @@ struct RowShape { int threads, vectors; };
 // vectors of twice the threads would stand half empty ([16384, 4608] 86 and 98; [16384, 6144] 120 and 111, [16384, 1400] 35 and 33) and
 // where that would be 1024 threads, whose registers do not hold two ([8192, 12000] 120 and 206); rows that are cut have none left
 // over (float16 [20011, 1301] 82 and 67).
-RowShape row_shape(int cols, int V, bool backward)
+RowShape row_shape(int cols, int V, bool backward, bool kept)
 {
     const int need = (cols + V - 1) / V;
     for (int tpr = 8; tpr <= 1024; tpr *= 2) {
         if (need <= 2 * tpr) return {tpr, 2};
         if (need > 3 * tpr || tpr < 32 || tpr > 512) continue;
-        if (!backward || tpr == 512 || (2 * need <= 5 * tpr && cols % V == 0)) return {tpr, 3};
+        const bool cut = cols % V != 0;
+        if (backward ? tpr == 512 || (2 * need <= 5 * tpr && !cut) : !cut && !kept) return {tpr, 3};
     }
     return {0, 0};
 }
 
 // Calls f<T, threads, vectors>() for the row's shape; false where no workgroup holds it.
 template <typename T, typename F>
-bool with_shape(F &&f, int cols, bool backward)
+bool with_shape(F &&f, int cols, bool backward, bool kept)
 {
-    const RowShape s = row_shape(cols, Vec16<T>::V, backward);
+    const RowShape s = row_shape(cols, Vec16<T>::V, backward, kept);
     switch (s.threads * 4 + s.vectors) {
 #define EWF_ROW(TPR, NV) case TPR * 4 + NV: return f.template operator()<T, TPR, NV>(), true;
     EWF_ROW(8, 2) EWF_ROW(16, 2) EWF_ROW(32, 2) EWF_ROW(32, 3) EWF_ROW(64, 2) EWF_ROW(64, 3) EWF_ROW(128, 2) EWF_ROW(128, 3)
@@ -532,7 +549,7 @@ struct Forward {
     }
     template <typename T> void operator()() const
     {
-        if (with_shape<T>(*this, a.r.cols, false)) return;
+        if (with_shape<T>(*this, a.r.cols, false, a.codes)) return;
         hipLaunchKernelGGL(k_norm_long<T>, dim3(at_most(a.r.rows, 4096)), dim3(kLongThreads), 0, stream, a);
     }
 };
@@ -549,7 +566,7 @@ struct Backward {
     }
     template <typename T> void operator()() const
     {
-        if (a.r.rows && !with_shape<T>(*this, a.r.cols, true)) {
+        if (a.r.rows && !with_shape<T>(*this, a.r.cols, true, a.codes)) {
             // (the sums first: dx may lie over dy or x)
             const int per = 256 * Vec16<T>::V;
             if (a.partials)
@@ -576,7 +593,7 @@ void plan_layer_norm_grad(NormLaunch &a, int units)
 {
     const int V = a.dtype == EWF_F32 ? 4 : 8;
     a.padded = (a.r.cols + 7) / 8 * 8;
-    const int tpr = row_shape(a.r.cols, V, true).threads;
+    const int tpr = row_shape(a.r.cols, V, true, a.codes).threads;
     const int groups = tpr == 0 || tpr > kThreads ? 1 : kThreads / tpr;
     const uint64_t trips = ((uint64_t)a.r.rows + groups - 1) / groups;
     // One workgroup of 512 threads for each unit, two where rows are cut (its kernels have the registers for two): bfloat16

@@ -17,8 +17,6 @@ constexpr int64_t kMaxCols = (int64_t)1 << 30;
 constexpr int64_t kMaxNormCols = (int64_t)1 << 24;      // what one workgroup's sums are accurate for
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxStepBytes = (int64_t)32 << 20;
-// Operands that a launch touches once, and far more than the caches hold: accesses that leave nothing behind.
-constexpr int64_t kStreamBytes = (int64_t)64 << 20;
 
 int float_size(int t) { return t == EWF_F32 ? 4 : 2; }
 bool is_float(int t) { return t == EWF_F32 || t == EWF_F16 || t == EWF_BF16; }
@@ -261,7 +259,6 @@ ewf_status norm_layout(const ewf_layer_norm_args *a, bool grad, NormLaunch &n)
     n.mean = (float *)a->mean.ptr; n.rstd = (float *)a->rstd.ptr;
     n.codes = (uint8_t *)a->codes.ptr; n.scales = (uint8_t *)a->scales.ptr;
     if (grad && n.codes) { n.x = nullptr; n.mean = nullptr; }
-    n.nt = (double)n.r.rows * (double)cols * isz >= (double)kStreamBytes;
     if (grad) plan_layer_norm_grad(n, device_cu_count());
     return EWF_OK;
 }
@@ -321,7 +318,6 @@ ewf_status act_layout(const ewf_activation_args *a, ActCall call, ActLaunch &n)
     if (st != EWF_OK) return st;
     n.r.cols = (int32_t)cols;
     n.codes = (uint8_t *)a->codes.ptr; n.scales = (uint8_t *)a->scales.ptr;
-    n.nt = (double)n.r.rows * (double)cols * isz >= (double)kStreamBytes;
     return EWF_OK;
 }
 

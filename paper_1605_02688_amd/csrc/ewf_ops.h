@@ -34,7 +34,6 @@ struct NormLaunch {
     float *partials;                     // backward: [blocks][2][padded cols]
     int blocks;                          // backward: workgroups that leave a partial
     int padded;                          // backward: cols rounded up
-    bool nt;                             // operands touched once and far larger than the caches
 };
 
 struct ActLaunch {
@@ -45,7 +44,6 @@ struct ActLaunch {
     void *y, *dx;
     uint8_t *codes, *scales;
     RowStride sx, sy, scodes, sscales, sdy, sdx;
-    bool nt;
 };
 
 struct RecTensor { void *p = nullptr; int64_t batch = 0, step = 0; };

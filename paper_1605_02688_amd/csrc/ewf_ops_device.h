@@ -35,17 +35,15 @@ template <> struct Vec16<F16> { static constexpr int V = 8; typedef u32x4_a2 at;
 template <> struct Vec16<BF16> { static constexpr int V = 8; typedef u32x4_a2 at; };
 
 template <typename T>
-EWF_OPS_DEV u32x4 load16(const typename T::raw *p, bool nt)
+EWF_OPS_DEV u32x4 load16(const typename T::raw *p)
 {
-    const typename Vec16<T>::at *q = reinterpret_cast<const typename Vec16<T>::at *>(p);
-    return nt ? (u32x4)__builtin_nontemporal_load(q) : (u32x4)*q;
+    return *reinterpret_cast<const typename Vec16<T>::at *>(p);
 }
 
 template <typename T>
-EWF_OPS_DEV void store16(typename T::raw *p, u32x4 v, bool nt)
+EWF_OPS_DEV void store16(typename T::raw *p, u32x4 v)
 {
-    typename Vec16<T>::at *q = reinterpret_cast<typename Vec16<T>::at *>(p);
-    if (nt) __builtin_nontemporal_store(v, q); else *q = v;
+    *reinterpret_cast<typename Vec16<T>::at *>(p) = v;
 }
 
 EWF_OPS_DEV float bits_to_float(uint32_t b) { return __builtin_bit_cast(float, b); }
@@ -121,19 +119,16 @@ EWF_OPS_DEV u32x4 move_down(u32x4 v, int s)
     return v;
 }
 
-// Elements c .. c + V - 1 of a row of `cols` elements, zeros behind its end.  Rows of whole vectors: one
-// access or none.  Rows that a vector is CUT by the end of: every lane reads a whole vector inside the row -- no lane
-// branches around a load, so a row's accesses are in flight together -- and moves it down by what it began too early.
+// Elements c .. c + V - 1 of a row of `cols` elements, zeros behind its end, in two steps: the access, and what makes the
+// vector of it, which waits for the access.  Rows that a vector is CUT by the end of: that vector's lane reads the row's last
+// whole vector -- one access as every other, in flight with them -- and moves it down by what it began too early.
 template <typename T, bool CUT = true>
-EWF_OPS_DEV u32x4 load_part(const typename T::raw *row, int c, int cols, bool nt)
+EWF_OPS_DEV u32x4 fetch_part(const typename T::raw *row, int c, int cols)
 {
     constexpr int V = Vec16<T>::V;
     u32x4 r = {0u, 0u, 0u, 0u};
-    if (!CUT || cols % V == 0) return c < cols ? load16<T>(row + c, nt) : r;
-    if (cols >= V) {
-        const int from = c <= cols - V ? c : cols - V;
-        return move_down<T>(load16<T>(row + from, nt), c - from < V ? c - from : V);
-    }
+    if (!CUT || cols % V == 0) return c < cols ? load16<T>(row + c) : r;
+    if (cols >= V) return c < cols ? load16<T>(row + (c <= cols - V ? c : cols - V)) : r;
 #pragma unroll
     for (int e = 0; e < V; e++)
         if (c + e < cols) {
@@ -144,10 +139,25 @@ EWF_OPS_DEV u32x4 load_part(const typename T::raw *row, int c, int cols, bool nt
 }
 
 template <typename T, bool CUT = true>
-EWF_OPS_DEV void store_part(typename T::raw *row, int c, int cols, u32x4 v, bool nt)
+EWF_OPS_DEV u32x4 settle_part(u32x4 v, int c, int cols)
 {
     constexpr int V = Vec16<T>::V;
-    if (!CUT || c + V <= cols) { store16<T>(row + c, v, nt); return; }
+    if (!CUT || cols % V == 0 || cols < V) return v;
+    const int early = c - (cols - V);
+    return move_down<T>(v, early < 0 ? 0 : early < V ? early : V);
+}
+
+template <typename T, bool CUT = true>
+EWF_OPS_DEV u32x4 load_part(const typename T::raw *row, int c, int cols)
+{
+    return settle_part<T, CUT>(fetch_part<T, CUT>(row, c, cols), c, cols);
+}
+
+template <typename T, bool CUT = true>
+EWF_OPS_DEV void store_part(typename T::raw *row, int c, int cols, u32x4 v)
+{
+    constexpr int V = Vec16<T>::V;
+    if (!CUT || c + V <= cols) { store16<T>(row + c, v); return; }
 #pragma unroll
     for (int e = 0; e < V; e++)
         if (c + e < cols) {
@@ -164,12 +174,12 @@ EWF_OPS_DEV void load_params(const void *p, bool f32, int c, int cols, float *ou
     if (f32) {
 #pragma unroll
         for (int q = 0; q < V; q += 4) {
-            u32x4 w = load_part<F32, CUT>((const float *)p, c + q, cols, false);
+            u32x4 w = load_part<F32, CUT>((const float *)p, c + q, cols);
 #pragma unroll
             for (int e = 0; e < 4; e++) out[q + e] = element<F32>(w, e);
         }
     } else {
-        u32x4 w = load_part<T, CUT>((const typename T::raw *)p, c, cols, false);
+        u32x4 w = load_part<T, CUT>((const typename T::raw *)p, c, cols);
 #pragma unroll
         for (int e = 0; e < V; e++) out[e] = element<T>(w, e);
     }
