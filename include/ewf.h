@@ -283,7 +283,8 @@ ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *fail
  * elements and >= 0, nothing is allocated, synchronised or kept between calls, launches go to the caller's stream (of
  * the current device) and may be captured into a HIP graph, sums are folded in a fixed order (equal calls give equal
  * bits), errors are statuses with a text.  A workspace needs no initialisation; calls that may overlap in time must not
- * share one (that includes two captured graphs).
+ * share one (that includes two captured graphs): results are then undefined, and those of a recurrence may come after
+ * seconds of waiting, as NaN.
  *
  * An argument structure is zeroed by the caller and filled in: a tensor whose ptr and shape are both NULL is absent.
  * Tensors are EWF_F32, EWF_F16 or EWF_BF16 as the structure's `dtype` says; arithmetic, sums, statistics and states
@@ -346,6 +347,8 @@ ewf_status ewf_read8(const ewf_activation_args *a, void *hip_stream);
  * updated in place; h may lie over u, v or w.  lengths (optional): int32 [batch] on the device; steps from
  * lengths[b] on (taken as 0 or `steps` where it is outside 0 .. steps) do not exist: what the inputs hold there has no
  * effect, results there are left as they were, and last is the state behind the sequence's own last step.
+ * At most 2^30 steps, fewer than 2^31 sequences times channels (EWF_ESHAPE), steps at most 32 MiB apart
+ * (EWF_EUNSUPPORTED).
  *
  * ewf_recurrence_grad: with G_t the gradient of h_t through all later steps (G = dh at the last step, plus dlast where
  * it is given; G_t = dh_t + f_(t+1) G_(t+1)),

@@ -1,4 +1,8 @@
 // Activations whose argument is kept in 8 bits for the backward pass: element-wise, one pass each way.
+//
+// A lane takes one 16-byte vector and a workgroup of 256 a contiguous piece; two or four vectors a lane are slower (bfloat16 [8192,
+// 8192], both passes, 117, 122 and 128 us), as for a plain copy.  Memory bounds them: forward 6.4 TB/s, backward, which
+// reads three streams for two written, 5.2.
 #include "ewf_ops_device.h"
 
 namespace ewf {

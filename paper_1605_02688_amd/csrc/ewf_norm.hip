@@ -1,4 +1,10 @@
 // Layer normalisation, forward and backward.
+//
+// Forward: mean, then the mean square of what is left of it, from the row in registers: two sums in turn, because a
+// sum of squares about zero loses the variance of rows far from it.  Backward: with g = dy weight and n the normalised
+// row, dx = rstd (g - mean(g) - n mean(g n)); two sums along the row, and down the columns the sums of dy n and dy.
+// Memory bounds both: bfloat16 [16384, 4096] forward 50 us for 268 MB (without its sums 51), backward 72 us for 403 MB and
+// 4 for the fold of the column sums.
 #include "ewf_ops_device.h"
 
 namespace ewf {
