@@ -28,6 +28,7 @@ struct Operand8 {
     const ewf_tensor *t;
     RawView view;
     bool out;
+    uint64_t begin = 0, end = 0;         // of its bytes; equal where it has no elements
 };
 
 // The tensors of one call, checked one by one as they are added.
@@ -52,6 +53,7 @@ struct Call {
         Operand8 o{name, &t, RawView{(uint64_t)(uintptr_t)t.ptr, isz, {0}, {0}, rank}, out};
         bool empty = false;
         double span = 1;
+        uint64_t reach = 1;
         for (int d = 0; d < rank; d++) {
             if (t.shape[d] != shape[d]) {
                 set_error("%s: dimension %d has extent %lld, expected %lld", name, d, (long long)t.shape[d], (long long)shape[d]);
@@ -62,13 +64,26 @@ struct Call {
             if (t.shape[d] == 0) empty = true;
             o.view.ext[d] = t.shape[d];
             o.view.str[d] = t.shape[d] > 1 ? t.strides[d] : 0;
-            if (t.shape[d] > 1) span += (double)(t.shape[d] - 1) * (double)t.strides[d];
+            if (t.shape[d] > 1) {
+                span += (double)(t.shape[d] - 1) * (double)t.strides[d];
+                reach += (uint64_t)(t.shape[d] - 1) * (uint64_t)t.strides[d];
+            }
         }
         if (empty) { ops[n++] = o; return true; }
         if (!t.ptr) { set_error("%s: null pointer", name); fail(EWF_EINVAL); return false; }
         if ((uintptr_t)t.ptr % (unsigned)isz) { set_error("%s: the pointer is not aligned to its element", name); fail(EWF_EINVAL); return false; }
         if (span * isz >= 0x1p62) { set_error("%s: its extents and strides reach beyond the address space", name); fail(EWF_ESHAPE); return false; }
-        if (out && !self_disjoint(o.view)) { set_error("%s: two of its elements share memory", name); fail(EWF_EALIAS); return false; }
+        o.begin = o.view.addr;
+        o.end = o.begin + reach * (uint64_t)isz;
+        // (each axis steps over what the axes behind it span: the usual case, found without sorting)
+        int64_t behind = 0;
+        bool apart = true;
+        for (int d = rank - 1; out && apart && d >= 0; d--) {
+            if (o.view.ext[d] <= 1) continue;
+            apart = o.view.str[d] > behind;
+            behind += (o.view.ext[d] - 1) * o.view.str[d];
+        }
+        if (out && !apart && !self_disjoint(o.view)) { set_error("%s: two of its elements share memory", name); fail(EWF_EALIAS); return false; }
         ops[n++] = o;
         return true;
     }
@@ -95,7 +110,8 @@ struct Call {
         for (size_t o = 0; o < n; o++) {
             if (!ops[o].out) continue;
             for (size_t k = 0; k < n; k++) {
-                if (k == o || (ops[k].out && k > o) || !views_overlap(ops[k].view, ops[o].view)) continue;
+                if (k == o || (ops[k].out && k > o) || ops[k].end <= ops[o].begin || ops[o].end <= ops[k].begin) continue;
+                if (!views_overlap(ops[k].view, ops[o].view)) continue;
                 bool ok = false;
                 for (auto &p : allowed)
                     ok = ok || (!ops[k].out && !strcmp(p.first, ops[o].name) && !strcmp(p.second, ops[k].name) &&

@@ -717,3 +717,43 @@ def test_a_block_of_a_recurrent_language_model():
     soft[torch.arange(B * T, device="cuda"), target.long()] -= 1
     hn.compare("dlogits", dlogits.cpu().numpy(), (soft / (B * T)).float().cpu().numpy(), 1e-5, 1e-9)
     check_norm_grad(dy, None, lw, None, rstd, dx, dlw, dlb, torch.float32, n=n)
+
+
+# ------------------------------------------------------------------ beyond 2^31 elements
+
+def test_tensors_of_more_than_2_31_elements():
+    bf = torch.bfloat16
+    g = gen(90)
+    rows, cols = 2_000_003, 1100
+    say("layer norm and codes", rows, cols)
+    x = torch.randn(rows, cols, dtype=bf, device="cuda", generator=g)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    codes, scales = torch.empty(rows, cols, dtype=torch.int8, device="cuda"), torch.empty(rows, 35, dtype=torch.uint8, device="cuda")
+    w, b = randn(g, cols), randn(g, cols)
+    run(ewf.layer_norm, x, w, b, y, mean=mean, rstd=rstd)
+    for part in (slice(0, 50), slice(rows - 50, rows)):
+        check_norm(x[part], w, b, y[part], mean[part], rstd[part])
+    dx = y                                                          # (dy is x: the gradient of half a square)
+    run(ewf.layer_norm_grad, x, w, rstd, dx, x=x, mean=mean)
+    n = (x[-50:].double() - mean[-50:].double()[:, None]) * rstd[-50:].double()[:, None]
+    want = ref.layer_norm_grad(x[-50:], w, n, rstd[-50:], 2 * ref.U * n.abs(), bf, torch.float32)
+    ref.close("dx", dx[-50:], want["dx"], want["e_dx"])
+    ewf.keep8(x, codes, scales, stream=stream())
+    for part in (slice(0, 50), slice(rows - 50, rows)):
+        code, byte, _, _ = ref.keep8(x[part], "i8")
+        assert torch.equal(scales[part], byte) and torch.equal(codes[part].double(), code)
+    ewf.read8(codes, scales, y, stream=stream())
+    assert torch.equal(y[-50:], ref.keep8(x[-50:], "i8")[2].to(bf))
+    del x, y, dx, codes, scales
+    B, T, D = 70_000, 33, 1000
+    say("recurrence", B, T, D)
+    u, v, dh = (torch.randn(B, T, D, dtype=bf, device="cuda", generator=g) for _ in range(3))
+    h, du, dv, last = torch.empty_like(u), torch.empty_like(u), torch.empty_like(u), torch.empty(B, D, device="cuda")
+    run(ewf.recurrence, u, v, h, last=last)
+    run(ewf.recurrence_grad, u, v, h, dh, du, dv)
+    for part in (slice(0, 3), slice(B - 3, B)):
+        c = dict(u=u[part], v=v[part], w=None, h0=None, lengths=None)
+        check_rec(c, h[part], last[part])
+        want = ref.recurrence_grad(u[part], v[part], None, h[part], None, dh[part], None, None, bf)
+        for k, got in (("du", du), ("dv", dv)):
+            ref.close(k, got[part], want[k], want["e_" + k])
