@@ -524,8 +524,10 @@ EWF_OPS_DEV float search(const uint64_t *record, int64_t back, int place)
     }
 }
 
+// (backward: registers for four wavefronts on each of a unit's four SIMDs, two workgroups; with two gates the compiler takes
+// a few more by itself, and the second workgroup is worth more: bfloat16 [8, 4096, 2048] 249 us and 264)
 template <typename T, bool TIED, bool BACK, int L, int R, int W>
-__global__ void __launch_bounds__(W * 64) k_rec_chain(RecLaunch a, uint32_t chains, uint32_t tiles)
+__global__ void __launch_bounds__(W * 64, BACK ? 4 : 1) k_rec_chain(RecLaunch a, uint32_t chains, uint32_t tiles)
 {
     typedef Tile<T, TIED, BACK, L, R, W> Tl;
     constexpr int C = Tl::C;
@@ -540,12 +542,12 @@ __global__ void __launch_bounds__(W * 64) k_rec_chain(RecLaunch a, uint32_t chai
         const uint32_t chain = job % chains, b = chain / strips;
         uint32_t place = 0;
         __syncthreads();                                // (the arrays of the job before are read)
+        if (tiles > 1 && threadIdx.x == 0) drawn = __hip_atomic_fetch_add(counters + chain, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const Tl tile(a, chain - b * strips, b);        // (reads the sequence's length while the place is drawn)
         if (tiles > 1) {
-            if (threadIdx.x == 0) drawn = __hip_atomic_fetch_add(counters + chain, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             __syncthreads();
             place = __builtin_amdgcn_readfirstlane(drawn);
         }
-        const Tl tile(a, chain - b * strips, b);
         const int k0 = (int)place * Tl::kSteps;
         if (k0 >= tile.len && place) continue;          // (no step: nobody looks for this tile)
         Raw<T, BACK> raw[R];
