@@ -466,7 +466,8 @@ __global__ void __launch_bounds__(W * 64) k_rec_march(RecLaunch a)
 // that run or are done, and it publishes its own map before it waits; the first tile waits for none, and each next one
 // only for words that workgroups publish without waiting, or after a wait that has ended.  Where a caller breaks the
 // rule that overlapping calls have workspaces of their own, words can be lost: a wait is given up after kMostLooks
-// looks (seconds; a tile takes microseconds), and the channel's states from there on are NaN.
+// looks (seconds; a tile takes microseconds), and the channel's states from there on are NaN.  A place that is not one of the
+// chain's is not taken: whatever the workspace holds, every access is in bounds.
 
 constexpr uint32_t kMapBit = 1u << 30, kStateBit = 1u << 31;
 
@@ -547,6 +548,7 @@ __global__ void __launch_bounds__(W * 64, BACK ? 4 : 1) k_rec_chain(RecLaunch a,
         if (tiles > 1) {
             __syncthreads();
             place = __builtin_amdgcn_readfirstlane(drawn);
+            if (place >= tiles) continue;               // (only where another call has written into the workspace)
         }
         const int k0 = (int)place * Tl::kSteps;
         if (k0 >= tile.len && place) continue;          // (no step: nobody looks for this tile)
