@@ -20,10 +20,13 @@ EWF_OPS_DEV float act_value(float x)
     else return x;
 }
 
-// d act / dx.  A NaN argument (a block without a finite scale) gives NaN for every activation.
+// d act / dx.  A NaN argument (a block without a finite scale) gives NaN for every activation.  The slopes of silu and gelu are 0
+// and 1 in float32 long before +-128 (their distance is less than 2^-118 there): farther arguments, up to the infinities that
+// the largest floats' codes stand for in 32 bits, are taken as those, because x times a gate that is only nearly shut is not small for them.
 template <int ACT>
 EWF_OPS_DEV float act_slope(float x)
 {
+    if constexpr (ACT == EWF_SILU || ACT == EWF_GELU) x = x < -128.f ? -128.f : x > 128.f ? 128.f : x;
     if constexpr (ACT == EWF_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
     else if constexpr (ACT == EWF_ACT_TANH) { const float t = tanhf(x); return fmaf(-t, t, 1.f); }
     else if constexpr (ACT == EWF_ACT_SIGMOID) { float p, m; gate(x, p, m); return p * m; }

@@ -310,6 +310,28 @@ def test_activation_and_its_gradient(dtype, act):
         assert torch.equal(dy, dx)
 
 
+@pytest.mark.parametrize("kind", sorted(CODES))
+@pytest.mark.parametrize("act", ("relu", "tanh", "sigmoid", "silu", "gelu"))
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_activation_of_the_largest_numbers(dtype, act, kind):
+    # far from zero the slopes are their limits (2^-100 is more than any of them is away from its own at 1000), also where
+    # the code of a type's largest number stands for 2^128
+    dt = DT[dtype]
+    big = torch.finfo(dt).max
+    x = torch.tensor([-big, big, -big / 4, big / 4] + ([-3e38, 3e38, -1e36, 1e36, -1e30, 1e30] if dtype != "f16" else []) + [-2000.0, 2000.0], device="cuda")
+    x = x.to(dt)[:, None].repeat(1, 40).contiguous()
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    codes = torch.empty(x.shape, dtype=CODES[kind], device="cuda")
+    scales = torch.empty(x.shape[0], 2, dtype=torch.uint8, device="cuda")
+    ewf.activation(act, x, y, codes=codes, scales=scales, stream=stream())
+    ewf.activation_grad(act, torch.ones_like(x), dx, codes=codes, scales=scales, stream=stream())
+    up = (x > 0).double()
+    value = {"tanh": 2 * up - 1, "sigmoid": up}.get(act, x.double() * up)
+    slope = 0 * up if act in ("tanh", "sigmoid") else up
+    assert float((y.double() - value).abs().max()) <= 2.0 ** -100
+    assert float((dx.double() - slope).abs().max()) <= 2.0 ** -100
+
+
 @pytest.mark.parametrize("dtype", sorted(DT))
 def test_activation_strides(dtype):
     dt, g = DT[dtype], gen(14)
