@@ -296,7 +296,7 @@ ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *fail
  * and, with g = dy weight,
  *     dx = rstd (g - sum g / cols - n sum (g n) / cols),  dweight = sum over rows of dy n,  dbias = sum over rows of dy.
  * The axes before the last are the rows (fewer than 2^31); where they do not merge into at most two axes
- * common to all tensors the call is EWF_EUNSUPPORTED.
+ * common to all tensors the call is EWF_EUNSUPPORTED.  A row whose sums leave float32's range gives infinities or NaN.
  *
  * ewf_layer_norm reads x and writes y; optional: weight, bias (absent: 1 and 0), mean and rstd (float32, the shape
  * of x without its last axis) to be written, codes and scales to be written (n in 8 bits, see ewf_activation).
@@ -341,6 +341,7 @@ ewf_status ewf_read8(const ewf_activation_args *a, void *hip_stream);
 
 /* Gated linear recurrence over time, channel by channel, from state h_(-1) = h0 (absent: 0):
  *     f = sigmoid(u),  i = sigmoid(w), or 1 - f with w absent,  h_t = f_t h_(t-1) + i_t v_t
+ * A gate of less than 2^-126 counts as 0.
  * u, v, w, h have shape [batch, steps, channels] (steps and batch may have any strides: column blocks of one
  * projection, time-major tensors); h0 and last, the state behind the last step, are float32 [batch, channels]
  * with contiguous channels.  With one step this is the form for single tokens: last may lie over h0, and the state is

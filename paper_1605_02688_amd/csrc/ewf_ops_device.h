@@ -220,13 +220,15 @@ EWF_OPS_DEV float group_sum(float x)
 constexpr float kLog2E = 1.44269504f;
 
 // f = sigmoid(u) and 1 - f, both to within a few units in the last place: e = 2^(-u log2 e), f = 1 / (1 + e),
-// 1 - f = e f.  e is kept finite (a gate of less than 2^-126 counts as that); a NaN stays one.
+// 1 - f = e f.  A gate of less than 2^-126 counts as zero and its complement as one, where e f would be infinity times zero; a
+// NaN stays one.
 EWF_OPS_DEV void gate(float u, float &f, float &g)
 {
-    float e = __builtin_amdgcn_exp2f(-u * kLog2E);
-    e = e > 0x1p126f ? 0x1p126f : e;
-    f = __builtin_amdgcn_rcpf(1.f + e);
-    g = e * f;
+    const float e = __builtin_amdgcn_exp2f(-u * kLog2E);
+    const float h = __builtin_amdgcn_rcpf(1.f + e);
+    const bool shut = e > 0x1p126f;
+    f = shut ? 0.f : h;
+    g = shut ? 1.f : e * h;
 }
 
 // sigmoid alone: 1 / (1 + 2^(-x log2 e)); e may overflow, and the result is then zero

@@ -109,7 +109,7 @@ EWF_OPS_DEV int sequence_length(const RecLaunch &a, int64_t b)
 }
 
 // One element's gradients from G, the gradient of its state; `f` and `before` are its gate and the state before it.  Returns what the
-// step hands to the one before.
+// step hands to the one before.  Gates first: a product that a shut gate makes small does not overflow on the way.
 template <bool TIED>
 EWF_OPS_DEV float gradients(float G, float u, float w, float v, float before, float &du, float &dv, float &dw)
 {
@@ -117,13 +117,13 @@ EWF_OPS_DEV float gradients(float G, float u, float w, float v, float before, fl
     gate(u, f, g);
     if constexpr (TIED) {
         dv = G * g;
-        du = dv * (before - v) * f;
+        du = dv * f * (before - v);
     } else {
         float i, j;
         gate(w, i, j);
         dv = G * i;
-        dw = dv * v * j;
-        du = G * before * (f * g);
+        dw = dv * j * v;
+        du = G * (f * g) * before;
     }
     return f * G;
 }

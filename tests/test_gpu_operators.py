@@ -478,6 +478,23 @@ def test_recurrence_gates_at_their_ends():
     assert torch.equal(last[0], v[0, 300])
 
 
+@pytest.mark.parametrize("tied", (True, False))
+@pytest.mark.parametrize("T", (1, 9, 40, 333))
+def test_recurrence_shut_gates_forget_the_largest_states(T, tied):
+    # e^-300 of 3e38 is nothing, of a state and of a gradient
+    g, D = gen(23), 70
+    u, v, dh = torch.full((2, T, D), -300.0, device="cuda"), randn(g, 2, T, D), randn(g, 2, T, D)
+    w = None if tied else torch.full_like(u, 300.0)
+    h0 = torch.full((2, D), 3e38, device="cuda")
+    h, last = torch.empty_like(u), torch.empty_like(h0)
+    run(ewf.recurrence, u, v, h, w=w, h0=h0, last=last)
+    assert torch.equal(h, v) and torch.equal(last, v[:, -1])
+    du, dv, dw, dh0 = torch.empty_like(u), torch.empty_like(u), None if tied else torch.empty_like(u), torch.empty_like(h0)
+    run(ewf.recurrence_grad, u, v, h, dh, du, dv, w=w, dw=dw, h0=h0, dh0=dh0, dlast=torch.full_like(h0, -1e38))
+    dh[:, -1] += -1e38
+    assert torch.equal(dv, dh) and (du == 0).all() and (dh0 == 0).all() and (tied or (dw == 0).all())
+
+
 @pytest.mark.parametrize("T", (5, 333))
 def test_recurrence_keeps_what_is_not_finite_in_its_channel(T):
     g = gen(20 + T)
