@@ -793,6 +793,9 @@ class BoundOperator:
         device = getattr(workspace, "device", None)
         if device is not None and filler._device is not None and device != filler._device:
             _refuse(EINVAL, f"workspace: on {device}, the tensors on {filler._device}")
+        if hasattr(workspace, "is_contiguous") and not workspace.is_contiguous():
+            _refuse(EINVAL, "workspace: not contiguous")
+        self._device = None if filler._device is None else filler._device.index
         self._keep = (filler, workspace)
         self._ref = ctypes.byref(filler.args)
         self._fn = operator._fn
@@ -802,7 +805,9 @@ class BoundOperator:
         self._stream = stream or None
 
     def launch(self, stream: Optional[int] = None) -> None:
-        """Launches on `stream`, or on the stream that the call was bound to."""
+        """Launches on `stream`, or on the stream that the call was bound to; the tensors' device is the current one."""
+        if self._device is not None and self._device != torch.cuda.current_device():
+            _refuse(EINVAL, f"bound on device {self._device}, the current one is {torch.cuda.current_device()}")
         s = self._stream if stream is None else (stream or None)
         st = self._fn(self._ref, self._ws, self._ws_bytes, s) if self._with_workspace else self._fn(self._ref, s)
         if st < 0:

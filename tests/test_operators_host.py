@@ -235,3 +235,22 @@ def test_reserved_words_and_unknown_types_are_refused():
     f = ewf._activation("relu", T((2, 8)), T((2, 8)))
     f.args.act = 99
     assert ewf._lib.ewf_activation(ewf.ctypes.byref(f.args), None) == ewf.EINVAL
+
+
+def test_a_workspace_is_contiguous():
+    # (a view's number of elements is not what lies behind its pointer)
+    for work in (torch.empty(1, dtype=torch.uint8).expand(1 << 24), torch.empty(64, 64, dtype=torch.uint8).t(), torch.empty(64, dtype=torch.uint8)[::2]):
+        args = T((1, 5000, 64)), T((1, 5000, 64)), T((1, 5000, 64))
+        refused(ewf.EINVAL, "contiguous", ewf.recurrence.bind, *args, workspace=work)
+
+
+def test_a_bound_call_stays_on_its_device(monkeypatch):
+    class OnDevice(ewf.TensorRef):
+        device = torch.device("cuda", 0)
+
+    at = lambda: OnDevice(*vars(T((4, 64))).values())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    call = ewf.layer_norm.bind(at(), None, None, at())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    refused(ewf.EINVAL, "device", call.launch)
+    refused(ewf.EINVAL, "device", ewf.layer_norm.bind, at(), None, None, at())
