@@ -57,23 +57,18 @@ template <> struct EightAt<F32> { typedef u32x2_a4 at; };
 template <typename T>
 EWF_OPS_DEV Eight<T> load_eight(const typename T::raw *p) { return {*reinterpret_cast<const typename EightAt<T>::at *>(p)}; }
 
-// A row's edge: p is where the lane's load begins, c the channel that is its first.
+// Rows of fewer than C channels, element by element: those behind the last are copies of it, and nobody's.
 template <typename T>
-EWF_OPS_DEV Eight<T> load_edge(const typename T::raw *p, const Lane &l, int c, int channels)
+EWF_OPS_DEV Eight<T> load_few(const typename T::raw *p, int channels)
 {
-    constexpr int C = kWidth<T>, bits = 64 / C;
-    if (channels >= C) {
-        Eight<T> x = load_eight<T>(p);
-        x.move_down(c - l.from);
-        return x;
-    }
+    constexpr int C = kWidth<T>;
     uint64_t w = 0;
 #pragma unroll
-    for (int e = 0; e < C - 1; e++)
-        if (e < l.have) {
-            if constexpr (sizeof(typename T::raw) == 4) w |= (uint64_t)float_to_bits(p[e]) << (e * bits);
-            else w |= (uint64_t)p[e] << (e * bits);
-        }
+    for (int e = 0; e < C; e++) {
+        const typename T::raw x = p[e < channels ? e : channels - 1];
+        if constexpr (C == 2) w |= (uint64_t)float_to_bits(x) << (e * 32);
+        else w |= (uint64_t)x << (e * 16);
+    }
     return {__builtin_bit_cast(u32x2, w)};
 }
 
@@ -130,7 +125,8 @@ EWF_OPS_DEV float gradients(float G, float u, float w, float v, float before, fl
 
 // ------------------------------------------------------------------ few steps: a lane walks through time
 
-template <typename T, bool TIED, bool BACK>
+// CUT: rows that end inside a lane's channels.
+template <typename T, bool TIED, bool BACK, bool CUT>
 __global__ void __launch_bounds__(64) k_rec_walk(RecLaunch a)
 {
     constexpr int C = kWidth<T>;
@@ -144,42 +140,83 @@ __global__ void __launch_bounds__(64) k_rec_walk(RecLaunch a)
     const int len = sequence_length(a, b);
     auto load = [&](const RecTensor &x, int64_t t) {
         const raw *p = (const raw *)x.p + b * x.batch + t * x.step + l.from;
-        return l.have == C ? load_eight<T>(p) : load_edge<T>(p, l, c, channels);
+        return CUT && channels < C ? load_few<T>(p, channels) : load_eight<T>(p);
     };
-    auto store = [&](const RecTensor &x, int64_t t, const float *f) { store_edge<T>((raw *)x.p + b * x.batch + t * x.step + c, l.have, f); };
+    auto store = [&](const RecTensor &x, int64_t t, const float *f) {
+        raw *p = (raw *)x.p + b * x.batch + t * x.step + c;
+        if constexpr (CUT) store_edge<T>(p, l.have, f);
+        else store_eight<T>(p, f);
+    };
+    const int drop = c - l.from;
+    auto settle = [&](Eight<T> x) {
+        if constexpr (CUT) x.move_down(drop);
+        return x;
+    };
     float s[C];
 #pragma unroll
     for (int e = 0; e < C; e++) s[e] = e < l.have ? load_state(BACK ? a.dlast : a.h0, b, c + e) : 0.f;
+    // (the operands of kAhead steps are read together: bfloat16 [128, 16, 2048] forward and backward 7.3 and 13.5 us; eight, 7.1 and 13.8)
+    constexpr int kAhead = 4;
     if constexpr (!BACK) {
-        for (int t = 0; t < len; t++) {
-            const Eight<T> u = load(a.u, t), v = load(a.v, t);
-            Eight<T> w = u;
-            if constexpr (!TIED) w = load(a.w, t);
+        for (int t0 = 0; t0 < len; t0 += kAhead) {
+            Eight<T> u[kAhead], v[kAhead], w[kAhead];
 #pragma unroll
-            for (int e = 0; e < C; e++) {
-                float f, i, less;
-                gate(u[e], f, i);
-                if constexpr (!TIED) gate(w[e], i, less);
-                s[e] = fmaf(f, s[e], i * v[e]);
+            for (int k = 0; k < kAhead; k++) {
+                const int t = t0 + k;
+                if (t >= len) break;
+                u[k] = load(a.u, t);
+                v[k] = load(a.v, t);
+                if constexpr (!TIED) w[k] = load(a.w, t);
             }
-            store(a.h, t, s);
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                if (t0 + k >= len) break;
+                u[k] = settle(u[k]);
+                v[k] = settle(v[k]);
+                if constexpr (!TIED) w[k] = settle(w[k]);
+#pragma unroll
+                for (int e = 0; e < C; e++) {
+                    float f, i, less;
+                    gate(u[k][e], f, i);
+                    if constexpr (!TIED) gate(w[k][e], i, less);
+                    s[e] = fmaf(f, s[e], i * v[k][e]);
+                }
+                store(a.h, t0 + k, s);
+            }
         }
     } else {
-        for (int t = len - 1; t >= 0; t--) {
-            const Eight<T> u = load(a.u, t), v = load(a.v, t), dh = load(a.dh, t);
-            Eight<T> w = u, h = u;
-            if constexpr (!TIED) w = load(a.w, t);
-            if (t > 0) h = load(a.h, t - 1);
-            float du[C], dv[C], dw[C];
+        for (int t0 = len - 1; t0 >= 0; t0 -= kAhead) {
+            Eight<T> u[kAhead], v[kAhead], w[kAhead], h[kAhead], dh[kAhead];
 #pragma unroll
-            for (int e = 0; e < C; e++) {
-                float before = h[e];
-                if (t == 0) before = e < l.have ? load_state(a.h0, b, c + e) : 0.f;
-                s[e] = gradients<TIED>(dh[e] + s[e], u[e], w[e], v[e], before, du[e], dv[e], dw[e]);
+            for (int k = 0; k < kAhead; k++) {
+                const int t = t0 - k;
+                if (t < 0) break;
+                u[k] = load(a.u, t);
+                v[k] = load(a.v, t);
+                dh[k] = load(a.dh, t);
+                if constexpr (!TIED) w[k] = load(a.w, t);
+                h[k] = load(a.h, t > 0 ? t - 1 : 0);
             }
-            store(a.du, t, du);
-            store(a.dv, t, dv);
-            if constexpr (!TIED) store(a.dw, t, dw);
+#pragma unroll
+            for (int k = 0; k < kAhead; k++) {
+                const int t = t0 - k;
+                if (t < 0) break;
+                u[k] = settle(u[k]);
+                v[k] = settle(v[k]);
+                dh[k] = settle(dh[k]);
+                h[k] = settle(h[k]);
+                if constexpr (!TIED) w[k] = settle(w[k]);
+                float du[C], dv[C], dw[C];
+#pragma unroll
+                for (int e = 0; e < C; e++) {
+                    float before = h[k][e];
+                    if (t == 0) before = e < l.have ? load_state(a.h0, b, c + e) : 0.f;
+                    s[e] = gradients<TIED>(dh[k][e] + s[e], u[k][e], TIED ? 0.f : w[k][e], v[k][e], before, du[e], dv[e], dw[e]);
+                }
+                store(a.du, t, du);
+                store(a.dv, t, dv);
+                if constexpr (!TIED) store(a.dw, t, dw);
+            }
         }
     }
 #pragma unroll
@@ -206,21 +243,25 @@ template <typename T> struct Raw<T, true> { Eight<T> u, v, w, h, dh; };
 // The rows of one tensor that a lane reads or writes, one after the other: an address that all lanes of a wavefront share, and
 // offsets of 32 bits to it (the host refuses steps that are further apart).  Reads stay between the first and the last
 // step that exists: steps that do not are read from there, and composing leaves them out.
-template <typename T, bool BACK>
+// FEW: rows of fewer than C channels.
+template <typename T, bool BACK, bool FEW>
 struct Rows {
     char *base;
     int at, step, lowest, highest;                      // bytes
+    int few;                                            // FEW: the channels
 
     EWF_OPS_DEV Eight<T> load() const
     {
         const int off = BACK ? (at > lowest ? at : lowest) : (at < highest ? at : highest);
-        return load_eight<T>((const typename T::raw *)(base + (uint32_t)off));
+        const typename T::raw *p = (const typename T::raw *)(base + (uint32_t)off);
+        if constexpr (FEW) return load_few<T>(p, few);
+        else return load_eight<T>(p);
     }
     EWF_OPS_DEV typename T::raw *pointer() const { return (typename T::raw *)(base + (uint32_t)at); }
     EWF_OPS_DEV void next() { at += BACK ? -step : step; }
 };
 
-template <typename T, bool TIED, bool BACK, int L, int R, int W>
+template <typename T, bool TIED, bool BACK, int L, int R, int W, bool FEW = false>
 struct Tile {
     static constexpr int C = kWidth<T>, G = 64 / L, kSteps = W * G * R, kStrip = L * C, size = sizeof(typename T::raw);
     static_assert(kStrip <= W * 64, "one thread for each channel of a strip");
@@ -255,21 +296,22 @@ struct Tile {
     }
 
     // `before` of the tensor: its rows one step earlier.
-    EWF_OPS_DEV Rows<T, BACK> rows(const RecTensor &x, int k0, bool read, bool before = false) const
+    EWF_OPS_DEV Rows<T, BACK, FEW> rows(const RecTensor &x, int k0, bool read, bool before = false) const
     {
         const int t0 = earliest(k0), shift = before ? 1 : 0;
         const int base = t0 >= shift ? t0 - shift : 0;                                  // (uniform)
         int rel = BACK ? len - 1 - first(k0) - shift - base : group * R;               // of the lane's first step
         if (BACK && rel < 0) rel = 0;                                                   // (all its rows are read at the earliest)
         const int more = len - 1 - base;
-        const int edge = channels - C < c0 ? channels - C : c0;                         // (uniform: reads of the last channels begin there)
+        const int edge = FEW ? 0 : channels - C < c0 ? channels - C : c0;                         // (uniform: reads of the last channels begin there)
         const int from = read ? edge : c0, c = (read ? l.from - edge : C * place) * size;
-        Rows<T, BACK> r;
+        Rows<T, BACK, FEW> r;
         r.base = (char *)x.p + (b * x.batch + base * x.step + from) * size;
         r.step = (int)(x.step * size);
         r.at = rel * r.step + c;
         r.lowest = c;
         r.highest = (more < G * R - 1 ? more : G * R - 1) * r.step + c;
+        r.few = channels;
         return r;
     }
 
@@ -287,7 +329,7 @@ struct Tile {
             fetch(a.dh, false, &Raw<T, BACK>::dh);
             fetch(a.h, true, &Raw<T, BACK>::h);
         }
-        if (!whole_strip) {
+        if (!FEW && !whole_strip) {
             const int drop = channel() - l.from;
 #pragma unroll
             for (int r = 0; r < R; r++) {
@@ -362,7 +404,7 @@ struct Tile {
     EWF_OPS_DEV void finish(int k0, const Raw<T, BACK> (&raw)[R], const Maps &maps, float (&s)[C]) const
     {
         const int from = first(k0);
-        auto put = [&](Rows<T, BACK> &p, int r, const float *f) {
+        auto put = [&](Rows<T, BACK, FEW> &p, int r, const float *f) {
             if (from + r < len) {
                 if (whole_strip) store_eight<T>(p.pointer(), f);
                 else store_edge<T>(p.pointer(), l.have, f);
@@ -527,10 +569,10 @@ EWF_OPS_DEV float search(const uint64_t *record, int64_t back, int place)
 
 // (backward: registers for four wavefronts on each of a unit's four SIMDs, two workgroups; with two gates the compiler takes
 // a few more by itself, and the second workgroup is worth more: bfloat16 [8, 4096, 2048] 249 us and 264)
-template <typename T, bool TIED, bool BACK, int L, int R, int W>
+template <typename T, bool TIED, bool BACK, int L, int R, int W, bool FEW>
 __global__ void __launch_bounds__(W * 64, BACK ? 4 : 1) k_rec_chain(RecLaunch a, uint32_t chains, uint32_t tiles)
 {
-    typedef Tile<T, TIED, BACK, L, R, W> Tl;
+    typedef Tile<T, TIED, BACK, L, R, W, FEW> Tl;
     constexpr int C = Tl::C;
     __shared__ Map totals[W][Tl::kStrip];
     __shared__ float states[W][Tl::kStrip];
@@ -602,15 +644,15 @@ __global__ void __launch_bounds__(W * 64, BACK ? 4 : 1) k_rec_chain(RecLaunch a,
 // ------------------------------------------------------------------ which kernel
 
 constexpr uint32_t kMostJobs = 1 << 20;  // workgroups of a launch; further jobs are taken in turn
-constexpr int kWalkSteps = 16;           // up to here a lane walks through time by itself
 
 // Lanes a row, steps a lane, wavefronts.
 template <int L_, int R_, int W_> struct Shape { static constexpr int L = L_, R = R_, W = W_, steps = W_ * (64 / L_) * R_; };
+typedef Shape<8, 4, 8> Slim;             // 64 bytes, 256 steps
 typedef Shape<16, 4, 8> Narrow;          // 128 bytes of a row, 128 steps
 typedef Shape<32, 16, 8> Long;           // 256 bytes, 256 steps
 typedef Shape<64, 8, 8> Wide;            // 512 bytes, 64 steps
 
-enum class How { Walk, March, Small, Large };
+enum class How { Walk, March, Slim, Small, Large };
 
 struct Plan {
     How how = How::Walk;
@@ -628,35 +670,62 @@ void cut(const RecLaunch &a, How how, Plan &p)
     p.bytes = p.tiles > 1 ? (p.chains * p.tiles * strip * 8 + p.chains * 4 + 15) / 16 * 16 : 0;
 }
 
+// A shape's strips fit rows that fill two thirds of them.
+template <typename S>
+bool filled(const RecLaunch &a)
+{
+    const int64_t strip = S::L * (a.dtype == EWF_F32 ? 2 : 4);
+    return a.channels * 3 >= (a.channels + strip - 1) / strip * strip * 2;
+}
+
+// Few steps: a lane walks through time by itself, at up to 1 us for four steps; tiles cost what their number does.  bfloat16, us,
+// forward and backward, walk / the better tiles: [32, 16, 1024] (512 strips of 128 bytes) 6.4, 8.6 / 6.7, 8.9; [16, 24, 2048]
+// (512) 7.2, 11.4 / 6.4, 9.1; [64, 32, 2048] (2048) 9.4, 18.0 / 15.8, 16.4; [128, 48, 2048] (4096) 16.8, 30.1 / 30.5, 33.9.  Rows that
+// are cut are walked more slowly: [2, 13, 74] 7.2, 10.7 / 6.3, 7.6.
+bool is_walked(const RecLaunch &a, int units)
+{
+    const int64_t strip = a.dtype == EWF_F32 ? 32 : 64, strips = (a.channels + strip - 1) / strip * a.batch, times = strips / (4 * (int64_t)units);
+    const bool cut = a.channels % (a.dtype == EWF_F32 ? 2 : 4) != 0;
+    return a.steps <= (cut ? 8 : 16) * (times < 1 ? 1 : times > 3 ? 3 : times);
+}
+
+// Rows of up to 64 bytes: slim tiles (bfloat16 [36, 34737, 26], us, forward and backward, slim / narrow / large / march: 67,
+// 137 / 115, 203 / 220, 565 / 732; [256, 4096, 26] 54, 111 / 89, 167 / 175, 465 / 91).
 // Forward, us, march / chains of long tiles / chains of narrow tiles, bfloat16 [8, 4096, 2048] (256 strips of 64 channels)
 // 91 / 105 / 121, [16, 512, 1024] (256) 13.0 / 15.3 / -, [3, 4096, 2048] (96) 73 / 44 / 48, [1, 65536, 1024] (16) 1047 / 103 / -: a
 // workgroup for a strip where there is one for nearly each unit, tiles where there are fewer.  Long tiles, of which fewer
 // search, where there is one for each unit ([4, 2048, 1024], 256 of them, 16.6 / 18.2; [2, 512, 2048], 64, 11.8 / 10.8).
 // Backward, wide tiles / narrow ones: [8, 4096, 2048] 176 / 206, [3, 4096, 2048] (1536 wide tiles) 77 / 82, [4, 2048, 1024] (512)
 // 34.1 / 32.8, float16 [5, 1237, 1000] (400) 30.9 / 23.0; sequences that one wide tile holds ([32, 64, 2048]) 14.5 / 19.0.
+// Where rows leave a part of them empty, [20, 8000, 160 | 200 | 300], long / narrow 62 / 49, 67 / 70, 104 / 103, wide / narrow
+// 103 / 97, 110 / 145, 202 / 196.
 Plan plan_of(const RecLaunch &a, bool backward, int units)
 {
     Plan p;
-    if (a.steps <= kWalkSteps || a.channels < (a.dtype == EWF_F32 ? 2 : 4)) return p;
+    if (is_walked(a, units)) return p;
+    if (a.channels <= (a.dtype == EWF_F32 ? 16 : 32)) {
+        cut<Slim>(a, How::Slim, p);
+        return p;
+    }
     if (!backward) {
         cut<Narrow>(a, How::March, p);
         if (p.chains * 8 >= (uint64_t)units * 7) return p;
         cut<Long>(a, How::Large, p);
-        if (p.chains * p.tiles >= (uint64_t)units) return p;
+        if (filled<Long>(a) && p.chains * p.tiles >= (uint64_t)units) return p;
     } else {
         cut<Wide>(a, How::Large, p);
-        if (p.chains * p.tiles >= 4 * (uint64_t)units || p.tiles == 1) return p;
+        if (filled<Wide>(a) && (p.chains * p.tiles >= 4 * (uint64_t)units || p.tiles == 1)) return p;
     }
     cut<Narrow>(a, How::Small, p);
     return p;
 }
 
-template <typename T, bool TIED, bool BACK, typename S>
+template <typename T, bool TIED, bool BACK, typename S, bool FEW = false>
 void run_chain(const RecLaunch &a, const Plan &p, hipStream_t stream)
 {
     if (p.bytes) aux_fill_zero(a.workspace, p.bytes, stream);
     const uint64_t jobs = p.chains * p.tiles;
-    hipLaunchKernelGGL((k_rec_chain<T, TIED, BACK, S::L, S::R, S::W>), dim3((uint32_t)(jobs < kMostJobs ? jobs : kMostJobs)), dim3(S::W * 64), 0, stream, a,
+    hipLaunchKernelGGL((k_rec_chain<T, TIED, BACK, S::L, S::R, S::W, FEW>), dim3((uint32_t)(jobs < kMostJobs ? jobs : kMostJobs)), dim3(S::W * 64), 0, stream, a,
                        (uint32_t)p.chains, (uint32_t)p.tiles);
 }
 
@@ -668,7 +737,8 @@ void run(const RecLaunch &a, const Plan &p, hipStream_t stream)
     case How::Walk: {
         // (fewer than 2^31 lanes: batch x channels is)
         const dim3 grid((uint32_t)(((uint64_t)((a.channels + C - 1) / C) * a.batch + 63) / 64));
-        hipLaunchKernelGGL((k_rec_walk<T, TIED, BACK>), grid, dim3(64), 0, stream, a);
+        if (a.channels % C) hipLaunchKernelGGL((k_rec_walk<T, TIED, BACK, true>), grid, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL((k_rec_walk<T, TIED, BACK, false>), grid, dim3(64), 0, stream, a);
         return;
     }
     case How::March:
@@ -676,6 +746,9 @@ void run(const RecLaunch &a, const Plan &p, hipStream_t stream)
             hipLaunchKernelGGL((k_rec_march<T, TIED, false, Narrow::L, Narrow::R, Narrow::W>), dim3((uint32_t)(p.chains < kMostJobs ? p.chains : kMostJobs)),
                                dim3(Narrow::W * 64), 0, stream, a);
         return;
+    case How::Slim:
+        if (a.channels < C) return run_chain<T, TIED, BACK, Slim, true>(a, p, stream);
+        return run_chain<T, TIED, BACK, Slim>(a, p, stream);
     case How::Small: return run_chain<T, TIED, BACK, Narrow>(a, p, stream);
     case How::Large:
         if constexpr (BACK) return run_chain<T, TIED, true, Wide>(a, p, stream);

@@ -443,6 +443,38 @@ def test_recurrence_of_many_tiles(B, T, D, dtype, tied):
         assert all(torch.equal(again[1][k], d[k]) for k in d if d[k] is not None)
 
 
+@pytest.mark.parametrize("B,T,D,dtype,tied", (
+    (4, 3000, 1, "bf16", False), (3, 2600, 2, "f16", True), (2, 300, 3, "bf16", True), (5, 1300, 1, "f32", False),   # rows of less than a lane's
+    (3, 2500, 26, "bf16", False), (40, 260, 13, "f32", True), (2, 1025, 32, "f16", False),                            # rows of a slim tile
+    (200, 40, 1032, "bf16", True), (200, 20, 1030, "f16", False), (130, 33, 520, "f32", False),                       # walks of many channels
+    (20, 800, 160, "bf16", False), (20, 800, 200, "bf16", True)))                                                     # strips part empty, and filled
+def test_recurrence_of_few_channels_and_of_many_rows(B, T, D, dtype, tied):
+    test_recurrence_of_many_tiles(B, T, D, dtype, tied)
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("T", (5, 700))
+@pytest.mark.parametrize("D", (1, 3, 29))
+def test_recurrence_of_few_channels_in_place(T, D, dtype):
+    g, dt, B = gen(24), DT[dtype], 3
+    lengths = torch.tensor([T, T // 2, 0], dtype=torch.int32, device="cuda")
+    both = randn(g, B, T, 3 * D + 1, dtype=dt)                        # column blocks of a projection
+    u, v, dh = both[:, :, 1: D + 1], both[:, :, D + 1: 2 * D + 1], both[:, :, 2 * D + 1:]
+    copies = [t.contiguous() for t in (u, v, dh)]
+    h, du, dv = (torch.full((B, T, D), 7.0, dtype=dt, device="cuda") for _ in range(3))
+    run(ewf.recurrence, copies[0], copies[1], h, lengths=lengths)
+    run(ewf.recurrence_grad, copies[0], copies[1], h, copies[2], du, dv, lengths=lengths)
+    before = both.clone()
+    run(ewf.recurrence_grad, u, v, h, dh, u, dh, lengths=lengths)     # du over u, dv over dh
+    on = torch.arange(T, device="cuda")[None, :] < lengths[:, None]
+    assert torch.equal(u[on], du[on]) and torch.equal(dh[on], dv[on]) and torch.equal(v, before[:, :, D + 1: 2 * D + 1])
+    assert torch.equal(both[~on], before[~on]) and torch.equal(both[:, :, 0], before[:, :, 0])
+    both.copy_(before)
+    run(ewf.recurrence, u, v, v, lengths=lengths)                     # h over v
+    assert torch.equal(v[on], h[on]) and torch.equal(both[~on], before[~on])
+    assert torch.equal(both[:, :, : D + 1], before[:, :, : D + 1]) and torch.equal(both[:, :, 2 * D + 1:], before[:, :, 2 * D + 1:])
+
+
 @pytest.mark.parametrize("T", (3, 40, 700))
 def test_recurrence_lengths_out_of_range_and_what_lies_behind(T):
     g = gen(T)
