@@ -211,8 +211,10 @@ EWF_OPS_DEV void normalised(const NormLaunch &a, u32x4 x, float mean, float rstd
 
 // One sweep over dy and x: a workgroup takes rows in turn and its threads keep their columns' sums for dweight and
 // dbias in registers; what remains across workgroups is one partial per workgroup, folded by k_norm_finish.
+// Rows that are cut: registers for two workgroups a unit (from 8 bits the compiler takes a few more by itself: float16 [20011, 1001] 33.9 us
+// and 44.9, [61060, 25] 18.6 and 25.8; from x bfloat16 [8192, 4001] 44.6 and 51.4).
 template <typename T, int TPR, int NV, bool CUT, bool KEPT>
-__global__ void __launch_bounds__(Held<TPR>::threads) k_norm_grad(NormLaunch a)
+__global__ void __launch_bounds__(Held<TPR>::threads, CUT && NV == 2 && TPR <= kThreads ? 4 : 1) k_norm_grad(NormLaunch a)
 {
     constexpr int V = Vec16<T>::V, G = Held<TPR>::groups;
     typedef typename T::raw raw;
