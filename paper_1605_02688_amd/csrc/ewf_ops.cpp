@@ -457,10 +457,12 @@ ewf_status ewf_layer_norm_grad(const ewf_layer_norm_args *a, void *workspace, si
         NormLaunch n;
         ewf_status st = norm_layout(a, true, n);
         if (st != EWF_OK) return st;
-        st = workspace_fits(norm_workspace(n), workspace, workspace_bytes);
+        const size_t need = norm_workspace(n);
+        st = workspace_fits(need, workspace, workspace_bytes);
         if (st != EWF_OK) return st;
         if (n.r.rows == 0 && !n.dweight && !n.dbias) return EWF_OK;
-        n.partials = (float *)workspace;
+        // (a workspace that the call does not need is not looked at, neither its size nor its alignment, and not written)
+        n.partials = need ? (float *)workspace : nullptr;
         launch_layer_norm_grad(n, (hipStream_t)hip_stream);
         return launched("layer normalisation, backward");
     });

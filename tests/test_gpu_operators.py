@@ -194,6 +194,26 @@ def test_layer_norm_of_no_rows():
     assert (dw == 0).all() and (db == 0).all()
 
 
+@pytest.mark.parametrize("dtype,rows,cols", (("bf16", 300, 1024), ("f16", 300, 1001), ("bf16", 9, 14171), ("f32", 700, 20), ("f32", 3, 40005)))
+def test_layer_norm_gradient_without_sums_leaves_a_workspace_alone(dtype, rows, cols):
+    # dx alone needs none: one that a program hands to every call may be of any size and alignment
+    say("dx alone", dtype, rows, cols)
+    dt, g = DT[dtype], gen(9)
+    x, dy, w = randn(g, rows, cols, dtype=dt), randn(g, rows, cols, dtype=dt), randn(g, cols)
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    codes = torch.empty((rows, cols), dtype=torch.int8, device="cuda")
+    scales = torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device="cuda")
+    ewf.keep8(x, codes, scales, stream=stream())
+    for source in (dict(x=x, mean=mean), dict(codes=codes, scales=scales)):
+        want, dx = torch.empty_like(x), torch.empty_like(x)
+        assert ewf.layer_norm_grad.workspace_bytes(dy, w, rstd, want, **source) == 0
+        ewf.layer_norm_grad(dy, w, rstd, want, stream=stream(), **source)
+        whole = torch.full((64 << 20,), 0x5A, dtype=torch.uint8, device="cuda")
+        for part in (whole[4096:4160], whole[4097:4098]):
+            ewf.layer_norm_grad(dy, w, rstd, dx, workspace=part, stream=stream(), **source)
+            assert torch.equal(dx, want) and (whole == 0x5A).all()
+
+
 @pytest.mark.parametrize("kind", sorted(CODES))
 @pytest.mark.parametrize("dtype", sorted(DT))
 def test_layer_norm_kept_in_8_bits(dtype, kind):
