@@ -275,20 +275,23 @@ __global__ void __launch_bounds__(Held<TPR>::threads, CUT && NV == 2 && TPR <= k
         const uint64_t then = (uint64_t)row + (uint64_t)gridDim.x * G;
         if (kAhead && then < a.r.rows) fetch((uint32_t)then);   // in flight during this row
         const float rstd = now.rstd;
-        // n, and g = dy weight: kept for the second half, or, where rows are cut, computed again (kernels of rows that are cut need the
+        // g = dy weight and n = c unit, from 8 bits as they stand (unit 1), from x with c = x - mean and unit = rstd, which is multiplied
+        // in outside the row's sum: behind the row's end dy is zero, but -mean rstd may be infinite where the row's own n are not (rows
+        // of one value beyond 10^36).  No sum leaves the range by it: where c passes 2^64 the forward pass's squares overflow.
+        // c and g are kept for the second half, or, where rows are cut, computed again (kernels of rows that are cut need the
         // registers: float16 [20011, 1001] 40 us and 58, where two workgroups share a unit and where they do not; bfloat16
         // [16384, 4096], kept, 77, computed again, 80)
-        float gr[NV][V], n[NV][V], s1 = 0.f, s2 = 0.f;
+        const float unit = KEPT ? 1.f : rstd;
+        float gr[NV][V], c[NV][V], s1 = 0.f, s2 = 0.f;
         auto elements = [&](int j) {
-            if constexpr (KEPT) decode_part<V>(now.code[j], now.byte[j], a.code_dtype == EWF_E4M3, n[j]);
+            if constexpr (KEPT) decode_part<V>(now.code[j], now.byte[j], a.code_dtype == EWF_E4M3, c[j]);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                if constexpr (!KEPT) n[j][e] = (element<T>(now.x[j], e) - now.mean) * rstd;
+                if constexpr (!KEPT) c[j][e] = element<T>(now.x[j], e) - now.mean;
                 gr[j][e] = element<T>(now.dy[j], e) * w[j][e];
             }
         };
         if (live) {
-            // (behind the row's end dy is zero, and n is finite wherever the row's own are)
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 elements(j);
@@ -296,24 +299,24 @@ __global__ void __launch_bounds__(Held<TPR>::threads, CUT && NV == 2 && TPR <= k
                 for (int e = 0; e < V; e++) {
                     const float d = element<T>(now.dy[j], e);
                     s1 += gr[j][e];
-                    s2 = fmaf(gr[j][e], n[j][e], s2);
-                    dw[j][e] = fmaf(d, n[j][e], dw[j][e]);
+                    s2 = fmaf(gr[j][e], c[j][e], s2);
+                    dw[j][e] = fmaf(d * unit, c[j][e], dw[j][e]);
                     db[j][e] += d;
                 }
             }
         }
         const float m1 = row_sum<TPR>(s1, red[0]) / (float)cols;
-        const float m2 = row_sum<TPR>(s2, red[1]) / (float)cols;
+        const float m2 = row_sum<TPR>(s2 * unit, red[1]) / (float)cols * unit;
         if (!live) continue;
         raw *dx = (raw *)a.dx + row_offset(a.r, row, a.sdx);
 #pragma unroll
         for (int j = 0; j < NV; j++) {
-            const int c = (j * TPR + t) * V;
+            const int at = (j * TPR + t) * V;
             float o[V];
             if constexpr (CUT) elements(j);
 #pragma unroll
-            for (int e = 0; e < V; e++) o[e] = rstd * fmaf(-n[j][e], m2, gr[j][e] - m1);
-            if (c < cols) store_part<T, CUT>(dx, c, cols, pack16<T>(o));
+            for (int e = 0; e < V; e++) o[e] = rstd * fmaf(-c[j][e], m2, gr[j][e] - m1);
+            if (at < cols) store_part<T, CUT>(dx, at, cols, pack16<T>(o));
         }
     }
     if (!sums) return;

@@ -194,6 +194,21 @@ def test_layer_norm_of_no_rows():
     assert (dw == 0).all() and (db == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("cols", (1, 3, 5, 7, 8, 15, 20, 24, 41, 136, 1001, 1032, 1300, 4100, 8199, 40005))
+def test_layer_norm_gradient_of_large_rows_of_one_value(dtype, cols):
+    # n is 0 throughout and -mean rstd, what a zero behind the row's end would have for it, infinite
+    dt, g = DT[dtype], gen(cols)
+    x = torch.full((5, cols), 4e36, dtype=dt, device="cuda")
+    x[1], x[3] = -4e36, 1.0
+    mean, rstd = x[:, 0].float(), torch.full((5,), 1e-5 ** -0.5, device="cuda")
+    dy, w = randn(g, 5, cols, dtype=dt), randn(g, cols)
+    dx, dw, db = torch.empty_like(x), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    run(ewf.layer_norm_grad, dy, w, rstd, dx, x=x, mean=mean, dweight=dw, dbias=db)
+    assert torch.isfinite(dx).all() and (dw == 0).all()
+    check_norm_grad(dy, x, w, mean, rstd, dx, dw, db, torch.float32)
+
+
 @pytest.mark.parametrize("dtype,rows,cols", (("bf16", 300, 1024), ("f16", 300, 1001), ("bf16", 9, 14171), ("f32", 700, 20), ("f32", 3, 40005)))
 def test_layer_norm_gradient_without_sums_leaves_a_workspace_alone(dtype, rows, cols):
     # dx alone needs none: one that a program hands to every call may be of any size and alignment
