@@ -9,6 +9,29 @@ namespace ewf {
 
 namespace {
 
+// The normal distribution function, to its own precision on both sides of zero (1 + erf loses what lies below -3 in 16 bits already), and
+// e = exp(-x^2 / 2).  Below zero, with a = -x: e t P(t), t = 1 / (1 + 0.35 a), P the polynomial of degree 8 whose largest relative
+// error up to a = 13.5, where float32 ends, is least (3.2e-8; fitted to erfc in 64 bits).  The square's rounding costs x^2 / 2 units: at
+// -9, 4e-6.  Both passes of gelu, bfloat16 [8192, 8192], take 134 us, with the device library's erf 153, with its erfc 198.
+struct Normal { float below, e; };
+EWF_OPS_DEV Normal normal(float x)
+{
+    const float a = fminf(fabsf(x), 16.f);              // (both are 0 there; a NaN goes on in x)
+    const float e = __builtin_amdgcn_exp2f(a * a * (-0.5f * kLog2E)), y = fmaf(0.35f, a, 1.f), r = __builtin_amdgcn_rcpf(y);
+    const float t = fmaf(fmaf(-y, r, 1.f), r, r);
+    float p = -0.0291258656f;
+    p = fmaf(p, t, 0.143872231f);
+    p = fmaf(p, t, -0.255504578f);
+    p = fmaf(p, t, 0.158929303f);
+    p = fmaf(p, t, -0.0229371525f);
+    p = fmaf(p, t, 0.105432943f);
+    p = fmaf(p, t, 0.119852431f);
+    p = fmaf(p, t, 0.139859080f);
+    p = fmaf(p, t, 0.139621571f);
+    const float tail = e * (t * p);
+    return {x < 0.f ? tail : 1.f - tail, e};
+}
+
 template <int ACT>
 EWF_OPS_DEV float act_value(float x)
 {
@@ -16,11 +39,12 @@ EWF_OPS_DEV float act_value(float x)
     else if constexpr (ACT == EWF_ACT_TANH) return tanhf(x);
     else if constexpr (ACT == EWF_ACT_SIGMOID) return sigmoid(x);
     else if constexpr (ACT == EWF_SILU) return x * sigmoid(x);
-    else if constexpr (ACT == EWF_GELU) return x * (0.5f + 0.5f * erff(x * 0.70710678f));
+    else if constexpr (ACT == EWF_GELU) return x * normal(x).below;
     else return x;
 }
 
-// d act / dx.  A NaN argument (a block without a finite scale) gives NaN for every activation.  The slopes of silu and gelu are 0
+// d act / dx.  A NaN argument (a block without a finite scale) gives NaN for every activation.  That of tanh is 4 f (1 - f), f the
+// sigmoid of 2 x, small numbers that 1 - tanh^2 would lose.  The slopes of silu and gelu are 0
 // and 1 in float32 long before +-128 (their distance is less than 2^-118 there): farther arguments, up to the infinities that
 // the largest floats' codes stand for in 32 bits, are taken as those, because x times a gate that is only nearly shut is not small for them.
 template <int ACT>
@@ -28,12 +52,12 @@ EWF_OPS_DEV float act_slope(float x)
 {
     if constexpr (ACT == EWF_SILU || ACT == EWF_GELU) x = x < -128.f ? -128.f : x > 128.f ? 128.f : x;
     if constexpr (ACT == EWF_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
-    else if constexpr (ACT == EWF_ACT_TANH) { const float t = tanhf(x); return fmaf(-t, t, 1.f); }
+    else if constexpr (ACT == EWF_ACT_TANH) { float p, m; gate(2.f * x, p, m); return 4.f * (p * m); }
     else if constexpr (ACT == EWF_ACT_SIGMOID) { float p, m; gate(x, p, m); return p * m; }
     else if constexpr (ACT == EWF_SILU) { float p, m; gate(x, p, m); return fmaf(x * p, m, p); }
     else if constexpr (ACT == EWF_GELU) {
-        const float density = 0.39894228f * __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2E));
-        return fmaf(x, density, 0.5f + 0.5f * erff(x * 0.70710678f));
+        const Normal n = normal(x);
+        return fmaf(x * 0.39894228f, n.e, n.below);
     } else return x == x ? 1.f : x;
 }
 

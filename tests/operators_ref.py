@@ -150,6 +150,20 @@ def act_bounds(act, x):
     return a * 6 * U, 6 * U + a * density * (4 * x * x + 8) * U
 
 
+def act_relative_bounds(act, x):
+    """Bounds for tanh's slope and for gelu's value and slope that hold far from zero, where they are small themselves.
+    tanh: 4 f (1 - f), f = sigmoid(2 x), each factor as in `act_bounds`.  gelu: the argument of erfc(z) / 2, z = -x / sqrt 2, may be
+    rounded twice, z erfc'(z) / erfc(z) is at most 2 z^2 + 2 = x^2 + 2 in size, 16 units in the last place for erfc itself,
+    and two products follow; the density as in `act_bounds`, its own two units among them."""
+    a = x.abs()
+    if act == "tanh":
+        return None, ACTS[act][1](x) * (2 * (4 * a + 6) + 2) * U
+    below = 0.5 * torch.erfc(-x / math.sqrt(2)) * (2 * x * x + 4 + 32 + 2) * U
+    density = torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+    slope = ACTS[act][1](x).abs()
+    return a * below, below + a * density * (4 * x * x + 8) * U + slope * U
+
+
 # ------------------------------------------------------------------ recurrence
 
 def recurrence(u, v, w, h0, lengths, dtype):

@@ -367,6 +367,28 @@ def test_activation_of_the_largest_numbers(dtype, act, kind):
     assert float((dx.double() - slope).abs().max()) <= 2.0 ** -100
 
 
+@pytest.mark.parametrize("kind", sorted(CODES))
+@pytest.mark.parametrize("act", ("tanh", "gelu"))
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_activation_far_from_zero_to_its_own_precision(dtype, act, kind):
+    # the slope of tanh at 9 is 6e-8, gelu of -9 is -1e-18: relative to what 1 - tanh^2 and 1 + erf are taken from, nothing
+    dt = DT[dtype]
+    x = torch.linspace(-12, -2, 4001, device="cuda").to(dt)[None]
+    if act == "tanh":
+        x = torch.cat((x, -x))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    codes = torch.empty(x.shape, dtype=CODES[kind], device="cuda")
+    scales = torch.empty(x.shape[0], 126, dtype=torch.uint8, device="cuda")
+    ewf.activation(act, x, y, codes=codes, scales=scales, stream=stream())
+    ewf.activation_grad(act, torch.ones_like(x), dx, codes=codes, scales=scales, stream=stream())
+    x8 = ref.keep8(x, kind)[2]
+    if act == "gelu":
+        want = ref.ACTS[act][0](x.double())
+        ref.close("y", y, want, ref.stored(ref.act_relative_bounds(act, x.double())[0], want, dt))
+    want = ref.ACTS[act][1](x8)
+    ref.close("dx", dx, want, ref.stored(ref.act_relative_bounds(act, x8)[1], want, dt))
+
+
 @pytest.mark.parametrize("dtype", sorted(DT))
 def test_activation_strides(dtype):
     dt, g = DT[dtype], gen(14)
