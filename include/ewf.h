@@ -288,7 +288,8 @@ ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *fail
  *
  * An argument structure is zeroed by the caller and filled in: a tensor whose ptr and shape are both NULL is absent.
  * Tensors are EWF_F32, EWF_F16 or EWF_BF16 as the structure's `dtype` says; arithmetic, sums, statistics and states
- * are float32.  The last axis of every tensor of full size must be contiguous (stride 1, or extent 1); other axes may
+ * are float32; sigmoids of float32 tensors are accurate (as in math_mode 1), those of 16-bit tensors native-rate.
+ * The last axis of every tensor of full size must be contiguous (stride 1, or extent 1); other axes may
  * have any strides; a result may lie exactly over the operands that are named, and over nothing else (EWF_EALIAS). */
 
 /* Layer normalisation along the last axis (`cols` elements, 1 .. 2^24) of x, rank ndim 1 .. EWF_MAX_DIMS:

@@ -17,8 +17,7 @@ struct Normal { float below, e; };
 EWF_OPS_DEV Normal normal(float x)
 {
     const float a = fminf(fabsf(x), 16.f);              // (both are 0 there; a NaN goes on in x)
-    const float e = __builtin_amdgcn_exp2f(a * a * (-0.5f * kLog2E)), y = fmaf(0.35f, a, 1.f), r = __builtin_amdgcn_rcpf(y);
-    const float t = fmaf(fmaf(-y, r, 1.f), r, r);
+    const float e = __builtin_amdgcn_exp2f(a * a * (-0.5f * kLog2E)), t = recip<F32>(fmaf(0.35f, a, 1.f));
     float p = -0.0291258656f;
     p = fmaf(p, t, 0.143872231f);
     p = fmaf(p, t, -0.255504578f);
@@ -32,13 +31,13 @@ EWF_OPS_DEV Normal normal(float x)
     return {x < 0.f ? tail : 1.f - tail, e};
 }
 
-template <int ACT>
+template <typename T, int ACT>
 EWF_OPS_DEV float act_value(float x)
 {
     if constexpr (ACT == EWF_RELU) return x > 0.f ? x : x != x ? x : 0.f;
     else if constexpr (ACT == EWF_ACT_TANH) return tanhf(x);
-    else if constexpr (ACT == EWF_ACT_SIGMOID) return sigmoid(x);
-    else if constexpr (ACT == EWF_SILU) return x * sigmoid(x);
+    else if constexpr (ACT == EWF_ACT_SIGMOID) return sigmoid<T>(x);
+    else if constexpr (ACT == EWF_SILU) return x * sigmoid<T>(x);
     else if constexpr (ACT == EWF_GELU) return x * normal(x).below;
     else return x;
 }
@@ -47,14 +46,14 @@ EWF_OPS_DEV float act_value(float x)
 // sigmoid of 2 x, small numbers that 1 - tanh^2 would lose.  The slopes of silu and gelu are 0
 // and 1 in float32 long before +-128 (their distance is less than 2^-118 there): farther arguments, up to the infinities that
 // the largest floats' codes stand for in 32 bits, are taken as those, because x times a gate that is only nearly shut is not small for them.
-template <int ACT>
+template <typename T, int ACT>
 EWF_OPS_DEV float act_slope(float x)
 {
     if constexpr (ACT == EWF_SILU || ACT == EWF_GELU) x = x < -128.f ? -128.f : x > 128.f ? 128.f : x;
     if constexpr (ACT == EWF_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
-    else if constexpr (ACT == EWF_ACT_TANH) { float p, m; gate(2.f * x, p, m); return 4.f * (p * m); }
-    else if constexpr (ACT == EWF_ACT_SIGMOID) { float p, m; gate(x, p, m); return p * m; }
-    else if constexpr (ACT == EWF_SILU) { float p, m; gate(x, p, m); return fmaf(x * p, m, p); }
+    else if constexpr (ACT == EWF_ACT_TANH) { float p, m; gate<T>(2.f * x, p, m); return 4.f * (p * m); }
+    else if constexpr (ACT == EWF_ACT_SIGMOID) { float p, m; gate<T>(x, p, m); return p * m; }
+    else if constexpr (ACT == EWF_SILU) { float p, m; gate<T>(x, p, m); return fmaf(x * p, m, p); }
     else if constexpr (ACT == EWF_GELU) {
         const Normal n = normal(x);
         return fmaf(x * 0.39894228f, n.e, n.below);
@@ -101,7 +100,7 @@ __global__ void __launch_bounds__(256) k_act(ActLaunch a, Items items)
                          a.code_dtype == EWF_E4M3);
         if (a.y && c < cols) {
 #pragma unroll
-            for (int e = 0; e < V; e++) f[e] = act_value<ACT>(f[e]);
+            for (int e = 0; e < V; e++) f[e] = act_value<T, ACT>(f[e]);
             store_part<T>((raw *)a.y + row_offset(a.r, at[i].row, a.sy), c, cols, pack16<T>(f));
         }
     }
@@ -140,7 +139,7 @@ __global__ void __launch_bounds__(256) k_act_grad(ActLaunch a, Items items)
         decode_part<V>(code[i], byte[i], a.code_dtype == EWF_E4M3, f);
         if (a.dy) {
 #pragma unroll
-            for (int e = 0; e < V; e++) f[e] = element<T>(dy[i], e) * act_slope<ACT>(f[e]);
+            for (int e = 0; e < V; e++) f[e] = element<T>(dy[i], e) * act_slope<T, ACT>(f[e]);
         }
         store_part<T>((raw *)a.dx + row_offset(a.r, at[i].row, a.sdx), c, cols, pack16<T>(f));
     }

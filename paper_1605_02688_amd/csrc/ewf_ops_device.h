@@ -219,20 +219,46 @@ EWF_OPS_DEV float group_sum(float x)
 
 constexpr float kLog2E = 1.44269504f;
 
-// f = sigmoid(u) and 1 - f, both to within a few units in the last place: e = 2^(-u log2 e), f = 1 / (1 + e),
-// 1 - f = e f.  A gate of less than 2^-126 counts as zero and its complement as one, where e f would be infinity times zero; a
-// NaN stays one.
+// e = 2^(-u log2 e) = exp(-u) and f = 1 / (1 + e), by the type that results are stored as.  float32: the product's rounding and what
+// float32 drops of log2 e correct e to first order, one Newton step the reciprocal: two units in the last place of float32.  16 bits: the
+// native operations alone, off by up to |u| units, at most 2^-17 of a gate that is not shut, where half a step of float16 is 2^-11.
+template <typename T>
+EWF_OPS_DEV float exp_neg(float u)
+{
+    const float t = -u * kLog2E, e = __builtin_amdgcn_exp2f(t);
+    if constexpr (sizeof(typename T::raw) == 2) return e;
+    const float r = fmaf(-u, 1.92596299e-8f, fmaf(-u, kLog2E, -t));
+    return e * __builtin_amdgcn_fmed3f(fmaf(r, 0.693147182f, 1.f), 0.5f, 2.f);     // (the median drops the NaN of infinite u)
+}
+
+template <typename T>
+EWF_OPS_DEV float recip(float y)                        // y finite, from 1
+{
+    const float r = __builtin_amdgcn_rcpf(y);
+    if constexpr (sizeof(typename T::raw) == 2) return r;
+    return fmaf(fmaf(-y, r, 1.f), r, r);
+}
+
+// f = sigmoid(u) and 1 - f = e f, small ones relative to themselves.  A gate of less than 2^-126 counts as zero and its complement
+// as one, where e f would be infinity times zero; a NaN stays one.
+template <typename T>
 EWF_OPS_DEV void gate(float u, float &f, float &g)
 {
-    const float e = __builtin_amdgcn_exp2f(-u * kLog2E);
-    const float h = __builtin_amdgcn_rcpf(1.f + e);
+    const float e = exp_neg<T>(u);
     const bool shut = e > 0x1p126f;
+    const float h = recip<T>(1.f + e);
     f = shut ? 0.f : h;
     g = shut ? 1.f : e * h;
 }
 
-// sigmoid alone: 1 / (1 + 2^(-x log2 e)); e may overflow, and the result is then zero
-EWF_OPS_DEV float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2E)); }
+template <typename T>
+EWF_OPS_DEV float sigmoid(float x)
+{
+    if constexpr (sizeof(typename T::raw) == 2) return recip<T>(1.f + exp_neg<T>(x));        // (e may overflow: zero)
+    float f, g;
+    gate<T>(x, f, g);
+    return f;
+}
 
 // ------------------------------------------------------------------ 8 bits
 

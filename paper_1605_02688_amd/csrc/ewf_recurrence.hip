@@ -105,17 +105,17 @@ EWF_OPS_DEV int sequence_length(const RecLaunch &a, int64_t b)
 
 // One element's gradients from G, the gradient of its state; `f` and `before` are its gate and the state before it.  Returns what the
 // step hands to the one before.  Gates first: a product that a shut gate makes small does not overflow on the way.
-template <bool TIED>
+template <typename T, bool TIED>
 EWF_OPS_DEV float gradients(float G, float u, float w, float v, float before, float &du, float &dv, float &dw)
 {
     float f, g;
-    gate(u, f, g);
+    gate<T>(u, f, g);
     if constexpr (TIED) {
         dv = G * g;
         du = dv * f * (before - v);
     } else {
         float i, j;
-        gate(w, i, j);
+        gate<T>(w, i, j);
         dv = G * i;
         dw = dv * j * v;
         du = G * (f * g) * before;
@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(64) k_rec_walk(RecLaunch a)
 #pragma unroll
                 for (int e = 0; e < C; e++) {
                     float f, i, less;
-                    gate(u[k][e], f, i);
-                    if constexpr (!TIED) gate(w[k][e], i, less);
+                    gate<T>(u[k][e], f, i);
+                    if constexpr (!TIED) gate<T>(w[k][e], i, less);
                     s[e] = fmaf(f, s[e], i * v[k][e]);
                 }
                 store(a.h, t0 + k, s);
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(64) k_rec_walk(RecLaunch a)
                 for (int e = 0; e < C; e++) {
                     float before = h[k][e];
                     if (t == 0) before = e < l.have ? load_state(a.h0, b, c + e) : 0.f;
-                    s[e] = gradients<TIED>(dh[k][e] + s[e], u[k][e], TIED ? 0.f : w[k][e], v[k][e], before, du[e], dv[e], dw[e]);
+                    s[e] = gradients<T, TIED>(dh[k][e] + s[e], u[k][e], TIED ? 0.f : w[k][e], v[k][e], before, du[e], dv[e], dw[e]);
                 }
                 store(a.du, t, du);
                 store(a.dv, t, dv);
@@ -350,12 +350,12 @@ struct Tile {
     EWF_OPS_DEV void step_map(const Raw<T, BACK> &x, int e, float &f, float &b) const
     {
         if constexpr (BACK) {
-            f = sigmoid(x.u[e]);
+            f = sigmoid<T>(x.u[e]);
             b = f * x.dh[e];
         } else {
             float i, less;
-            gate(x.u[e], f, i);
-            if constexpr (!TIED) gate(x.w[e], i, less);
+            gate<T>(x.u[e], f, i);
+            if constexpr (!TIED) gate<T>(x.w[e], i, less);
             b = i * x.v[e];
         }
     }
@@ -434,7 +434,7 @@ struct Tile {
                 for (int e = 0; e < C; e++) {
                     float state = x.h[e];
                     if (from + r == len - 1) state = e < l.have ? load_state(a.h0, b, channel() + e) : 0.f;
-                    s[e] = gradients<TIED>(x.dh[e] + s[e], x.u[e], TIED ? 0.f : x.w[e], x.v[e], state, du[e], dv[e], dw[e]);
+                    s[e] = gradients<T, TIED>(x.dh[e] + s[e], x.u[e], TIED ? 0.f : x.w[e], x.v[e], state, du[e], dv[e], dw[e]);
                 }
                 put(pu, r, du);
                 put(pv, r, dv);

@@ -164,6 +164,11 @@ def act_relative_bounds(act, x):
     return a * below, below + a * density * (4 * x * x + 8) * U + slope * U
 
 
+# float32 gates, relative, over all of float32's range: e = exp(-u) is off by its native unit (2 U) and a correction's rounding, 1 + e by U,
+# its reciprocal by U and what one Newton step leaves; 1 - f = e f by another product
+GATE = 8 * U
+
+
 # ------------------------------------------------------------------ recurrence
 
 def recurrence(u, v, w, h0, lengths, dtype):

@@ -389,6 +389,27 @@ def test_activation_far_from_zero_to_its_own_precision(dtype, act, kind):
     ref.close("dx", dx, want, ref.stored(ref.act_relative_bounds(act, x8)[1], want, dt))
 
 
+def gate_arguments():
+    return torch.cat((torch.linspace(-80, 80, 3001), torch.randn(1095) * 4)).cuda()
+
+
+def test_float32_sigmoids_to_float32s_precision():
+    x = gate_arguments()[None]
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    codes, scales = torch.empty(x.shape, dtype=torch.int8, device="cuda"), torch.empty(1, 128, dtype=torch.uint8, device="cuda")
+    for act, rel, slope in (("sigmoid", ref.GATE, 2 * ref.GATE + ref.U), ("silu", ref.GATE + ref.U, None), ("tanh", None, 2 * ref.GATE + ref.U)):
+        ewf.activation(act, x, y, codes=codes, scales=scales, stream=stream())
+        if rel:
+            want = ref.ACTS[act][0](x.double())
+            ref.close(act, y, want, rel * want.abs() + ref.TINY[torch.float32])
+        if slope:
+            ewf.activation_grad(act, torch.ones_like(x), dx, codes=codes, scales=scales, stream=stream())
+            x8 = ref.keep8(x, "i8")[2]
+            want = ref.ACTS[act][1](x8)
+            normal = want > 2.0 ** -123                              # (a factor below 2^-126 counts as 0)
+            ref.close(act, dx[normal], want[normal], slope * want[normal])
+
+
 @pytest.mark.parametrize("dtype", sorted(DT))
 def test_activation_strides(dtype):
     dt, g = DT[dtype], gen(14)
@@ -582,6 +603,39 @@ def test_recurrence_shut_gates_forget_the_largest_states(T, tied):
     run(ewf.recurrence_grad, u, v, h, dh, du, dv, w=w, dw=dw, h0=h0, dh0=dh0, dlast=torch.full_like(h0, -1e38))
     dh[:, -1] += -1e38
     assert torch.equal(dv, dh) and (du == 0).all() and (dh0 == 0).all() and (tied or (dw == 0).all())
+
+
+@pytest.mark.parametrize("tied", (True, False))
+@pytest.mark.parametrize("T", (1, 40, 300))
+def test_recurrence_float32_gates_to_float32s_precision(T, tied):
+    # one step with gates to be looked at, the others hold what it leaves
+    x = gate_arguments()
+    D = x.numel()
+    u, v, w = torch.full((1, T, D), 200.0, device="cuda"), torch.zeros(1, T, D, device="cuda"), torch.full((1, T, D), -200.0, device="cuda")
+    u[0, 0], w[0, 0] = x, x
+    h, last, h0 = torch.empty_like(u), torch.empty(1, D, device="cuda"), torch.zeros(1, D, device="cuda")
+    f, g = torch.sigmoid(x.double()), torch.sigmoid(-x.double())
+    i = g if tied else f
+    some = dict(w=None if tied else w, h0=h0, last=last)
+    for a, b, want in ((1.0, 0.0, f), (0.0, 1.0, i)):                # from the state, from the input
+        h0.fill_(a)
+        v[0, 0] = b
+        run(ewf.recurrence, u, v, h, **some)
+        ref.close("last", last[0], want, (ref.GATE + ref.U) * want)
+        assert torch.equal(h[0, -1], last[0])
+    h0.fill_(1.0)
+    v.zero_()
+    du, dv, dw, dh0, dh = torch.empty_like(u), torch.empty_like(u), torch.empty_like(u), torch.empty_like(h0), torch.zeros_like(u)
+    dh[0, 0] = 1.0
+    if not tied:
+        v[0, 0] = 1.0
+    run(ewf.recurrence, u, v, h, **some)
+    run(ewf.recurrence_grad, u, v, h, dh, du, dv, w=some["w"], dw=None if tied else dw, h0=h0, dh0=dh0)
+    ref.close("dv", dv[0, 0], i, (ref.GATE + ref.U) * i)
+    ref.close("dh0", dh0[0], f, (ref.GATE + ref.U) * f)
+    ref.close("du", du[0, 0], f * g, (2 * ref.GATE + 3 * ref.U) * f * g)
+    if not tied:
+        ref.close("dw", dw[0, 0], f * g, (2 * ref.GATE + 3 * ref.U) * f * g)
 
 
 @pytest.mark.parametrize("T", (5, 333))
