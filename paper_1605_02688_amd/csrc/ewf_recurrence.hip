@@ -112,7 +112,7 @@ EWF_OPS_DEV float gradients(float G, float u, float w, float v, float before, fl
     gate<T>(u, f, g);
     if constexpr (TIED) {
         dv = G * g;
-        du = dv * f * (before - v);
+        du = dv * (f + f) * fmaf(0.5f, before, -0.5f * v);        // (halves: states of both signs may lie further apart than float32 reaches)
     } else {
         float i, j;
         gate<T>(w, i, j);

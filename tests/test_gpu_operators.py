@@ -606,6 +606,27 @@ def test_recurrence_shut_gates_forget_the_largest_states(T, tied):
 
 
 @pytest.mark.parametrize("tied", (True, False))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("T", (1, 9, 40, 333))
+def test_recurrence_gradients_of_the_largest_states(T, dtype, tied):
+    # shut gates, the largest inputs in turn positive and negative: two states are further apart than float32 reaches, and each gradient
+    # is finite; one gate stands half open
+    dt, g, D = DT[dtype], gen(25), 70
+    u, v = torch.full((2, T, D), -300.0, dtype=dt, device="cuda"), torch.full((2, T, D), 3e38, dtype=dt, device="cuda")
+    v[:, ::2] = -3e38
+    u[:, T // 2] = 0
+    c = dict(u=u, v=v, w=None if tied else torch.full_like(u, 300.0), h0=torch.full((2, D), 3e38, device="cuda"), lengths=None)
+    if not tied:
+        c["w"][:, T // 2] = 0
+    h, last = rec_forward(c)
+    check_rec(c, h, last)
+    dh, dlast = randn(g, 2, T, D, std=1e-3, dtype=dt), randn(g, 2, D, std=1e-3)
+    d = rec_backward(c, h, dh, dlast)
+    assert all(torch.isfinite(t).all() for t in d.values() if t is not None)
+    check_rec_grad(c, h, dh, dlast, d)
+
+
+@pytest.mark.parametrize("tied", (True, False))
 @pytest.mark.parametrize("T", (1, 40, 300))
 def test_recurrence_float32_gates_to_float32s_precision(T, tied):
     # one step with gates to be looked at, the others hold what it leaves
