@@ -257,6 +257,30 @@ def test_layer_norm_kept_in_8_bits(dtype, kind):
         check_norm_grad(dy, None, w, None, rstd, dx, dw, db, pt, n=n8)
 
 
+@pytest.mark.parametrize("kind", sorted(CODES))
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("cols", (1, 8, 33, 64, 136, 300, 1000, 1001, 1400, 2048, 4097, 4608, 8192, 8199, 12000, 16384, 20000, 40005))
+def test_layer_norm_kept_in_8_bits_block_by_block(cols, dtype, kind):
+    # A scale is that of n's block in 64 bits, but where the block's largest n lies within its own error of a border; a code is n's, but
+    # where n lies within its error of half a step
+    dt, rows, g = DT[dtype], 5, gen(cols)
+    x = randn(g, rows, cols, mean=0.3, std=1.7, dtype=dt)
+    x[1] *= torch.exp2(torch.arange(cols, device="cuda") % 64 // 4 - 8.0).to(dt)          # blocks of different powers in a row
+    y = torch.empty_like(x)
+    codes = torch.empty((rows, cols), dtype=CODES[kind], device="cuda")
+    scales = torch.full((rows, (cols + 31) // 32), 99, dtype=torch.uint8, device="cuda")
+    run(ewf.layer_norm, x, None, None, y, codes=codes, scales=scales)
+    want = ref.layer_norm(x, None, None, 1e-5, dt)
+    n, e = want["n"], want["e_n"]
+    lo, hi = (ref.keep8(torch.clamp_min(n.abs() + s * e, 0.0), kind)[1].int() for s in (-1, 1))
+    got = scales.int()
+    assert ((lo <= got) & (got <= hi)).all()
+    assert float((lo == hi).double().mean()) > 0.9 or cols < 64
+    unit = ref.pow2(got - 127).repeat_interleave(32, -1)[:, :cols]
+    step = unit if kind == "i8" else unit * ref.e4m3_step(torch.maximum(n.abs() + e, codes.double().abs() * unit) / unit)
+    ref.close("codes", codes.double() * unit, n, 0.5 * step + e)
+
+
 # ------------------------------------------------------------------ activations in 8 bits
 
 def special_values(dt):
