@@ -616,7 +616,7 @@ __global__ void __launch_bounds__(W * 64, BACK ? 4 : 1) k_rec_chain(RecLaunch a,
                     part[q] = totals[q][threadIdx.x];
                     all = after(part[q], all);
                 }
-            uint64_t *record = records + (uint64_t)place * back + chain * Tl::kStrip + threadIdx.x;
+            uint64_t *record = records + (uint64_t)place * back + (uint64_t)chain * Tl::kStrip + threadIdx.x;
             float state;
             if (place) {
                 publish(record, map_word(all));

@@ -984,3 +984,28 @@ def test_tensors_of_more_than_2_31_elements():
         want = ref.recurrence_grad(u[part], v[part], None, h[part], None, dh[part], None, None, bf)
         for k, got in (("du", du), ("dv", dv)):
             ref.close(k, got[part], want[k], want["e_" + k])
+
+
+def test_recurrence_of_more_than_2_32_records():
+    # 2^27 chains of two tiles, 32 records each; inputs that all sequences share, states of their own
+    torch.cuda.empty_cache()
+    B, T = (1 << 27) + 1000, 257
+    g = gen(91)
+    u, v = torch.full((1, T, 1), 8.0, dtype=torch.bfloat16, device="cuda"), randn(g, 1, T, 1, dtype=torch.bfloat16)
+    h0 = torch.rand(B, 1, device="cuda", generator=g) * 20 - 10
+    h, last = torch.empty(B, T, 1, dtype=torch.bfloat16, device="cuda"), torch.empty_like(h0)
+    say("recurrence", B, T, 1)
+    run(ewf.recurrence, u.expand(B, T, 1), v.expand(B, T, 1), h, h0=h0, last=last)
+    torch.cuda.synchronize()
+    # the last state is linear in the first, and its bound largest where that is
+    ends = torch.tensor([[0.0], [10.0]], device="cuda")
+    want = ref.recurrence(u.expand(2, T, 1), v.expand(2, T, 1), None, ends, None, torch.bfloat16)
+    offset, slope, bound = want["last"][0, 0], (want["last"][1, 0] - want["last"][0, 0]) / 10, float(want["e_last"].max())
+    for at in range(0, B, 1 << 24):
+        part = slice(at, min(B, at + (1 << 24)))
+        assert float((last[part].double() - (h0[part].double() * slope + offset)).abs().max()) <= bound, at
+    for part in (slice(0, 3), slice((1 << 27) - 2, (1 << 27) + 3), slice(B - 3, B)):
+        k = part.stop - part.start
+        check_rec(dict(u=u.expand(k, T, 1), v=v.expand(k, T, 1), w=None, h0=h0[part], lengths=None), h[part], last[part])
+    del h, last, h0
+    torch.cuda.empty_cache()
