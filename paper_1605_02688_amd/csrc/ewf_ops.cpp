@@ -175,8 +175,12 @@ ewf_status base_shape(const char *name, const ewf_tensor &t, int32_t ndim, int64
     return EWF_OK;
 }
 
-ewf_status launched(const char *what)
+// Launches, and says what came of it (an error that an earlier call of the program's has left unread is not this one's).
+template <typename F>
+ewf_status launched(const char *what, F &&launch)
 {
+    (void)hipGetLastError();
+    launch();
     hipError_t he = hipGetLastError();
     if (he == hipSuccess) return EWF_OK;
     set_error("%s: %s", what, hipGetErrorString(he));
@@ -420,8 +424,7 @@ ewf_status rec_run(const ewf_recurrence_args *a, bool grad, void *workspace, siz
     if (st != EWF_OK) return st;
     if (n.batch == 0 || n.channels == 0) return EWF_OK;
     n.workspace = workspace;
-    launch_recurrence(n, grad, units, (hipStream_t)stream);
-    return launched(grad ? "recurrence, backward" : "recurrence");
+    return launched(grad ? "recurrence, backward" : "recurrence", [&] { launch_recurrence(n, grad, units, (hipStream_t)stream); });
 }
 
 }  // namespace
@@ -435,8 +438,7 @@ ewf_status ewf_layer_norm(const ewf_layer_norm_args *a, void *hip_stream)
         ewf_status st = norm_layout(a, false, n);
         if (st != EWF_OK) return st;
         if (n.r.rows == 0) return EWF_OK;
-        launch_layer_norm(n, device_cu_count(), (hipStream_t)hip_stream);
-        return launched("layer normalisation");
+        return launched("layer normalisation", [&] { launch_layer_norm(n, device_cu_count(), (hipStream_t)hip_stream); });
     });
 }
 
@@ -463,8 +465,7 @@ ewf_status ewf_layer_norm_grad(const ewf_layer_norm_args *a, void *workspace, si
         if (n.r.rows == 0 && !n.dweight && !n.dbias) return EWF_OK;
         // (a workspace that the call does not need is not looked at, neither its size nor its alignment, and not written)
         n.partials = need ? (float *)workspace : nullptr;
-        launch_layer_norm_grad(n, (hipStream_t)hip_stream);
-        return launched("layer normalisation, backward");
+        return launched("layer normalisation, backward", [&] { launch_layer_norm_grad(n, (hipStream_t)hip_stream); });
     });
 }
 
@@ -475,8 +476,7 @@ ewf_status ewf_activation(const ewf_activation_args *a, void *hip_stream)
         ewf_status st = act_layout(a, ActCall::Forward, n);
         if (st != EWF_OK) return st;
         if (n.r.rows == 0 || n.r.cols == 0) return EWF_OK;
-        launch_activation(n, (hipStream_t)hip_stream);
-        return launched("activation");
+        return launched("activation", [&] { launch_activation(n, (hipStream_t)hip_stream); });
     });
 }
 
@@ -487,8 +487,7 @@ ewf_status ewf_activation_grad(const ewf_activation_args *a, void *hip_stream)
         ewf_status st = act_layout(a, ActCall::Grad, n);
         if (st != EWF_OK) return st;
         if (n.r.rows == 0 || n.r.cols == 0) return EWF_OK;
-        launch_activation_grad(n, (hipStream_t)hip_stream);
-        return launched("activation, backward");
+        return launched("activation, backward", [&] { launch_activation_grad(n, (hipStream_t)hip_stream); });
     });
 }
 
@@ -499,8 +498,7 @@ ewf_status ewf_read8(const ewf_activation_args *a, void *hip_stream)
         ewf_status st = act_layout(a, ActCall::Read, n);
         if (st != EWF_OK) return st;
         if (n.r.rows == 0 || n.r.cols == 0) return EWF_OK;
-        launch_read8(n, (hipStream_t)hip_stream);
-        return launched("reading 8 bits");
+        return launched("reading 8 bits", [&] { launch_read8(n, (hipStream_t)hip_stream); });
     });
 }
 

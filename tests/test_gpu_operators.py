@@ -884,6 +884,19 @@ def test_workspace_of_the_wrong_size_is_refused():
     assert e.value.status == ewf.ENOMEM
 
 
+def test_an_error_of_an_earlier_call_is_not_the_operators():
+    import ctypes
+    hip = ctypes.CDLL(next(line.split()[-1] for line in open("/proc/self/maps") if "libamdhip64" in line))
+    calls = small_calls(gen(72))
+    try:
+        for call, _ in calls:
+            assert hip.hipSetDevice(99) != 0                          # refused, and left unread
+            call.launch(stream())
+    finally:
+        hip.hipGetLastError()
+    torch.cuda.synchronize()
+
+
 # ------------------------------------------------------------------ all together
 
 def test_a_block_of_a_recurrent_language_model():
