@@ -282,9 +282,11 @@ ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *fail
  * its backward pass.  The conventions above hold: tensors are strided views of the caller's device memory, strides in
  * elements and >= 0, nothing is allocated, synchronised or kept between calls, launches go to the caller's stream (of
  * the current device) and may be captured into a HIP graph, sums are folded in a fixed order (equal calls give equal
- * bits), errors are statuses with a text.  A workspace needs no initialisation; calls that may overlap in time must not
+ * bits), errors are statuses with a text.  A workspace needs no initialisation and overlaps no tensor of the call; one that a
+ * call does not need is not looked at.  Calls that may overlap in time must not
  * share one (that includes two captured graphs): results are then undefined, and those of a recurrence may come after
- * seconds of waiting, as NaN.
+ * seconds of waiting, as NaN (a part of a recurrence that has waited for another for some four million looks gives up so; a launch has
+ * no other way to say it).
  *
  * An argument structure is zeroed by the caller and filled in: a tensor whose ptr and shape are both NULL is absent.
  * Tensors are EWF_F32, EWF_F16 or EWF_BF16 as the structure's `dtype` says; arithmetic, sums, statistics and states
@@ -300,7 +302,9 @@ ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *fail
  * common to all tensors the call is EWF_EUNSUPPORTED.  A row whose sums leave float32's range gives infinities or NaN.
  *
  * ewf_layer_norm reads x and writes y; optional: weight, bias (absent: 1 and 0), mean and rstd (float32, the shape
- * of x without its last axis) to be written, codes and scales to be written (n in 8 bits, see ewf_activation).
+ * of x without its last axis) to be written, codes and scales to be written (n in 8 bits, see ewf_activation; n is itself computed
+ * in float32, so that a code may be its neighbour's where n lies within a few roundings of half a step, and a scale where
+ * the block's largest n does of a border: about one code in a million from those of n in 64 bits).
  * y may lie over x.
  * ewf_layer_norm_grad reads dy, rstd and either x and mean or codes and scales (which then stand for n), and writes
  * dx; optional: weight, dweight, dbias.  dx may lie over dy or x.  The gradients of no rows are zero.
@@ -320,8 +324,8 @@ ewf_status ewf_layer_norm_grad(const ewf_layer_norm_args *a, void *workspace, si
 /* Activations kept in 8 bits.  Blocks of 32 elements along the last axis (the last block of a row may be shorter) share
  * a scale 2^k, the smallest with k >= -126 and max |x| <= L 2^k, L = 127 (EWF_I8) or 448 (EWF_E4M3); an element's code
  * is x 2^-k rounded to nearest, ties to even, as a signed byte or as a float of 4 exponent and 3 mantissa bits; it
- * stands for code 2^k.  The scale is stored as the byte k + 127.  Both steps are exact but for the one rounding, so codes are
- * defined to the bit.  A block that holds a NaN or an infinity has scale byte 255 and codes 0, and stands for NaN.
+ * stands for code 2^k.  The scale is stored as the byte k + 127.  Both steps are exact but for the one rounding, so the codes of a
+ * tensor that is read are defined to the bit.  A block that holds a NaN or an infinity has scale byte 255 and codes 0, and stands for NaN.
  * codes has the shape of x, scales that of x with ceil(cols / 32) as its last extent; both are bytes.
  *
  * ewf_activation reads x and writes y = act(x) (may lie over x) and codes and scales of x; either may be absent.

@@ -211,8 +211,11 @@ EWF_OPS_DEV void normalised(const NormLaunch &a, u32x4 x, float mean, float rstd
 
 // One sweep over dy and x: a workgroup takes rows in turn and its threads keep their columns' sums for dweight and
 // dbias in registers; what remains across workgroups is one partial per workgroup, folded by k_norm_finish.
-// Rows that are cut: registers for two workgroups a unit (from 8 bits the compiler takes a few more by itself: float16 [20011, 1001] 33.9 us
-// and 44.9, [61060, 25] 18.6 and 25.8; from x bfloat16 [8192, 4001] 44.6 and 51.4).
+// Rows that are cut: registers for two workgroups a unit, up to 512 threads of two vectors (without the bound: float16 from 8 bits [20011,
+// 1001] 33.9 us and 44.9, [61060, 25] 18.6 and 25.8; from x bfloat16 [8192, 4001] 44.6 and 51.4).  What does not fit spills: in 16 bits from
+// codes 2 to 8 registers, on 512 threads 20 (float16 [8192, 7001] writes 165 MB for 143), from x at most 4.  Workgroups of 1024
+// threads hold 128 registers a thread whatever is asked for: whole rows spill 8 to 10 (bfloat16 [8192, 16384] 248 us, 336 MB written for 302),
+// cut ones 73 from x and 220 to 234 from codes (float16 [143, 14170] 17 and 25 us, 37 and 61 MB written for 20).
 template <typename T, int TPR, int NV, bool CUT, bool KEPT>
 __global__ void __launch_bounds__(Held<TPR>::threads, CUT && NV == 2 && TPR <= kThreads ? 4 : 1) k_norm_grad(NormLaunch a)
 {

@@ -508,7 +508,8 @@ __global__ void __launch_bounds__(W * 64) k_rec_march(RecLaunch a)
 // that run or are done, and it publishes its own map before it waits; the first tile waits for none, and each next one
 // only for words that workgroups publish without waiting, or after a wait that has ended.  Where a caller breaks the
 // rule that overlapping calls have workspaces of their own, words can be lost: a wait is given up after kMostLooks
-// looks (seconds; a tile takes microseconds), and the channel's states from there on are NaN.  A place that is not one of the
+// looks (seconds; a tile takes microseconds), and the channel's states from there on are NaN.  The looks are counted by the wavefront
+// that waits: while its queue is held back it does not look either.  A place that is not one of the
 // chain's is not taken: whatever the workspace holds, every access is in bounds.
 
 constexpr uint32_t kMapBit = 1u << 30, kStateBit = 1u << 31;
@@ -567,8 +568,10 @@ EWF_OPS_DEV float search(const uint64_t *record, int64_t back, int place)
     }
 }
 
-// (backward: registers for four wavefronts on each of a unit's four SIMDs, two workgroups; with two gates the compiler takes
-// a few more by itself, and the second workgroup is worth more: bfloat16 [8, 4096, 2048] 249 us and 264)
+// (backward: registers for four wavefronts on each of a unit's four SIMDs, two workgroups; with two gates the wide tile then spills 9
+// (float32), 13 (float16) and 19 (bfloat16) registers, and the second workgroup is worth more: bfloat16 [8, 4096, 2048] 249 us, 545 MB
+// written for 420, and 264.  Forward long tiles have 224 registers in 16 bits, 163 in float32: one workgroup a unit, which loads nothing while it
+// searches)
 template <typename T, bool TIED, bool BACK, int L, int R, int W, bool FEW>
 __global__ void __launch_bounds__(W * 64, BACK ? 4 : 1) k_rec_chain(RecLaunch a, uint32_t chains, uint32_t tiles)
 {
