@@ -220,8 +220,9 @@ EWF_OPS_DEV float group_sum(float x)
 constexpr float kLog2E = 1.44269504f;
 
 // e = 2^(-u log2 e) = exp(-u) and f = 1 / (1 + e), by the type that results are stored as.  float32: the product's rounding and what
-// float32 drops of log2 e correct e to first order, one Newton step the reciprocal: two units in the last place of float32.  16 bits: the
-// native operations alone, off by up to |u| units, at most 2^-17 of a gate that is not shut, where half a step of float16 is 2^-11.
+// float32 drops of log2 e correct e to first order, one Newton step the reciprocal: f and 1 - f are off by at most 4.6 times 2^-24 (2^25
+// arguments up to 86).  16 bits: the native operations alone, off by about |u| times 2^-24, at most 2^-18 of a gate that is not shut, where half
+// a step of float16 is 2^-11.
 template <typename T>
 EWF_OPS_DEV float exp_neg(float u)
 {
