@@ -19,7 +19,7 @@
  *   ewf_run_static                the same without a caller's workspace      (asynchronous)
  *
  * Beside the expressions the library has operators of sequence models with kernels of their own
- * (ewf_layer_norm, ewf_activation, ewf_recurrence and their backward passes, below).
+ * (ewf_layer_norm, ewf_activation, ewf_recurrence, ewf_token_logprobs, ewf_distill and their backward passes, below).
  *
  * Conventions
  *   - Every function returns 0 (EWF_OK) or a negative ewf_status.  No C++ exception crosses
@@ -277,9 +277,9 @@ ewf_status ewf_run_sequence(const ewf_call *calls, int32_t ncalls, int32_t *fail
 
 /* ---- operators of sequence models ----
  *
- * Three operators whose kernels are written by hand, beside the expressions above: layer normalisation, activations
- * whose argument is kept in 8 bits for the backward pass, and a gated linear recurrence over time; each with
- * its backward pass.  The conventions above hold: tensors are strided views of the caller's device memory, strides in
+ * Five operators whose kernels are written by hand, beside the expressions above: layer normalisation, activations
+ * whose argument is kept in 8 bits for the backward pass, a gated linear recurrence over time, log probabilities of tokens
+ * with entropy and alternatives, and the loss against a teacher's top logits; each with its backward pass.  The conventions above hold: tensors are strided views of the caller's device memory, strides in
  * elements and >= 0, nothing is allocated, synchronised or kept between calls, launches go to the caller's stream (of
  * the current device) and may be captured into a HIP graph, sums are folded in a fixed order (equal calls give equal
  * bits), errors are statuses with a text.  A workspace needs no initialisation and overlaps no tensor of the call; one that a
@@ -372,6 +372,65 @@ ewf_status ewf_recurrence_workspace(const ewf_recurrence_args *a, size_t *worksp
 ewf_status ewf_recurrence(const ewf_recurrence_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
 ewf_status ewf_recurrence_grad_workspace(const ewf_recurrence_args *a, size_t *workspace_bytes);
 ewf_status ewf_recurrence_grad(const ewf_recurrence_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Log probabilities of given tokens under rows of logits (the last axis of `logits`, 1 .. 2^24 of them, rank ndim 1 ..
+ * EWF_MAX_DIMS; the axes before it are the rows, as for layer normalisation), for scoring, sampling and training:
+ *     peak = max x,  logsum = log sum exp(scale (x - peak)),  log p_j = scale (x_j - peak) - logsum,
+ *     logprob = log p_token,  entropy = - sum p_j log p_j   (p_j = 0 counts 0)
+ * and the `k` most likely tokens, k = 1 .. 128: top_indices, by descending logit, equal ones by ascending index, and
+ * top_values, their log p.  scale is one over the temperature, 2^-64 .. 2^64.
+ * tokens is int32, top_indices int32 [..., k], top_values float32 [..., k], the other results float32, each with the shape of logits
+ * without its last axis; every result is optional, logprob comes with tokens.  Without tokens all rows count; with them a
+ * row whose token is outside 0 .. cols - 1 is padding: its logits are not read, its results are 0, and it has no alternatives.
+ * Alternatives that do not exist (logits of minus infinity, k > cols) have index -1 and value minus infinity.  In a row without any logit above
+ * minus infinity peak, logsum and logprob are minus infinity and entropy is 0.  A row that holds a NaN or plus infinity has NaN in all its
+ * results, and indices -1.  The lowest finite number is a logit like others.
+ *
+ * ewf_token_logprobs_grad: with g = dlogprob and h = dentropy (float32, one of them at least; dlogprob comes with tokens, dentropy with
+ * entropy)
+ *     dlogits_j = scale (g ([j = token] - p_j) - h p_j (log p_j + entropy)),
+ * from logits, peak, logsum and entropy as ewf_token_logprobs wrote them; 0 for rows of padding and for rows without any logit.
+ * Alternatives have no gradient.  dlogits has the logits' type and may lie over logits. */
+typedef struct {
+    ewf_tensor logits, tokens, logprob, peak, logsum, entropy, top_values, top_indices, dlogprob, dentropy, dlogits;
+    int32_t dtype;            /* ewf_dtype of logits and dlogits                            */
+    int32_t ndim;
+    float scale;
+    int32_t reserved;         /* 0                                                          */
+} ewf_token_logprobs_args;
+ewf_status ewf_token_logprobs_workspace(const ewf_token_logprobs_args *a, size_t *workspace_bytes);
+ewf_status ewf_token_logprobs(const ewf_token_logprobs_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
+ewf_status ewf_token_logprobs_grad(const ewf_token_logprobs_args *a, void *hip_stream);
+
+/* The loss of rows of a student's logits (as above) against a teacher's entries: teacher_indices (int32 [..., k], k = 1 .. 128)
+ * and teacher_values ([..., k], teacher_dtype: dtype or EWF_F32).  An entry whose index is outside 0 .. cols - 1 does not exist, whatever its
+ * value; an index that comes twice counts with both its probabilities.  log p as above.
+ * Without `tail`, q = softmax(teacher_scale teacher_values) over the entries that exist, and
+ *     loss = sum_i q_i (log q_i - log p_(index i)),   dlogits_j = dloss scale (p_j - sum of the q_i with index j).
+ * With `tail` the values are log probabilities (as ewf_token_logprobs writes top_values), q_i = exp(teacher_scale value_i), and the rest of the
+ * vocabulary is one more class: q_t = max(0, 1 - sum q), p_t = the sum of p over the tokens that no entry names,
+ *     loss = sum_i q_i (log q_i - log p_(index i)) + q_t (log q_t - log p_t),
+ *     dlogits_j = dloss scale (m p_j - sum of the q_i with index j, or where there is no such entry - q_t p_j / p_t),   m = q_t + sum q;
+ * a tail with p_t < 2^-126 (nothing is left of the vocabulary, or masks) does not count: q_t is taken as 0.
+ * Terms with q = 0 count 0.  A row without entries is padding, its logits are not read, results and gradients are 0; so are loss and gradient
+ * where all values are minus infinity and there is no tail.  A student's row without any logit above minus infinity has p = 0 and, where some
+ * q > 0, an infinite loss.  A NaN or plus infinity among a row's logits, or among the values of entries that exist, makes its loss and gradient
+ * NaN or infinite (logits: NaN).
+ *
+ * ewf_distill writes loss and, where given, peak, logsum and tail (log of the sum of exp(scale (x - peak)) over the tail; its presence chooses the
+ * second form): float32, the shape of logits without its last axis; and, with dlogits, the gradient for the weights dloss (float32, the same shape;
+ * absent: 1) in the same call, which may lie over logits.
+ * ewf_distill_grad writes the gradient alone, from peak, logsum and, for the second form, tail, as ewf_distill wrote them. */
+typedef struct {
+    ewf_tensor logits, teacher_values, teacher_indices, loss, peak, logsum, tail, dloss, dlogits;
+    int32_t dtype, teacher_dtype;             /* ewf_dtype                                  */
+    int32_t ndim;
+    float scale, teacher_scale;               /* 2^-64 .. 2^64                              */
+    int32_t reserved;         /* 0                                                          */
+} ewf_distill_args;
+ewf_status ewf_distill_workspace(const ewf_distill_args *a, size_t *workspace_bytes);
+ewf_status ewf_distill(const ewf_distill_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
+ewf_status ewf_distill_grad(const ewf_distill_args *a, void *hip_stream);
 
 const char *ewf_last_error(void);
 

@@ -1,5 +1,5 @@
-// The operators of sequence models: argument checks and layouts.  The kernels are in ewf_norm.hip, ewf_act8.hip and
-// ewf_recurrence.hip; everything that they assume about their operands is established here.
+// The operators of sequence models: argument checks and layouts.  The kernels are in ewf_norm.hip, ewf_act8.hip,
+// ewf_recurrence.hip and ewf_vocab.hip; everything that they assume about their operands is established here.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -127,8 +127,9 @@ struct Call {
 
 // The axes before the last of the row tensors, merged into at most two that all of them share.
 struct RowLayout {
+    static constexpr int kMaxRowTensors = 12;
     struct Entry { const ewf_tensor *t; RowStride *to; };
-    Entry e[8];
+    Entry e[kMaxRowTensors];
     size_t n = 0;
     void add(const ewf_tensor &t, RowStride *to) { if (present(t)) e[n++] = {&t, to}; }
 
@@ -138,7 +139,7 @@ struct RowLayout {
         for (int d = 0; d < lead; d++) total *= (double)shape[d];
         if (total > (double)kMaxRows) { set_error("%.0f rows: fewer than 2^31 are supported", total); return EWF_ESHAPE; }
         if (total == 0) { r.rows = 0; r.n1 = 1; return EWF_OK; }
-        struct Axis { int64_t ext, st[8]; } axes[kMaxDims];
+        struct Axis { int64_t ext, st[kMaxRowTensors]; } axes[kMaxDims];
         int naxes = 0;
         for (int d = 0; d < lead; d++) {
             if (shape[d] == 1) continue;
@@ -427,9 +428,247 @@ ewf_status rec_run(const ewf_recurrence_args *a, bool grad, void *workspace, siz
     return launched(grad ? "recurrence, backward" : "recurrence", [&] { launch_recurrence(n, grad, units, (hipStream_t)stream); });
 }
 
+// ------------------------------------------------------------------ rows of logits
+
+constexpr int64_t kMaxVocab = (int64_t)1 << 24;
+
+// What the operators over a vocabulary have in common: their logits, scale and results by row.
+struct VocabCall {
+    Call c;
+    RowLayout l;
+    VocabLaunch &n;
+    int64_t shape[kMaxDims];
+    int nd = 0;
+
+    explicit VocabCall(VocabLaunch &n) : n(n) { n = VocabLaunch(); }
+
+    ewf_status begin(const ewf_tensor &logits, int32_t dtype, int32_t ndim, float scale)
+    {
+        if (!is_float(dtype)) { set_error("tensors are float32, float16 or bfloat16"); return c.fail(EWF_ETYPE); }
+        ewf_status st = base_shape("logits", logits, ndim, shape);
+        if (st != EWF_OK) return c.fail(st);
+        nd = ndim;
+        if (shape[nd - 1] < 1 || shape[nd - 1] > kMaxVocab) {
+            set_error("rows of %lld logits: 1 to 2^24 are supported", (long long)shape[nd - 1]);
+            return c.fail(EWF_ESHAPE);
+        }
+        if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) { set_error("scale: 2^-64 to 2^64 are supported"); return c.fail(EWF_EINVAL); }
+        n.dtype = dtype;
+        n.scale = scale;
+        n.c = scale * 1.44269504f;
+        n.lag = 8.f / n.c;
+        full("logits", logits, false, true, &n.slogits);
+        n.logits = logits.ptr;
+        return c.status;
+    }
+    void full(const char *name, const ewf_tensor &t, bool out, bool required, RowStride *to)
+    {
+        if (!c.add(name, t, float_size(n.dtype), nd, shape, out, required)) return;
+        c.unit_last(t, name, nd);
+        l.add(t, to);
+    }
+    // A number a row: 4 bytes.
+    template <typename P> void column(const char *name, const ewf_tensor &t, bool out, bool required, RowStride *to, P *&p)
+    {
+        if (!c.add(name, t, 4, nd - 1, shape, out, required)) return;
+        l.add(t, to);
+        p = (P *)t.ptr;
+    }
+    // `count` elements a row; count is the first such tensor's.
+    bool few(const char *name, const ewf_tensor &t, int isz, bool out, int &count, RowStride *to)
+    {
+        if (c.status != EWF_OK) return false;
+        if (!present(t)) { set_error("%s is needed", name); c.fail(EWF_EINVAL); return false; }
+        if (!t.shape || !t.strides) { set_error("%s: null shape or strides", name); c.fail(EWF_EINVAL); return false; }
+        int64_t s[kMaxDims];
+        for (int d = 0; d < nd; d++) s[d] = shape[d];
+        s[nd - 1] = count ? count : t.shape[nd - 1];
+        if (s[nd - 1] < 1 || s[nd - 1] > kMaxTop) {
+            set_error("%s: %lld a row: 1 to %d are supported", name, (long long)s[nd - 1], kMaxTop);
+            c.fail(EWF_ESHAPE);
+            return false;
+        }
+        if (!c.add(name, t, isz, nd, s, out, true)) return false;
+        if (c.unit_last(t, name, nd) != EWF_OK) return false;
+        count = (int)s[nd - 1];
+        l.add(t, to);
+        return true;
+    }
+    ewf_status end()
+    {
+        if (c.status != EWF_OK) return c.status;
+        ewf_status st = l.merge(shape, nd - 1, n.r);
+        n.r.cols = (int32_t)shape[nd - 1];
+        return st;
+    }
+};
+
+ewf_status logprobs_layout(const ewf_token_logprobs_args *a, bool grad, VocabLaunch &n)
+{
+    if (!a) { set_error("null arguments"); return EWF_EINVAL; }
+    if (a->reserved) { set_error("reserved must be 0"); return EWF_EINVAL; }
+    VocabCall v(n);
+    if (v.begin(a->logits, a->dtype, a->ndim, a->scale) != EWF_OK) return v.c.status;
+    v.column("tokens", a->tokens, false, false, &n.stokens, n.tokens);
+    if (!grad) {
+        if (v.c.status == EWF_OK && present(a->logprob) && !present(a->tokens)) { set_error("logprob comes with tokens"); return EWF_EINVAL; }
+        v.column("logprob", a->logprob, true, false, &n.slogprob, n.logprob);
+        v.column("peak", a->peak, true, false, &n.speak, n.peak);
+        v.column("logsum", a->logsum, true, false, &n.slogsum, n.logsum);
+        v.column("entropy", a->entropy, true, false, &n.sentropy, n.entropy);
+        if (v.c.status == EWF_OK && present(a->top_values) != present(a->top_indices)) {
+            set_error("top_values and top_indices come together");
+            return EWF_EINVAL;
+        }
+        if (present(a->top_values)) {
+            v.few("top_values", a->top_values, 4, true, n.top, &n.stop_values);
+            v.few("top_indices", a->top_indices, 4, true, n.top, &n.stop_indices);
+            n.top_values = (float *)a->top_values.ptr;
+            n.top_indices = (int32_t *)a->top_indices.ptr;
+        }
+        if (v.c.status == EWF_OK && !present(a->logprob) && !present(a->peak) && !present(a->logsum) && !present(a->entropy) && !n.top) {
+            set_error("a result is needed: logprob, peak, logsum, entropy or top_values and top_indices");
+            return EWF_EINVAL;
+        }
+        v.c.check_results({});
+    } else {
+        if (v.c.status == EWF_OK && !present(a->dlogprob) && !present(a->dentropy)) { set_error("dlogprob or dentropy is needed"); return EWF_EINVAL; }
+        if (v.c.status == EWF_OK && present(a->dlogprob) && !present(a->tokens)) { set_error("dlogprob comes with tokens"); return EWF_EINVAL; }
+        v.column("peak", a->peak, false, true, &n.speak, n.peak);
+        v.column("logsum", a->logsum, false, true, &n.slogsum, n.logsum);
+        v.column("dlogprob", a->dlogprob, false, false, &n.sdlogprob, n.dlogprob);
+        v.column("dentropy", a->dentropy, false, false, &n.sdentropy, n.dentropy);
+        v.column("entropy", a->entropy, false, present(a->dentropy), &n.sentropy, n.entropy);
+        v.full("dlogits", a->dlogits, true, true, &n.sdlogits);
+        n.dlogits = a->dlogits.ptr;
+        v.c.check_results({{"dlogits", "logits"}});
+    }
+    ewf_status st = v.end();
+    if (st == EWF_OK && !grad) plan_vocab(n, device_cu_count());
+    return st;
+}
+
+ewf_status distill_layout(const ewf_distill_args *a, bool grad, VocabLaunch &n)
+{
+    if (!a) { set_error("null arguments"); return EWF_EINVAL; }
+    if (a->reserved) { set_error("reserved must be 0"); return EWF_EINVAL; }
+    VocabCall v(n);
+    if (v.begin(a->logits, a->dtype, a->ndim, a->scale) != EWF_OK) return v.c.status;
+    if (a->teacher_dtype != a->dtype && a->teacher_dtype != EWF_F32) { set_error("the teacher's values have the logits' type or float32"); return EWF_ETYPE; }
+    if (!(a->teacher_scale >= 0x1p-64f && a->teacher_scale <= 0x1p64f)) { set_error("teacher_scale: 2^-64 to 2^64 are supported"); return EWF_EINVAL; }
+    n.teacher_dtype = a->teacher_dtype;
+    n.teacher_scale = a->teacher_scale;
+    n.with_tail = present(a->tail);
+    if (v.few("teacher_values", a->teacher_values, float_size(a->teacher_dtype), false, n.entries, &n.steacher_values))
+        v.few("teacher_indices", a->teacher_indices, 4, false, n.entries, &n.steacher_indices);
+    n.teacher_values = a->teacher_values.ptr;
+    n.teacher_indices = (const int32_t *)a->teacher_indices.ptr;
+    if (!grad) v.column("loss", a->loss, true, true, &n.sloss, n.loss);
+    v.column("peak", a->peak, !grad, grad, &n.speak, n.peak);
+    v.column("logsum", a->logsum, !grad, grad, &n.slogsum, n.logsum);
+    v.column("tail", a->tail, !grad, false, &n.stail, n.tail);
+    if (v.c.status == EWF_OK && !grad && present(a->dloss) && !present(a->dlogits)) { set_error("dloss comes with dlogits"); return EWF_EINVAL; }
+    v.column("dloss", a->dloss, false, false, &n.sdloss, n.dloss);
+    v.full("dlogits", a->dlogits, true, grad, &n.sdlogits);
+    n.dlogits = a->dlogits.ptr;
+    v.c.check_results({{"dlogits", "logits"}});
+    ewf_status st = v.end();
+    if (st == EWF_OK && !grad) plan_vocab(n, device_cu_count());
+    return st;
+}
+
+// The parts of rows that several workgroups share, and the statistics of a loss whose gradient is a launch of its own and which
+// keeps none.
+size_t vocab_workspace(VocabLaunch &n, void *workspace)
+{
+    size_t bytes = 0;
+    auto take = [&](size_t more) {
+        void *at = workspace ? (char *)workspace + bytes : nullptr;
+        bytes += (more + 15) / 16 * 16;
+        return at;
+    };
+    const size_t rows = n.r.rows, parts = rows * (size_t)n.splits;
+    if (n.splits > 1) {
+        n.parts = (float *)take(parts * 4 * sizeof(float));
+        n.part_keys = (unsigned long long *)take(parts * (size_t)n.top * sizeof(unsigned long long));
+    }
+    if (n.entries && n.dlogits && !n.held) {
+        const RowStride dense{(int64_t)n.r.n1, 1};
+        if (!n.peak) { n.peak = (float *)take(rows * sizeof(float)); n.speak = dense; }
+        if (!n.logsum) { n.logsum = (float *)take(rows * sizeof(float)); n.slogsum = dense; }
+    }
+    return bytes;
+}
+
 }  // namespace
 
 extern "C" {
+
+ewf_status ewf_token_logprobs_workspace(const ewf_token_logprobs_args *a, size_t *workspace_bytes)
+{
+    return guarded([&]() -> ewf_status {
+        if (!workspace_bytes) { set_error("null argument"); return EWF_EINVAL; }
+        VocabLaunch n;
+        ewf_status st = logprobs_layout(a, false, n);
+        if (st == EWF_OK) *workspace_bytes = vocab_workspace(n, nullptr);
+        return st;
+    });
+}
+
+ewf_status ewf_token_logprobs(const ewf_token_logprobs_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&]() -> ewf_status {
+        VocabLaunch n;
+        ewf_status st = logprobs_layout(a, false, n);
+        if (st != EWF_OK) return st;
+        st = workspace_fits(vocab_workspace(n, workspace), workspace, workspace_bytes);
+        if (st != EWF_OK || n.r.rows == 0) return st;
+        return launched("log probabilities", [&] { launch_token_logprobs(n, (hipStream_t)hip_stream); });
+    });
+}
+
+ewf_status ewf_token_logprobs_grad(const ewf_token_logprobs_args *a, void *hip_stream)
+{
+    return guarded([&]() -> ewf_status {
+        VocabLaunch n;
+        ewf_status st = logprobs_layout(a, true, n);
+        if (st != EWF_OK || n.r.rows == 0) return st;
+        return launched("log probabilities, backward", [&] { launch_token_logprobs_grad(n, (hipStream_t)hip_stream); });
+    });
+}
+
+ewf_status ewf_distill_workspace(const ewf_distill_args *a, size_t *workspace_bytes)
+{
+    return guarded([&]() -> ewf_status {
+        if (!workspace_bytes) { set_error("null argument"); return EWF_EINVAL; }
+        VocabLaunch n;
+        ewf_status st = distill_layout(a, false, n);
+        if (st == EWF_OK) *workspace_bytes = vocab_workspace(n, nullptr);
+        return st;
+    });
+}
+
+ewf_status ewf_distill(const ewf_distill_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return guarded([&]() -> ewf_status {
+        VocabLaunch n;
+        ewf_status st = distill_layout(a, false, n);
+        if (st != EWF_OK) return st;
+        st = workspace_fits(vocab_workspace(n, workspace), workspace, workspace_bytes);
+        if (st != EWF_OK || n.r.rows == 0) return st;
+        return launched("distillation", [&] { launch_distill(n, (hipStream_t)hip_stream); });
+    });
+}
+
+ewf_status ewf_distill_grad(const ewf_distill_args *a, void *hip_stream)
+{
+    return guarded([&]() -> ewf_status {
+        VocabLaunch n;
+        ewf_status st = distill_layout(a, true, n);
+        if (st != EWF_OK || n.r.rows == 0) return st;
+        return launched("distillation, backward", [&] { launch_distill_grad(n, (hipStream_t)hip_stream); });
+    });
+}
 
 ewf_status ewf_layer_norm(const ewf_layer_norm_args *a, void *hip_stream)
 {

@@ -58,6 +58,31 @@ struct RecLaunch {
     void *workspace;
 };
 
+constexpr int kMaxTop = 128;             // alternatives, or a teacher's entries, of a row
+constexpr int kMaxJoin = 4096;           // alternatives of a row's parts
+constexpr int kHeldVectors = 16384;      // 16-byte vectors that one workgroup's registers hold
+
+struct VocabLaunch {
+    Rows r;
+    int dtype, teacher_dtype;
+    float scale, c, lag;                 // c = scale log2 e; lag: how far a sum's point may be behind the largest logit
+    float teacher_scale;
+    int top, entries, with_tail;
+    const void *logits, *teacher_values;
+    const int32_t *tokens, *teacher_indices;
+    const float *dlogprob, *dentropy, *dloss;
+    float *logprob, *peak, *logsum, *entropy, *top_values, *loss, *tail;
+    int32_t *top_indices;
+    void *dlogits;
+    RowStride slogits, steacher_values, stokens, steacher_indices, sdlogprob, sdentropy, sdloss, slogprob, speak, slogsum, sentropy, stop_values,
+        sloss, stail, stop_indices, sdlogits;
+    // the plan
+    uint32_t row0;                       // first row of a launch
+    int threads, splits, held;           // a row's workgroup, its workgroups; whether its logits are held in registers
+    float *parts;                        // [rows][splits][4]: peak, sums
+    unsigned long long *part_keys;       // [rows][splits][top]
+};
+
 // ---- kernels' launchers (device translation units).  They launch on `stream` and report nothing: the caller asks the runtime.
 void launch_layer_norm(const NormLaunch &a, int units, ihipStream_t *stream);
 // Chooses the backward pass's workgroups: fills blocks and padded.
@@ -66,6 +91,12 @@ void launch_layer_norm_grad(const NormLaunch &a, ihipStream_t *stream);
 void launch_activation(const ActLaunch &a, ihipStream_t *stream);
 void launch_activation_grad(const ActLaunch &a, ihipStream_t *stream);
 void launch_read8(const ActLaunch &a, ihipStream_t *stream);
+// Chooses the workgroups of launch_token_logprobs and launch_distill: fills threads, splits and held.
+void plan_vocab(VocabLaunch &a, int units);
+void launch_token_logprobs(const VocabLaunch &a, ihipStream_t *stream);
+void launch_token_logprobs_grad(const VocabLaunch &a, ihipStream_t *stream);
+void launch_distill(const VocabLaunch &a, ihipStream_t *stream);
+void launch_distill_grad(const VocabLaunch &a, ihipStream_t *stream);
 size_t recurrence_workspace(const RecLaunch &a, bool backward, int units);
 void launch_recurrence(const RecLaunch &a, bool backward, int units, ihipStream_t *stream);
 

@@ -88,6 +88,15 @@ ewf_recurrence_args = _args(
     "ewf_recurrence_args", ("u", "v", "w", "h", "h0", "last", "lengths", "dh", "dlast", "du", "dv", "dw", "dh0"),
     [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)])
 
+ewf_token_logprobs_args = _args(
+    "ewf_token_logprobs_args", ("logits", "tokens", "logprob", "peak", "logsum", "entropy", "top_values", "top_indices", "dlogprob", "dentropy",
+                                "dlogits"),
+    [("dtype", ctypes.c_int32), ("ndim", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)])
+ewf_distill_args = _args(
+    "ewf_distill_args", ("logits", "teacher_values", "teacher_indices", "loss", "peak", "logsum", "tail", "dloss", "dlogits"),
+    [("dtype", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32), ("ndim", ctypes.c_int32), ("scale", ctypes.c_float),
+     ("teacher_scale", ctypes.c_float), ("reserved", ctypes.c_int32)])
+
 
 class ewf_plan_info(ctypes.Structure):
     _fields_ = [("kernel_class", ctypes.c_int32), ("rank", ctypes.c_int32),
@@ -144,6 +153,12 @@ _sigs = {
     "ewf_recurrence": (_i32, [ctypes.POINTER(ewf_recurrence_args), _vp, ctypes.c_size_t, _vp]),
     "ewf_recurrence_grad_workspace": (_i32, [ctypes.POINTER(ewf_recurrence_args), ctypes.POINTER(ctypes.c_size_t)]),
     "ewf_recurrence_grad": (_i32, [ctypes.POINTER(ewf_recurrence_args), _vp, ctypes.c_size_t, _vp]),
+    "ewf_token_logprobs_workspace": (_i32, [ctypes.POINTER(ewf_token_logprobs_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "ewf_token_logprobs": (_i32, [ctypes.POINTER(ewf_token_logprobs_args), _vp, ctypes.c_size_t, _vp]),
+    "ewf_token_logprobs_grad": (_i32, [ctypes.POINTER(ewf_token_logprobs_args), _vp]),
+    "ewf_distill_workspace": (_i32, [ctypes.POINTER(ewf_distill_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "ewf_distill": (_i32, [ctypes.POINTER(ewf_distill_args), _vp, ctypes.c_size_t, _vp]),
+    "ewf_distill_grad": (_i32, [ctypes.POINTER(ewf_distill_args), _vp]),
     "ewf_last_error": (ctypes.c_char_p, []),
     "ewf_debug_graph_count": (_i32, [_vp]),
     "ewf_debug_graph_node": (_i32, [_vp, _i32, ctypes.POINTER(ewf_node_info)]),
@@ -785,6 +800,54 @@ def _recurrence_grad(u, v, h, dh, du, dv, *, w=None, dw=None, h0=None, dh0=None,
     return f
 
 
+def _token_logprobs(logits, tokens=None, logprob=None, *, peak=None, logsum=None, entropy=None, top_values=None, top_indices=None, scale=1.0):
+    f = _Filler(ewf_token_logprobs_args())
+    a, nd = f.args, _rank(logits, "logits")
+    a.ndim, a.dtype, a.scale = nd, _dtype_of(logits, "logits"), scale
+    f.tensor("logits", logits, nd)
+    f.typed("tokens", tokens, nd - 1, I32)
+    for name, t in (("logprob", logprob), ("peak", peak), ("logsum", logsum), ("entropy", entropy)):
+        f.typed(name, t, nd - 1, F32)
+    f.typed("top_values", top_values, nd, F32)
+    f.typed("top_indices", top_indices, nd, I32)
+    return f
+
+
+def _token_logprobs_grad(logits, tokens, dlogprob, dlogits, *, peak, logsum, entropy=None, dentropy=None, scale=1.0):
+    f = _token_logprobs(logits, tokens, None, peak=peak, logsum=logsum, entropy=entropy, scale=scale)
+    nd = f.args.ndim
+    f.typed("dlogprob", dlogprob, nd - 1, F32)
+    f.typed("dentropy", dentropy, nd - 1, F32)
+    f.typed("dlogits", dlogits, nd, f.args.dtype)
+    return f
+
+
+def _distill_common(logits, teacher_values, teacher_indices, peak, logsum, tail, dloss, dlogits, scale, teacher_scale):
+    f = _Filler(ewf_distill_args())
+    a, nd = f.args, _rank(logits, "logits")
+    _rank(teacher_values, "teacher_values")
+    a.ndim, a.dtype, a.teacher_dtype = nd, _dtype_of(logits, "logits"), _dtype_of(teacher_values, "teacher_values")
+    a.scale, a.teacher_scale = scale, teacher_scale
+    f.tensor("logits", logits, nd)
+    f.tensor("teacher_values", teacher_values, nd)
+    f.typed("teacher_indices", teacher_indices, nd, I32)
+    for name, t in (("peak", peak), ("logsum", logsum), ("tail", tail), ("dloss", dloss)):
+        f.typed(name, t, nd - 1, F32)
+    f.typed("dlogits", dlogits, nd, a.dtype)
+    return f
+
+
+def _distill(logits, teacher_values, teacher_indices, loss, *, peak=None, logsum=None, tail=None, dloss=None, dlogits=None, scale=1.0,
+             teacher_scale=1.0):
+    f = _distill_common(logits, teacher_values, teacher_indices, peak, logsum, tail, dloss, dlogits, scale, teacher_scale)
+    f.typed("loss", loss, f.args.ndim - 1, F32)
+    return f
+
+
+def _distill_grad(logits, teacher_values, teacher_indices, dlogits, *, peak, logsum, tail=None, dloss=None, scale=1.0, teacher_scale=1.0):
+    return _distill_common(logits, teacher_values, teacher_indices, peak, logsum, tail, dloss, dlogits, scale, teacher_scale)
+
+
 class BoundOperator:
     """An operator's call with its argument structure prepared once (see ``Operator.bind``).  Keeps the
     tensors alive."""
@@ -861,3 +924,15 @@ workspace=None, stream=0): h_t = f_t h_(t-1) + i_t v_t over axis 1 of [batch, st
 1 - f; h0 and last are the float32 states before the first step and behind the last.""")
 recurrence_grad = Operator("ewf_recurrence_grad", _recurrence_grad, True, """recurrence_grad(u, v, h, dh, du, dv, *, w=None, dw=None,
 h0=None, dh0=None, dlast=None, lengths=None, workspace=None, stream=0): the backward pass of recurrence, which stored h.""")
+token_logprobs = Operator("ewf_token_logprobs", _token_logprobs, True, """token_logprobs(logits, tokens=None, logprob=None, *, peak=None,
+logsum=None, entropy=None, top_values=None, top_indices=None, scale=1.0, workspace=None, stream=0): log probabilities of the given tokens (int32;
+outside the vocabulary: padding) under the rows of logits at temperature 1 / scale, with the rows' statistics, entropies and most likely tokens
+where given (float32; indices int32).""")
+token_logprobs_grad = Operator("ewf_token_logprobs_grad", _token_logprobs_grad, False, """token_logprobs_grad(logits, tokens, dlogprob, dlogits, *,
+peak, logsum, entropy=None, dentropy=None, scale=1.0, stream=0): the gradient of log probabilities and entropies, from what token_logprobs saved.
+dlogits may lie over logits.""")
+distill = Operator("ewf_distill", _distill, True, """distill(logits, teacher_values, teacher_indices, loss, *, peak=None, logsum=None, tail=None,
+dloss=None, dlogits=None, scale=1.0, teacher_scale=1.0, workspace=None, stream=0): the loss against a teacher's top logits, or with tail against its
+top log probabilities and their remainder, and with dlogits the gradient for the weights dloss (absent: 1) in the same call.""")
+distill_grad = Operator("ewf_distill_grad", _distill_grad, False, """distill_grad(logits, teacher_values, teacher_indices, dlogits, *, peak, logsum,
+tail=None, dloss=None, scale=1.0, teacher_scale=1.0, stream=0): the gradient of distill's loss, from what it saved.""")
