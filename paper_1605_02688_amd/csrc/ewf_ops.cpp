@@ -588,10 +588,8 @@ size_t vocab_workspace(VocabLaunch &n, void *workspace)
         return at;
     };
     const size_t rows = n.r.rows, parts = rows * (size_t)n.splits;
-    if (n.splits > 1) {
-        n.parts = (float *)take(parts * 4 * sizeof(float));
-        n.part_keys = (unsigned long long *)take(parts * (size_t)n.top * sizeof(unsigned long long));
-    }
+    if (n.splits > 1 || n.top) n.parts = (float *)take(parts * 4 * sizeof(float));
+    if (n.pieces_per_part) n.pieces = (float *)take(parts * (size_t)n.pieces_per_part * sizeof(float));
     if (n.entries && n.dlogits && !n.held) {
         const RowStride dense{(int64_t)n.r.n1, 1};
         if (!n.peak) { n.peak = (float *)take(rows * sizeof(float)); n.speak = dense; }

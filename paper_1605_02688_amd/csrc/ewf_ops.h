@@ -59,13 +59,12 @@ struct RecLaunch {
 };
 
 constexpr int kMaxTop = 128;             // alternatives, or a teacher's entries, of a row
-constexpr int kMaxJoin = 4096;           // alternatives of a row's parts
 constexpr int kHeldVectors = 16384;      // 16-byte vectors that one workgroup's registers hold
 
 struct VocabLaunch {
     Rows r;
     int dtype, teacher_dtype;
-    float scale, c, lag;                 // c = scale log2 e; lag: how far a sum's point may be behind the largest logit
+    float scale, c, lag;                 // c = scale log2 e; lag = 8 / c: logits that far apart are 2^8 apart
     float teacher_scale;
     int top, entries, with_tail;
     const void *logits, *teacher_values;
@@ -77,10 +76,12 @@ struct VocabLaunch {
     RowStride slogits, steacher_values, stokens, steacher_indices, sdlogprob, sdentropy, sdloss, slogprob, speak, slogsum, sentropy, stop_values,
         sloss, stail, stop_indices, sdlogits;
     // the plan
-    uint32_t row0;                       // first row of a launch
-    int threads, splits, held;           // a row's workgroup, its workgroups; whether its logits are held in registers
-    float *parts;                        // [rows][splits][4]: peak, sums
-    unsigned long long *part_keys;       // [rows][splits][top]
+    uint32_t row0, rows;                 // of a launch
+    int resident;                        // workgroups of launch_token_logprobs and launch_distill, which take rows in turn
+    int threads, splits, held, stream;   // a row's workgroup, its workgroups; whether its logits are held in registers; whether they pass caches by
+    float *parts;                        // [rows][splits][4]: peak, sums; null where rows are finished by the workgroup that sums them
+float *pieces;                       // [rows][splits][pieces_per_part]: the largest logits of a part's pieces
+    int pieces_per_part;
 };
 
 // ---- kernels' launchers (device translation units).  They launch on `stream` and report nothing: the caller asks the runtime.

@@ -1,14 +1,18 @@
 // Operators over rows of logits: log probabilities of given tokens with entropy and the largest alternatives, the loss against a
 // teacher's top logits, and the gradients of both.
 //
-// A row's statistics are kept about a point m that lags behind the largest logit seen: with t = c (x - m) in powers of two (c = scale log2 e) a
-// thread adds e = 2^t and, for the entropy, e t; it moves m only where a logit is 2^8 beyond it, so that the moves are rare and e cannot
-// overflow.  Threads' sums are then moved to the row's largest logit and added in a fixed order.
+// With c = scale log2 e a logit x stands for 2^(c x).  A thread adds e = 2^(c x - m), and for the entropy e (c x - m), about a whole number m that lags
+// behind: it moves only where a logit is 2^8 beyond it, so that moves are rare, exact, and e cannot overflow; c x - m is one multiply-add with one
+// rounding.  Threads' sums are moved to a common m and added in a fixed order, and come out about the row's largest logit.  Where c x itself leaves float32
+// (rows of the type's lowest or largest numbers) a row is swept again about its largest.
 #include <algorithm>
 #include <type_traits>
 
 #include "ewf_ops_device.h"
 
+#ifndef NTBITS
+#define NTBITS 0
+#endif
 namespace ewf {
 
 namespace {
@@ -17,9 +21,8 @@ typedef unsigned long long u64;
 
 constexpr float kLn2 = 0.693147181f;
 constexpr float kInf = __builtin_huge_valf();
-constexpr float kLowest = -3.40282347e38f;
 constexpr float kFloor = -1e4f;          // powers of two below which nothing is left; products with it stay finite
-constexpr int kCandidates = 1024;        // alternatives that a row's last selection ranks
+constexpr int kCandidates = 512;         // logits that a row's last selection ranks
 
 template <typename T> constexpr uint32_t kNothing = 0xff80ff80u;        // a word of minus infinities
 template <> constexpr uint32_t kNothing<F16> = 0xfc00fc00u;
@@ -27,14 +30,15 @@ template <> constexpr uint32_t kNothing<F32> = 0xff800000u;
 
 // A row on the 16-byte grid of `grid` (the address that decides: the results' where there are any): whole vectors from element `head` on,
 // and at most 2 V - 2 elements on its two edges.
+constexpr int kEdges = 16;
 template <typename T>
 struct Span {
-    static constexpr int V = Vec16<T>::V;
+    static constexpr int V = Vec16<T>::V, LINE = 16;
     int cols, head, nvec;
     EWF_OPS_DEV Span(const void *grid, int cols) : cols(cols)
     {
-        const int over = (int)((uintptr_t)grid & 15) / (int)sizeof(typename T::raw);
-        head = over ? V - over : 0;
+        const int over = (int)((uintptr_t)grid & (LINE - 1)) / (int)sizeof(typename T::raw);
+        head = over ? LINE / (int)sizeof(typename T::raw) - over : 0;
         head = head < cols ? head : cols;
         nvec = (cols - head) / V;
     }
@@ -44,74 +48,124 @@ struct Span {
     EWF_OPS_DEV bool inside(int c) const { return c >= head && c < head + nvec * V; }
 };
 
-EWF_OPS_DEV float wave_max(float x)
+// The largest of L lanes, in every one.
+template <int L>
+EWF_OPS_DEV float group_most(float x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    x = fmaxf(x, bits_to_float(lane_move<kSwap1>(float_to_bits(x))));
+    x = fmaxf(x, bits_to_float(lane_move<kSwap2>(float_to_bits(x))));
+    x = fmaxf(x, bits_to_float(lane_move<kHalfMirror>(float_to_bits(x))));
+    x = fmaxf(x, bits_to_float(lane_move<kMirror>(float_to_bits(x))));
+    if constexpr (L >= 32) x = fmaxf(x, __shfl_xor(x, 16));
+    if constexpr (L >= 64) x = fmaxf(x, __shfl_xor(x, 32));
     return x;
 }
+EWF_OPS_DEV float wave_max(float x) { return group_most<64>(x); }
 
-// Sums of a thread, a workgroup or a row.  e's sum s and e t's sum w are about m; peak is the largest logit.
+// A row's place on the (at most two) axes that rows have.
+struct RowAt { uint32_t outer, inner; };
+EWF_OPS_DEV RowAt row_at(const Rows &r, uint32_t row)
+{
+    if (r.rows == r.n1) return {0, row};
+    const uint32_t o = row / r.n1;
+    return {o, row - o * r.n1};
+}
+EWF_OPS_DEV int64_t at(const RowAt &row, const RowStride &s) { return (int64_t)row.outer * s.outer + (int64_t)row.inner * s.inner; }
+
+// Sums of a thread: s of the e, w of e times their exponent, about m, which moves for a logit above `limit`; peak is the largest logit.
 struct Sums {
-    float m = kLowest, s = 0.f, w = 0.f, peak = -kInf;
+    float m = -1e38f, limit = -kInf, s = 0.f, w = 0.f, peak = -kInf;
 };
 
-// Moves upwards (sums of nothing move anywhere).
+// Moves the point from `from` to `to` powers of two, upwards (sums of nothing move anywhere).
 template <bool ENT>
-EWF_OPS_DEV void move_to(Sums &a, float m, float c)
+EWF_OPS_DEV void move(Sums &a, float from, float to)
 {
-    const float d = __builtin_amdgcn_fmed3f((a.m - m) * c, kFloor, 0.f), r = __builtin_amdgcn_exp2f(d);
+    const float d = __builtin_amdgcn_fmed3f(from - to, kFloor, 0.f), r = __builtin_amdgcn_exp2f(d);
     if (ENT) a.w = r * fmaf(a.s, d, a.w);
     a.s *= r;
-    a.m = m;
 }
 
-// Adds n logits whose largest is `top`.
+// Adds n logits whose largest is `top`; lag = 8 / c.
 template <bool ENT, int n>
 EWF_OPS_DEV void add(Sums &a, const float *x, float top, float c, float lag)
 {
     a.peak = fmaxf(a.peak, top);
-    if (__any(top > a.m + lag)) move_to<ENT>(a, fmaxf(a.m, top), c);
+    if (__any(top > a.limit)) {
+        const float to = fmaxf(a.m, rintf(top * c));
+        move<ENT>(a, a.m, to);
+        a.m = to;
+        a.limit = fmaxf(a.limit, top + lag);
+    }
+    float w = 0.f;
 #pragma unroll
     for (int e = 0; e < n; e++) {
-        const float t = (x[e] - a.m) * c, p = __builtin_amdgcn_exp2f(t);
+        const float t = fmaf(x[e], c, -a.m), p = __builtin_amdgcn_exp2f(t);
         a.s += p;
-        if (ENT) a.w = fmaf(p, fmaxf(t, kFloor), a.w);
+        if (ENT) w = fmaf(p, t, w);
     }
+    if (ENT && __any(w != w)) {          // (a minus infinity: 0 times that)
+        w = 0.f;
+#pragma unroll
+        for (int e = 0; e < n; e++) {
+            const float t = fmaf(x[e], c, -a.m);
+            w = fmaf(__builtin_amdgcn_exp2f(t), fmaxf(t, kFloor), w);
+        }
+    }
+    if (ENT) a.w += w;
+}
+
+// (the compiler takes the largest of three only after a canonicalising step for each operand; a NaN loses either way)
+EWF_OPS_DEV float max3(float a, float b, float c)
+{
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
 }
 
 template <int V>
 EWF_OPS_DEV float max_of(const float *x)
 {
-    float m = x[0];
+    float m = max3(x[0], x[1], x[2]);
 #pragma unroll
-    for (int e = 1; e < V; e++) m = fmaxf(m, x[e]);
-    return m;
+    for (int e = 3; e + 1 < V; e += 2) m = max3(m, x[e], x[e + 1]);
+    return V % 2 ? m : max3(m, x[V - 1], x[V - 1]);
 }
 
-// The sums of N threads, in every thread, about the row's largest logit (0 where that is minus infinity).
+// A whole number of powers of two near a largest logit: what sums of a wavefront are brought to.
+EWF_OPS_DEV float point_of(float peak, float c) { return peak == -kInf ? 0.f : rintf(peak * c); }
+// Whether a row whose largest logit this is cannot be summed about such a point.
+EWF_OPS_DEV bool beyond(float peak, float c) { return fabsf(peak) < kInf && !(fabsf(peak * c) < 0x1p100f); }
+
+// The sums of N threads, in every thread, about the row's largest logit.
 template <int N, bool ENT>
 EWF_OPS_DEV Sums workgroup_sums(Sums a, float c, float *lds)        // lds: 3 * 16 words
 {
     constexpr int W = N / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float peak = wave_max(a.peak);
-    if (W > 1) {
-        if (lane == 0) lds[wave] = peak;
-        __syncthreads();
-        peak = wave_max(lane < W ? lds[lane] : -kInf);
-    }
-    move_to<ENT>(a, peak == -kInf ? 0.f : peak, c);
+    a.peak = wave_max(a.peak);
+    float m = point_of(a.peak, c);
+    move<ENT>(a, a.m, m);
     a.s = group_sum<64>(a.s);
     if (ENT) a.w = group_sum<64>(a.w);
     if (W > 1) {
-        if (lane == 0) { lds[16 + wave] = a.s; if (ENT) lds[32 + wave] = a.w; }
+        if (lane == 0) { lds[wave] = a.peak; lds[16 + wave] = a.s; if (ENT) lds[32 + wave] = a.w; }
         __syncthreads();
-        a.s = group_sum<16>(lane < W ? lds[16 + lane] : 0.f);
-        a.s = __shfl(a.s, 0);
-        if (ENT) { a.w = group_sum<16>(lane < W ? lds[32 + lane] : 0.f); a.w = __shfl(a.w, 0); }
+        const int from = lane & 15;
+        const float part = from < W ? lds[from] : -kInf;
+        a.s = from < W ? lds[16 + from] : 0.f;
+        if (ENT) a.w = from < W ? lds[32 + from] : 0.f;
+        a.peak = group_most<16>(part);
+        m = point_of(a.peak, c);
+        move<ENT>(a, point_of(part, c), m);
+        a.s = group_sum<16>(a.s);
+        if (ENT) a.w = group_sum<16>(a.w);
     }
-    a.peak = peak;
+    if (a.peak != -kInf) {
+        const float d = fmaf(-a.peak, c, m), r = __builtin_amdgcn_exp2f(d);       // (at most half a power of two)
+        if (ENT) a.w = r * fmaf(a.s, d, a.w);
+        a.s *= r;
+    }
     return a;
 }
 
@@ -127,223 +181,326 @@ EWF_OPS_DEV uint32_t ordered(float x)
 EWF_OPS_DEV float unordered(uint32_t k) { return bits_to_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 EWF_OPS_DEV u64 key_of(float x, uint32_t at) { return x > -kInf ? (u64)ordered(x) << 32 | (uint32_t)~at : 0; }
 
-// The bound that exactly k of n keys (different ones; n at most 64 R) reach, or 1 where there are no more than k.  One wavefront.
-// Bits from the top, values first, until the count is met: one look at all keys each.
-template <int R>
-EWF_OPS_DEV u64 kth_largest(const u64 *keys, int n, int k)
-{
-    const int lane = threadIdx.x & 63;
-    uint32_t hi[R], lo[R];
-    int some = 0;
-#pragma unroll
-    for (int r = 0; r < R; r++) {
-        const u64 v = r * 64 + lane < n ? keys[r * 64 + lane] : 0;
-        hi[r] = (uint32_t)(v >> 32);
-        lo[r] = (uint32_t)v;
-        some += __popcll(__ballot(hi[r] != 0));
-    }
-    if (some <= k) return 1;
-    uint32_t at = 0;
-    for (int bit = 31; bit >= 0; bit--) {
-        const uint32_t next = at | 1u << bit;
-        int count = 0;
-#pragma unroll
-        for (int r = 0; r < R; r++) count += __popcll(__ballot(hi[r] >= next));
-        if (count >= k) at = next;
-        if (count == k) return (u64)at << 32;
-    }
-    int over = 0;
-#pragma unroll
-    for (int r = 0; r < R; r++) over += __popcll(__ballot(hi[r] > at));
-    uint32_t low = 0;
-    for (int bit = 31; bit >= 0; bit--) {
-        const uint32_t next = low | 1u << bit;
-        int count = over;
-#pragma unroll
-        for (int r = 0; r < R; r++) count += __popcll(__ballot(hi[r] == at && lo[r] >= next));
-        if (count >= k) low = next;
-        if (count == k) break;
-    }
-    return (u64)at << 32 | low;
-}
-
-struct Best {
-    float value = -kInf;
-    int vec = 0;
-};
+// The largest logits of pieces of a row: a piece is what kPieceLanes lanes (a cache line) take in kPieceTrips trips.
+constexpr int kPieceLanes = 8, kPieceTrips = 4;
+constexpr int kBins = 1024, kBinShift = 16, kChosen = 320;
 
 template <int N>
 struct TopLds {
-    u64 keys[N], found[kCandidates], bound;
-    int chosen[N], nchosen, nfound, count[2];
+    uint32_t bins[kBins];
+    alignas(16) u64 found[kCandidates];
+    int chosen[N > 64 ? kChosen : 1], hits[N > 64 ? kCandidates : 1], nchosen, nhits, nfound;
+    int bin, upto, before, total;
 };
 
-// Writes the k largest logits of the vectors j0 .. j1 - 1 of a row and of its edges (where `edges`) to found[], as keys in descending order,
-// and 0 behind the last.  best: of each thread, the largest logit of its vectors j0 + thread, + N ... and the first vector that has it.
-//
-// The k largest lie in the k threads whose best are largest: each other thread's elements have k larger ones before them.  Those
-// threads' vectors are read a second time, by all threads, and what reaches the k-th best is collected.
-template <typename T, int N>
-EWF_OPS_DEV void largest(TopLds<N> &l, const typename T::raw *row, const Span<T> &s, int j0, int j1, bool edges, float edge, const Best &best, int k)
+// Where a bin is kept: a lane's 16 are 64 apart.
+EWF_OPS_DEV int bin_at(uint32_t bin) { return (int)((bin & 15) << 6 | bin >> 4); }
+
+// Of bins that count numbers from the largest down: the first bin with which there are k of them, how many there are up to its end and before
+// it; all of them.  One wavefront.
+template <int N>
+EWF_OPS_DEV void find_bin(TopLds<N> &l, int k)
 {
-    constexpr int V = Vec16<T>::V, U = 4;
-    const int tid = threadIdx.x;
-    const u64 mine = key_of(best.value, best.vec);
-    l.keys[tid] = mine;
-    if (tid == 0) l.nchosen = l.nfound = 0;
-    __syncthreads();
-    if (tid < 64) {
-        const u64 b = kth_largest<N / 64>(l.keys, N, k);
-        if (tid == 0) l.bound = b;
+    const int lane = threadIdx.x & 63;
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) sum += l.bins[i * 64 + lane];
+    auto up_to = [&](int v, int lanes) {
+#pragma unroll
+        for (int d = 1; d < lanes; d *= 2) {
+            const int u = __shfl_up(v, d);
+            v += (lane & (lanes - 1)) >= d ? u : 0;
+        }
+        return v;
+    };
+    const int upto = up_to(sum, 64);                     // of this lane's bins and those before
+    const u64 reach = __ballot(upto >= k);
+    const int at = reach ? __builtin_ctzll(reach) : 63, had = __shfl(upto - sum, at), all = __shfl(upto, 63);
+    const int mine = l.bins[(lane & 15) * 64 + at], within = had + up_to(mine, 16);
+    const uint32_t ends = (uint32_t)__ballot(within >= k) & 0xffff;
+    const int in = ends ? __builtin_ctz(ends) : 15;
+    if (lane == in) { l.bin = at * 16 + in; l.before = within - mine; l.upto = within; l.total = all; }
+}
+
+// The k-th largest of the lanes' numbers, k up to 64, as ordered() has it, 0 where fewer are above minus infinity: bit by bit.
+EWF_OPS_DEV uint32_t kth_of_lanes(float x, int k)
+{
+    const uint32_t v = x > -kInf ? ordered(x) : 0;
+    uint32_t at = 0;
+    for (int bit = 31; bit >= 0; bit--) {
+        const uint32_t next = at | 1u << bit;
+        if (__popcll(__ballot(v >= next)) >= k) at = next;
     }
-    __syncthreads();
-    const u64 bound = l.bound;
-    // the same bound for elements: the last of the vector that it names
-    u64 least = bound;
-    if ((uint32_t)bound > 1) {
-        const u64 last = (u64)(uint32_t)~(uint32_t)bound * V + V - 1 + s.head;
-        least = (bound & 0xffffffff00000000ull) | (uint32_t)~(uint32_t)(last < 0xffffffffu ? last : 0xffffffffu);
-    }
+    return at;
+}
+
+// Collects the k largest logits of a row, and perhaps some that are smaller, in found[]: returns how many.  peak: the largest, a number.  pieces: the
+// largest of each of the row's pieces, per_part in each part of `per` vectors, of which a thread has the first ones in `mine` (minus infinity
+// behind the last); or null.
+//
+// Logits are counted by their distance below the peak in steps of 2^kBinShift of their order (1/128 of a power of two): the bins that have k of
+// them give a bound, and what reaches it is collected and ranked.  With pieces, those are counted in the logits' place: k pieces whose largest reach a
+// bound hold k logits that do, and no others can.  A single wavefront takes its lanes' largest for that.
+constexpr int kOwnPieces = 4;
+template <typename T, int N>
+EWF_OPS_DEV int largest(TopLds<N> &l, const typename T::raw *row, const Span<T> &s, const float *pieces, const float *mine, float edge, int parts, int per_part,
+                        int per, float peak, int k)
+{
+    constexpr int V = Vec16<T>::V, W = N / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t top = ordered(peak);
+    const typename T::raw *first = row + s.head;
+    auto clear_bins = [&] {
+        for (int i = tid; i < kBins; i += N) l.bins[i] = 0;
+        if (tid == 0) l.nchosen = l.nhits = l.nfound = 0;
+        __syncthreads();
+    };
+    auto count_in = [&](uint32_t bin) { atomicAdd(&l.bins[bin_at(bin < kBins - 1 ? bin : kBins - 1)], 1u); };
+    auto find = [&] {
+        __syncthreads();
+        if (tid < 64) find_bin(l, k);
+        __syncthreads();
+    };
+    // the number that a bin's end stands for, 0 where it has none
+    auto end_of = [&](uint32_t bin) { return bin == kBins - 1 || bin + 1 > top >> kBinShift ? 0u : top - ((bin + 1) << kBinShift) + 1; };
+    uint32_t bound = 0;
     auto collect = [&](float x, int at) {
         const u64 key = key_of(x, at);
-        if (key >= least && key) {
+        if (key && (uint32_t)(key >> 32) >= bound) {
             const int i = atomicAdd(&l.nfound, 1);
             if (i < kCandidates) l.found[i] = key;
         }
     };
-    if (mine >= bound && mine) l.chosen[atomicAdd(&l.nchosen, 1)] = tid;
-    if (edges && tid < s.edges()) collect(edge, s.edge(tid));
-    __syncthreads();
-    const int nchosen = l.nchosen, trips = (j1 - j0 + N - 1) / N, items = nchosen * trips;
+    // all logits of the row (what follows them is no hurry's: one access at a time)
     auto sweep = [&](auto &&each) {
-        for (int i0 = tid; i0 < items; i0 += U * N) {
-            u32x4 v[U];
-            int j[U];
+        for (int j = tid; j < s.nvec; j += N) {
+            const u32x4 v = load16<T>(first + (int64_t)j * V);
 #pragma unroll
-            for (int u = 0; u < U; u++) {
-                const int i = i0 + u * N;
-                j[u] = i < items ? j0 + (i / nchosen) * N + l.chosen[i % nchosen] : j1;
+            for (int e = 0; e < V; e++) each(element<T>(v, e), s.head + j * V + e);
+        }
+        if (tid < s.edges()) each(edge, s.edge(tid));
+    };
+    auto floor_of = [&](uint32_t bound) { return bound > ordered(-kInf) ? unordered(bound) : -kInf; };      // (below minus infinity lie NaN)
+    bool collected = false;
+    if constexpr (N == 64) {
+        if (s.nvec <= 256 && k <= 64) {
+            u32x4 v[4];
+            float most = edge;
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
                 v[u] = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
-                if (j[u] < j1) v[u] = load16<T>(row + s.head + (int64_t)j[u] * V);
+                if (tid + u * N < s.nvec) v[u] = load16<T>(first + (int64_t)(tid + u * N) * V);
             }
 #pragma unroll
-            for (int u = 0; u < U; u++)
+            for (int u = 0; u < 4; u++)
 #pragma unroll
-                for (int e = 0; e < V; e++) each(element<T>(v[u], e), s.head + j[u] * V + e);
+                for (int e = 0; e < V; e++) most = fmaxf(most, element<T>(v[u], e));
+            bound = kth_of_lanes(most, k);
+            if (bound) {
+                const float floor = unordered(bound);
+                if (tid == 0) l.nfound = 0;
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < 4; u++)
+#pragma unroll
+                    for (int e = 0; e < V; e++)
+                        if (element<T>(v[u], e) >= floor) collect(element<T>(v[u], e), s.head + (tid + u * N) * V + e);
+                if (tid < s.edges()) collect(edge, s.edge(tid));
+                __syncthreads();
+                collected = l.nfound <= kCandidates;
+                __syncthreads();
+            }
         }
-    };
-    sweep(collect);
-    __syncthreads();
-    int n = l.nfound;
-    if (n > kCandidates) {
-        // (more than fit, as where logits repeat with the threads' period: the k-th key bit by bit, a sweep for each)
-        u64 at = 0;
-        for (int bit = 63; bit >= 0; bit--) {
-            const u64 next = at | 1ull << bit;
-            int count = 0;
-            auto ask = [&](float x, int p) { const u64 key = key_of(x, p); count += key >= next && key ? 1 : 0; };
-            sweep(ask);
-            if (edges && tid < s.edges()) ask(edge, s.edge(tid));
-            if (tid == 0) l.count[bit & 1] = 0;
+    } else if (pieces) {
+        const int n = parts * per_part;
+        auto each_piece = [&](auto &&each) {
+#pragma unroll
+            for (int i = 0; i < kOwnPieces; i++) each(mine[i], i * N + tid);
+            for (int i = kOwnPieces * N + tid; i < n; i += N) each(pieces[i], i);
+        };
+        clear_bins();
+        each_piece([&](float x, int) { if (x > -kInf) count_in((top - ordered(x)) >> kBinShift); });
+        find();
+        if (l.total >= k && l.upto <= kChosen && end_of(l.bin)) {
+            bound = end_of(l.bin);
+            const float floor = floor_of(bound);
+            each_piece([&](float x, int i) { if (x >= floor) l.chosen[atomicAdd(&l.nchosen, 1)] = i; });
+            if (tid < s.edges()) collect(edge, s.edge(tid));
             __syncthreads();
-            if (count) atomicAdd(&l.count[bit & 1], count);
+            // half a wavefront takes a piece
+            constexpr int U = 4;
+            static_assert(kPieceLanes * kPieceTrips == 32, "");
+            const int half = lane >> 5, trip = (lane >> 3) & 3, in_line = lane & 7, nchosen = l.nchosen;
+            for (int c0 = 2 * wave + half; c0 - half < nchosen; c0 += 2 * U * W) {
+                u32x4 v[U];
+                int j[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int c = c0 + u * 2 * W, i = l.chosen[c < nchosen ? c : 0];
+                    const int part = parts == 1 ? 0 : i / per_part, q = i - part * per_part, end = (part + 1) * per < s.nvec ? (part + 1) * per : s.nvec;
+                    j[u] = part * per + (q / 32 * kPieceTrips + trip) * 256 + q % 32 * kPieceLanes + in_line;
+                    if (c >= nchosen || j[u] >= end) j[u] = -1;
+                    v[u] = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
+                    if (j[u] >= 0) v[u] = load16<T>(first + (int64_t)j[u] * V);
+                }
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    float x[V];
+#pragma unroll
+                    for (int e = 0; e < V; e++) x[e] = element<T>(v[u], e);
+                    if (j[u] >= 0 && max_of<V>(x) >= floor) {
+                        const int h = atomicAdd(&l.nhits, 1);
+                        if (h < kCandidates) l.hits[h] = j[u];
+                    }
+                }
+            }
             __syncthreads();
-            if (l.count[bit & 1] >= k) at = next;
+            const int hits = l.nhits;
+            if (hits <= kCandidates)
+                for (int i = tid; i < hits * V; i += N) {
+                    const int c = s.head + l.hits[i / V] * V + i % V;
+                    collect(load1<T>(row + c), c);
+                }
+            __syncthreads();
+            collected = hits <= kCandidates && l.nfound <= kCandidates;
+            __syncthreads();
         }
-        if (tid == 0) l.nfound = 0;
-        least = at;
-        __syncthreads();
-        if (edges && tid < s.edges()) collect(edge, s.edge(tid));
-        sweep(collect);
-        __syncthreads();
-        n = l.nfound;
     }
-    if (n > 2 * k + 64) {
-        // ranking takes n looks a key: fewer keys first
-        if (tid < 64) {
-            const u64 b = kth_largest<kCandidates / 64>(l.found, n, k);
-            if (tid == 0) { l.bound = b; l.nchosen = 0; }
+    if (!collected) {
+        clear_bins();
+        sweep([&](float x, int) { if (x > -kInf) count_in((top - ordered(x)) >> kBinShift); });
+        find();
+        const bool all = l.total <= k;
+        bound = all ? 0 : end_of(l.bin);
+        if (all || (bound && l.upto <= kCandidates)) {
+            sweep(collect);
+            __syncthreads();
+        } else {
+            // many equal or nearly equal ones, or a few far above all others: the k-th value digit by digit
+            uint32_t value = 0;
+            int need = k;
+            for (int shift : {22, 12, 2, 0}) {
+                const int bits = shift ? 10 : 2;
+                clear_bins();
+                sweep([&](float x, int) {
+                    const uint32_t d = top - ordered(x);
+                    if (x > -kInf && (shift == 22 || d >> (shift + bits) == value)) atomicAdd(&l.bins[bin_at(d >> shift & ((1u << bits) - 1))], 1u);
+                });
+                __syncthreads();
+                if (tid < 64) find_bin(l, need);
+                __syncthreads();
+                value = value << bits | (uint32_t)l.bin;
+                need -= l.before;
+                __syncthreads();
+            }
+            // what is larger, and the first `need` that are equal
+            const uint32_t kth = top - value;
+            bound = kth + 1;
+            clear_bins();
+            sweep(collect);
+            __syncthreads();
+            int *counts = (int *)l.bins;                 // of a window's threads
+            int had = 0;
+            for (int c0 = 0; c0 < s.cols && had < need; c0 += N * V) {
+                int c = c0 + tid * V, mine = 0;
+                bool equal[V];
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const float x = c + e < s.cols ? load1<T>(row + c + e) : -kInf;
+                    equal[e] = x > -kInf && ordered(x) == kth;
+                    mine += equal[e] ? 1 : 0;
+                }
+                int upto = mine;
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const int v = __shfl_up(upto, d);
+                    upto += lane >= d ? v : 0;
+                }
+                if (lane == 63) counts[wave] = upto;
+                __syncthreads();
+                int place = had + upto - mine;
+                for (int w = 0; w < W; w++) {
+                    if (w < wave) place += counts[w];
+                    had += counts[w];
+                }
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    if (equal[e]) {
+                        if (place < need) l.found[atomicAdd(&l.nfound, 1)] = (u64)kth << 32 | (uint32_t)~(c + e);
+                        place++;
+                    }
+                __syncthreads();
+            }
         }
-        __syncthreads();
-        u64 keep[kCandidates / N > 0 ? kCandidates / N : 1];
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(keep) / sizeof(u64)); i++) keep[i] = i * N + tid < n ? l.found[i * N + tid] : 0;
-        const u64 b = l.bound;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(keep) / sizeof(u64)); i++)
-            if (keep[i] >= b && keep[i]) l.found[atomicAdd(&l.nchosen, 1)] = keep[i];
-        __syncthreads();
-        n = l.nchosen;
     }
-    // each key's place is the number of larger ones
-    constexpr int M = (2 * 128 + 64 + N - 1) / N;
-    u64 key[M];
-    int place[M];
-#pragma unroll
-    for (int i = 0; i < M; i++) { key[i] = i * N + tid < n ? l.found[i * N + tid] : 0; place[i] = 0; }
-    for (int q = 0; q < n; q++) {
-        const u64 other = l.found[q];
-#pragma unroll
-        for (int i = 0; i < M; i++) place[i] += other > key[i] ? 1 : 0;
-    }
+    const int n = l.nfound;
+    for (int i = n + tid; i < (n + 7) / 8 * 8; i += N) l.found[i] = 0;
     __syncthreads();
+    return n;
+}
+
+// A key's place among n: the number of larger ones.
+EWF_OPS_DEV int place_of(const u64 *found, int n, u64 key)
+{
+    int place = 0;
+    for (int q = 0; q < n; q += 8)
 #pragma unroll
-    for (int i = 0; i < M; i++)
-        if (key[i] && place[i] < k) l.found[place[i]] = key[i];
-    for (int i = n + tid; i < k; i += N) l.found[i] = 0;
-    __syncthreads();
+        for (int e = 0; e < 8; e++) place += found[q + e] > key ? 1 : 0;
+    return place;
 }
 
 // ------------------------------------------------------------------ a row's results
 
-// Writes what a row's sums give.  w is that of e t about the peak.
+// Writes what a row's sums give, and its alternatives from nfound keys among which they are.
 template <int N>
-EWF_OPS_DEV void finish_logprobs(const VocabLaunch &a, uint32_t row, const Sums &sum, float token_logit, const u64 *found)
+EWF_OPS_DEV void finish_logprobs(const VocabLaunch &a, const RowAt &row, const Sums &sum, float token_logit, const u64 *found, int nfound)
 {
     const bool none = sum.peak == -kInf && sum.s == 0.f;
     const float logsum = none ? -kInf : logf(sum.s);
     const bool nan = !none && !(sum.s < kInf);           // a NaN or an infinity among the logits
     const float bad = __builtin_nanf("");
     if (threadIdx.x == 0) {
-        if (a.logprob) a.logprob[row_offset(a.r, row, a.slogprob)] = nan ? bad : none ? -kInf : fmaf(token_logit - sum.peak, a.scale, -logsum);
-        if (a.peak) a.peak[row_offset(a.r, row, a.speak)] = nan ? bad : sum.peak;
-        if (a.logsum) a.logsum[row_offset(a.r, row, a.slogsum)] = nan ? bad : logsum;
-        if (a.entropy) a.entropy[row_offset(a.r, row, a.sentropy)] = nan ? bad : none ? 0.f : logsum - kLn2 * (sum.w / sum.s);
+        if (a.logprob) a.logprob[at(row, a.slogprob)] = nan ? bad : none ? -kInf : fmaf(token_logit - sum.peak, a.scale, -logsum);
+        if (a.peak) a.peak[at(row, a.speak)] = nan ? bad : sum.peak;
+        if (a.logsum) a.logsum[at(row, a.slogsum)] = nan ? bad : logsum;
+        if (a.entropy) a.entropy[at(row, a.sentropy)] = nan ? bad : none ? 0.f : logsum - kLn2 * (sum.w / sum.s);
     }
     if (a.top) {
-        float *value = a.top_values + row_offset(a.r, row, a.stop_values);
-        int32_t *index = a.top_indices + row_offset(a.r, row, a.stop_indices);
-        for (int i = threadIdx.x; i < a.top; i += N) {
+        float *value = a.top_values + at(row, a.stop_values);
+        int32_t *index = a.top_indices + at(row, a.stop_indices);
+        for (int i = threadIdx.x; i < nfound; i += N) {
             const u64 key = found[i];
-            value[i] = nan ? bad : key ? fmaf(unordered((uint32_t)(key >> 32)) - sum.peak, a.scale, -logsum) : -kInf;
-            index[i] = nan || !key ? -1 : (int32_t)~(uint32_t)key;
+            const int place = place_of(found, nfound, key);
+            if (place >= a.top) continue;
+            value[place] = fmaf(unordered((uint32_t)(key >> 32)) - sum.peak, a.scale, -logsum);
+            index[place] = (int32_t)~(uint32_t)key;
         }
+        for (int i = nfound + threadIdx.x; i < a.top; i += N) { value[i] = nan ? bad : -kInf; index[i] = -1; }
     }
 }
 
 // A row without a token: zeros, and no alternatives.
 template <int N>
-EWF_OPS_DEV void padding_logprobs(const VocabLaunch &a, uint32_t row)
+EWF_OPS_DEV void padding_logprobs(const VocabLaunch &a, const RowAt &row)
 {
     if (threadIdx.x == 0) {
-        if (a.logprob) a.logprob[row_offset(a.r, row, a.slogprob)] = 0.f;
-        if (a.peak) a.peak[row_offset(a.r, row, a.speak)] = 0.f;
-        if (a.logsum) a.logsum[row_offset(a.r, row, a.slogsum)] = 0.f;
-        if (a.entropy) a.entropy[row_offset(a.r, row, a.sentropy)] = 0.f;
+        if (a.logprob) a.logprob[at(row, a.slogprob)] = 0.f;
+        if (a.peak) a.peak[at(row, a.speak)] = 0.f;
+        if (a.logsum) a.logsum[at(row, a.slogsum)] = 0.f;
+        if (a.entropy) a.entropy[at(row, a.sentropy)] = 0.f;
     }
     if (a.top) {
-        float *value = a.top_values + row_offset(a.r, row, a.stop_values);
-        int32_t *index = a.top_indices + row_offset(a.r, row, a.stop_indices);
+        float *value = a.top_values + at(row, a.stop_values);
+        int32_t *index = a.top_indices + at(row, a.stop_indices);
         for (int i = threadIdx.x; i < a.top; i += N) { value[i] = -kInf; index[i] = -1; }
     }
 }
 
-EWF_OPS_DEV bool is_padding(const VocabLaunch &a, uint32_t row, int &token)
+EWF_OPS_DEV bool is_padding(const VocabLaunch &a, const RowAt &row, int &token)
 {
     token = -1;
     if (!a.tokens) return false;
-    token = a.tokens[row_offset(a.r, row, a.stokens)];
+    token = a.tokens[at(row, a.stokens)];
     return (uint32_t)token >= (uint32_t)a.r.cols;
 }
 
@@ -356,7 +513,7 @@ struct Entries {
     int head[N];                                        // last entry of each thread's list, -1
     int next[kMaxTop], index[kMaxTop], trip[kMaxTop], owner[kMaxTop];
     float q[kMaxTop], logq[kMaxTop], logit[kMaxTop], grad[kMaxTop];
-    int edge[16];                                       // an entry on each edge element, -1
+    int edge[kEdges];                                   // an entry on each edge element, -1
     float tail_q, total_q;                              // 1 - sum q; sum q
     int live;                                           // entries that exist
     float gradient[4];                                  // of the logits that no entry names (see Slope)
@@ -366,7 +523,7 @@ template <int N>
 EWF_OPS_DEV void clear(Entries<N> &l)
 {
     l.head[threadIdx.x] = -1;
-    if (threadIdx.x < 16) l.edge[threadIdx.x] = -1;
+    if (threadIdx.x < kEdges) l.edge[threadIdx.x] = -1;
 }
 
 EWF_OPS_DEV float load_teacher(const VocabLaunch &a, int64_t at)
@@ -379,11 +536,11 @@ EWF_OPS_DEV float load_teacher(const VocabLaunch &a, int64_t at)
 // Reads and ranks a row's entries: one wavefront, two entries a lane, after clear() and a barrier.  The vectors of this workgroup are j0 .. j1 - 1 (thread
 // (j - j0) mod N takes vector j); `edges`: and the edges.
 template <typename T, int N>
-EWF_OPS_DEV void read_entries(Entries<N> &l, const VocabLaunch &a, uint32_t row, const typename T::raw *logits, const Span<T> &s, int j0, int j1, bool edges)
+EWF_OPS_DEV void read_entries(Entries<N> &l, const VocabLaunch &a, const RowAt &row, const typename T::raw *logits, const Span<T> &s, int j0, int j1, bool edges)
 {
     constexpr int V = Vec16<T>::V;
     const int lane = threadIdx.x;
-    const int64_t values = row_offset(a.r, row, a.steacher_values), indices = row_offset(a.r, row, a.steacher_indices);
+    const int64_t values = at(row, a.steacher_values), indices = at(row, a.steacher_indices);
     int c[2];
     float v[2], x[2];
     bool live[2];
@@ -430,8 +587,9 @@ EWF_OPS_DEV void read_entries(Entries<N> &l, const VocabLaunch &a, uint32_t row,
         l.trip[i] = -1;
         int owner;
         if (j < 0) {
-            owner = s.edge_of(c[h]) & 15;
-            if (edges) l.edge[owner] = i;               // (of several that are the same one, any: they have the same gradient)
+            const int e = s.edge_of(c[h]);
+            owner = (uint32_t)e % N;
+            if (edges) l.edge[e] = i;                   // (of several that are the same one, any: they have the same gradient)
         } else {
             owner = (uint32_t)j % N;
             if (j >= j0 && j < j1) { owner = (j - j0) % N; l.trip[i] = (j - j0) / N; }
@@ -486,7 +644,7 @@ EWF_OPS_DEV Slope slope_of(const VocabLaunch &a, float peak, float logsum, float
 // Behind the row's sums (of all logits, or with a tail of those that no entry names) and a barrier: one wavefront writes the loss and the
 // statistics, and with `slope` what the gradients need.
 template <int N>
-EWF_OPS_DEV void finish_distill(const VocabLaunch &a, Entries<N> &l, uint32_t row, Sums sum, bool slope, Slope &g)
+EWF_OPS_DEV void finish_distill(const VocabLaunch &a, Entries<N> &l, const RowAt &row, Sums sum, bool slope, Slope &g)
 {
     const int lane = threadIdx.x & 63;
     bool first[2];
@@ -507,8 +665,7 @@ EWF_OPS_DEV void finish_distill(const VocabLaunch &a, Entries<N> &l, uint32_t ro
         for (int h = 0; h < 2; h++) e += first[h] ? __builtin_amdgcn_exp2f((x[h] - ref) * a.c) : 0.f;
         e = group_sum<64>(e);
         if (sum.s != 0.f) tail = fmaf(sum.peak - ref, a.scale, logf(sum.s));
-        move_to<false>(sum, ref, a.c);
-        total = sum.s + e;
+        total = e + (sum.peak == -kInf ? 0.f : sum.s * __builtin_amdgcn_exp2f((sum.peak - ref) * a.c));
     }
     const bool none = total == 0.f;
     const float logsum = none ? -kInf : logf(total);
@@ -524,13 +681,13 @@ EWF_OPS_DEV void finish_distill(const VocabLaunch &a, Entries<N> &l, uint32_t ro
     const float tail_q = l.tail_q, bad = __builtin_nanf("");
     if (a.with_tail && tail_q != 0.f && (tail_counts(tail, logsum) || tail_q != tail_q)) loss += tail_q * (logf(tail_q) - (tail - logsum));
     if (lane == 0) {
-        if (a.loss) a.loss[row_offset(a.r, row, a.sloss)] = nan ? bad : loss;
-        if (a.peak) a.peak[row_offset(a.r, row, a.speak)] = nan ? bad : peak;
-        if (a.logsum) a.logsum[row_offset(a.r, row, a.slogsum)] = nan ? bad : logsum;
-        if (a.tail) a.tail[row_offset(a.r, row, a.stail)] = nan ? bad : tail;
+        if (a.loss) a.loss[at(row, a.sloss)] = nan ? bad : loss;
+        if (a.peak) a.peak[at(row, a.speak)] = nan ? bad : peak;
+        if (a.logsum) a.logsum[at(row, a.slogsum)] = nan ? bad : logsum;
+        if (a.tail) a.tail[at(row, a.stail)] = nan ? bad : tail;
     }
     if (!slope) return;
-    const float weight = a.dloss ? a.dloss[row_offset(a.r, row, a.sdloss)] : 1.f;
+    const float weight = a.dloss ? a.dloss[at(row, a.sdloss)] : 1.f;
     g = slope_of(a, nan ? bad : peak, nan ? bad : logsum, tail, tail_q, l.total_q, weight);
 #pragma unroll
     for (int h = 0; h < 2; h++)
@@ -538,138 +695,242 @@ EWF_OPS_DEV void finish_distill(const VocabLaunch &a, Entries<N> &l, uint32_t ro
     if (lane == 0) { l.gradient[0] = g.ref; l.gradient[1] = g.off; l.gradient[2] = g.coef; }
 }
 
-EWF_OPS_DEV void padding_distill(const VocabLaunch &a, uint32_t row)
+EWF_OPS_DEV void padding_distill(const VocabLaunch &a, const RowAt &row)
 {
     if (threadIdx.x) return;
-    if (a.loss) a.loss[row_offset(a.r, row, a.sloss)] = 0.f;
-    if (a.peak) a.peak[row_offset(a.r, row, a.speak)] = 0.f;
-    if (a.logsum) a.logsum[row_offset(a.r, row, a.slogsum)] = 0.f;
-    if (a.tail) a.tail[row_offset(a.r, row, a.stail)] = 0.f;
+    if (a.loss) a.loss[at(row, a.sloss)] = 0.f;
+    if (a.peak) a.peak[at(row, a.speak)] = 0.f;
+    if (a.logsum) a.logsum[at(row, a.slogsum)] = 0.f;
+    if (a.tail) a.tail[at(row, a.stail)] = 0.f;
 }
 
 // ------------------------------------------------------------------ sums over rows
 
 enum { kLogprobs = 0, kDistill = 1, kDistillTail = 2 };
 
-// One workgroup a row, or one of a.splits that share it and leave their sums and their largest in the workspace.
-template <typename T, int N, bool ENT, bool TOP, int KIND>
+// The sums of a row that cannot be taken about a whole number of powers of two (see beyond): about its largest logit, element by element.
+template <typename T, int N, int KIND, typename L>
+EWF_OPS_DEV void sum_again(const VocabLaunch &a, const typename T::raw *p, const Span<T> &s, int j0, int j1, bool edges, const L &entries, float *lds,
+                                       Sums &sum)
+{
+    constexpr int V = Vec16<T>::V;
+    const int tid = threadIdx.x, end = s.head + j1 * V;
+    float total = 0.f, weighted = 0.f;
+    for (int c = s.head + j0 * V + tid; c < end + (edges ? s.edges() : 0); c += N) {
+        const int at = c < end ? c : s.edge(c - end);
+        float x = load1<T>(p + at);
+        if constexpr (KIND == kDistillTail)
+            for (int k = 0; k < a.entries; k++) x = entries.index[k] == at ? -kInf : x;
+        const float t = fmaxf((x - sum.peak) * a.c, kFloor), e = __builtin_amdgcn_exp2f(t);
+        total += x == x ? e : x;
+        weighted = fmaf(e, t, weighted);
+    }
+    total = group_sum<64>(total);
+    weighted = group_sum<64>(weighted);
+    __syncthreads();
+    if ((tid & 63) == 0) { lds[tid >> 6] = total; lds[16 + (tid >> 6)] = weighted; }
+    __syncthreads();
+    sum.s = group_sum<16>((tid & 15) < N / 64 ? lds[tid & 15] : 0.f);
+    sum.w = group_sum<16>((tid & 15) < N / 64 ? lds[16 + (tid & 15)] : 0.f);
+}
+
+// A workgroup takes rows, or parts of rows (a.splits of each), one after the other, the next one's first vectors in flight while it finishes.  Where rows
+// have parts or alternatives are asked for it leaves sums and, TOP, the largest of their pieces in the workspace.
+template <typename T, int N, bool ENT, bool TOP, int KIND, bool STREAM>
 __global__ void __launch_bounds__(N) k_rows(VocabLaunch a)
 {
     typedef typename T::raw raw;
-    constexpr int V = Vec16<T>::V, U = 4;
+    constexpr int V = Vec16<T>::V, U = kPieceTrips;
     __shared__ float sums[48];
-    __shared__ typename std::conditional<TOP, TopLds<N>, int>::type top;
     __shared__ typename std::conditional<KIND != kLogprobs, Entries<N>, int>::type entries;
     const int tid = threadIdx.x;
-    const uint32_t block = blockIdx.x, splits = (uint32_t)a.splits;
-    const uint32_t row = a.row0 + block / splits, split = block - block / splits * splits;
-    const raw *p = (const raw *)a.logits + row_offset(a.r, row, a.slogits);
-    const Span<T> s(p, a.r.cols);
-    const int per = (s.nvec + (int)splits - 1) / (int)splits;
-    const int j0 = (int)split * per < s.nvec ? (int)split * per : s.nvec, j1 = j0 + per < s.nvec ? j0 + per : s.nvec;
-    const bool edges = split == 0;
-    int token = 0;
-    if constexpr (KIND == kLogprobs) {
-        if (is_padding(a, row, token)) {
-            if (splits == 1) padding_logprobs<N>(a, row);
-            return;
-        }
-    } else if (KIND == kDistillTail || splits == 1) {
-        clear(entries);
-        __syncthreads();
-        if (tid < 64) read_entries<T>(entries, a, row, p, s, j0, j1, edges);
-        __syncthreads();
-        if (entries.live == 0) {
-            if (splits == 1) padding_distill(a, row);
-            return;
-        }
-    }
-    float token_logit = 0.f;
-    if (KIND == kLogprobs && splits == 1 && token >= 0) token_logit = load1<T>(p + token);
-    Sums sum;
-    Best best;
-    float edge = -kInf;
-    if (edges && tid < s.edges()) edge = load1<T>(p + s.edge(tid));
-    if constexpr (KIND == kDistillTail)
-        if (edges && tid < 16 && entries.edge[tid] >= 0) edge = -kInf;
-    int hit = 0x7fffffff;                                // the next of this thread's trips that holds an entry
-    auto next_hit = [&](int from) {
-        hit = 0x7fffffff;
-        if constexpr (KIND == kDistillTail)
-            for (int k = entries.head[tid]; k >= 0; k = entries.next[k])
-                if (entries.trip[k] >= from && entries.trip[k] < hit) hit = entries.trip[k];
+    const bool parts = a.parts != nullptr;
+    const uint32_t splits = (uint32_t)a.splits, items = a.rows * splits;
+
+    struct Item { RowAt row; uint32_t part; const raw *p; int token, j0, j1; bool edges; };
+    auto item_at = [&](uint32_t i) {
+        Item t;
+        const uint32_t row = splits == 1 ? i : i / splits, split = i - row * splits;
+        t.part = i;
+        t.edges = split == 0;
+        t.row = row_at(a.r, a.row0 + row);
+        t.p = (const raw *)a.logits + at(t.row, a.slogits);
+        const Span<T> s(t.p, a.r.cols);
+        const int per = splits == 1 ? s.nvec : (s.nvec + (int)splits - 1) / (int)splits;
+        t.j0 = (int)split * per < s.nvec ? (int)split * per : s.nvec;
+        t.j1 = t.j0 + per < s.nvec ? t.j0 + per : s.nvec;
+        return t;
     };
-    next_hit(0);
-    const raw *first = p + s.head;
-    for (int j = j0 + tid, trip = 0; j - tid < j1; j += U * N, trip += U) {
-        u32x4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            v[u] = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
-            if (j + u * N < j1) v[u] = load16<T>(first + (int64_t)(j + u * N) * V);
-        }
-        float x[U * V];
-#pragma unroll
-        for (int u = 0; u < U; u++)
-#pragma unroll
-            for (int e = 0; e < V; e++) x[u * V + e] = element<T>(v[u], e);
-        if constexpr (KIND == kDistillTail)
-            if (hit < trip + U) {
-                for (int k = entries.head[tid]; k >= 0; k = entries.next[k]) {
-                    const int at = (entries.trip[k] - trip) * V + (entries.index[k] - s.head) % V;
-                    if (entries.trip[k] < trip) continue;
-#pragma unroll
-                    for (int e = 0; e < U * V; e++) x[e] = e == at ? -kInf : x[e];
+    // the first item from i on that is no padding (whose results it writes)
+    auto next_item = [&](uint32_t &i, Item &t) {
+        for (; i < items; i += gridDim.x) {
+            t = item_at(i);
+            if constexpr (KIND == kLogprobs) {
+                if (is_padding(a, t.row, t.token)) {
+                    if (!parts) padding_logprobs<N>(a, t.row);
+                    continue;
                 }
-                next_hit(trip + U);
             }
-        float most[U], over = -kInf;
+            return true;
+        }
+        return false;
+    };
+    // vector j of an item (behind its end: the last one, left out later)
+    auto fetch = [&](const Item &t, const raw *first, int j) {
+        const u32x4 *from = (const u32x4 *)((const char *)first + (uint32_t)(j < t.j1 ? j : t.j1 - 1) * 16u);
+        return STREAM ? __builtin_nontemporal_load(from) : *from;
+    };
+    uint32_t i = blockIdx.x;
+    Item t;
+    u32x4 v[U];
+    bool more = next_item(i, t);
+    auto begin = [&](const Item &t) {
+        const raw *first = t.p + Span<T>(t.p, a.r.cols).head;
+        if (t.j0 < t.j1)
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            most[u] = max_of<V>(x + u * V);
-            if (TOP && most[u] > best.value) { best.value = most[u]; best.vec = j + u * N; }
-            over = fmaxf(over, most[u]);
+            for (int u = 0; u < U; u++) v[u] = fetch(t, first, t.j0 + tid + u * N);
+    };
+    if (more) begin(t);
+    while (more) {
+        const Span<T> s(t.p, a.r.cols);
+        const int j0 = t.j0, j1 = t.j1;
+        const bool edges = t.edges;
+        const RowAt row = t.row;
+        const raw *p = t.p;
+        float edge = -kInf;
+        if (edges && tid < s.edges()) edge = load1<T>(p + s.edge(tid));
+        float token_logit = 0.f;
+        if (KIND == kLogprobs && !parts && t.token >= 0) token_logit = load1<T>(p + t.token);
+        bool live = true;
+        if constexpr (KIND != kLogprobs)
+            if (KIND == kDistillTail || !parts) {
+                clear(entries);
+                __syncthreads();
+                if (tid < 64) read_entries<T>(entries, a, row, p, s, j0, j1, edges);
+                __syncthreads();
+                live = entries.live != 0;
+            }
+        if constexpr (KIND == kDistillTail)
+            if (edges && tid < kEdges && entries.edge[tid] >= 0) edge = -kInf;
+        int hit = 0x7fffffff;                                // the next of this thread's trips that holds an entry
+        auto next_hit = [&](int from) {
+            hit = 0x7fffffff;
+            if constexpr (KIND == kDistillTail)
+                for (int k = entries.head[tid]; k >= 0; k = entries.next[k])
+                    if (entries.trip[k] >= from && entries.trip[k] < hit) hit = entries.trip[k];
+        };
+        next_hit(0);
+        Sums sum;
+        float most_of_piece = -kInf;
+        auto take = [&](const u32x4 &v, int trip) {
+            float x[V];
+#pragma unroll
+            for (int e = 0; e < V; e++) x[e] = element<T>(v, e);
+            if constexpr (KIND == kDistillTail)
+                if (hit == trip) {
+                    for (int k = entries.head[tid]; k >= 0; k = entries.next[k]) {
+                        const int at = entries.trip[k] == trip ? (entries.index[k] - s.head) % V : V;
+#pragma unroll
+                        for (int e = 0; e < V; e++) x[e] = e == at ? -kInf : x[e];
+                    }
+                    next_hit(trip + 1);
+                }
+            const float most = max_of<V>(x);
+            if (TOP) most_of_piece = fmaxf(most_of_piece, most);
+            add<ENT, V>(sum, x, most, a.c, a.lag);
+        };
+        uint32_t ni = i + gridDim.x;
+        Item nt;
+        const bool nmore = next_item(ni, nt);
+        float *pieces = TOP ? a.pieces + (int64_t)t.part * a.pieces_per_part + tid / kPieceLanes : nullptr;
+        int pieces_left = TOP ? a.pieces_per_part : 0;
+        auto end_of_pieces = [&] {
+            if constexpr (TOP) {
+                static_assert(U == kPieceTrips && N == 256, "");
+                float m = most_of_piece;
+                m = fmaxf(m, bits_to_float(lane_move<kSwap1>(float_to_bits(m))));
+                m = fmaxf(m, bits_to_float(lane_move<kSwap2>(float_to_bits(m))));
+                m = fmaxf(m, bits_to_float(lane_move<kHalfMirror>(float_to_bits(m))));
+                if (tid % kPieceLanes == 0) *pieces = m;
+                pieces += N / kPieceLanes;
+                pieces_left -= N / kPieceLanes;
+                most_of_piece = -kInf;
+            }
+        };
+        // each vector's registers take the next block's, or the next item's first, as soon as it is done
+        if (live && j0 < j1) {
+            const raw *first = p + s.head;
+            int j = j0 + tid, trip = 0;
+            for (; j - tid + U * N < j1; j += U * N, trip += U) {
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    take(v[u], trip + u);
+                    v[u] = fetch(t, first, j + (U + u) * N);
+                }
+                end_of_pieces();
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                if (__any(j + u * N < j1)) {
+                    if (j + u * N >= j1) v[u] = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
+                    take(v[u], trip + u);
+                }
+            end_of_pieces();
         }
-        add<ENT, U * V>(sum, x, over, a.c, a.lag);
-    }
-    add<ENT, 1>(sum, &edge, edge, a.c, a.lag);
-    sum = workgroup_sums<N, ENT>(sum, a.c, sums);
-    if constexpr (TOP) largest<T, N>(top, p, s, j0, j1, edges, edge, best, a.top);
-    if (splits > 1) {
-        const int64_t part = (int64_t)(row - a.row0) * splits + split;
-        if (tid == 0) {
-            float *out = a.parts + part * 4;
-            out[0] = sum.peak; out[1] = sum.s; out[2] = sum.w;
-        }
-        if constexpr (TOP)
-            for (int i = tid; i < a.top; i += N) a.part_keys[part * a.top + i] = top.found[i];
-        return;
-    }
-    if constexpr (KIND == kLogprobs) {
-        const u64 *found = nullptr;
-        if constexpr (TOP) found = top.found;
-        finish_logprobs<N>(a, row, sum, token_logit, found);
-    } else if (tid < 64) {
-        Slope g;
-        finish_distill(a, entries, row, sum, false, g);
+        while (pieces_left > 0) end_of_pieces();          // (rows that begin in a vector have fewer, and a row's last part)
+        if (nmore) begin(nt);
+        if (live) {
+            add<ENT, 1>(sum, &edge, edge, a.c, a.lag);
+            sum = workgroup_sums<N, ENT>(sum, a.c, sums);
+            if (beyond(sum.peak, a.c)) sum_again<T, N, KIND>(a, p, s, j0, j1, edges, entries, sums, sum);
+            if (parts) {
+                if (tid == 0) {
+                    float *out = a.parts + (int64_t)t.part * 4;
+                    out[0] = sum.peak; out[1] = sum.s; out[2] = sum.w;
+                }
+            } else if constexpr (KIND == kLogprobs) {
+                finish_logprobs<N>(a, row, sum, token_logit, nullptr, 0);
+            } else if (tid < 64) {
+                Slope g;
+                finish_distill(a, entries, row, sum, false, g);
+            }
+        } else if (!parts) padding_distill(a, row);
+        if (N > 64 || KIND != kLogprobs) __syncthreads();          // (LDS is the next item's)
+        i = ni;
+        t = nt;
+        more = nmore;
     }
 }
 
 // Joins the parts of a row.
 template <typename T, int N, bool TOP, int KIND>
-__global__ void __launch_bounds__(N) k_join(VocabLaunch a)
+__global__ void __launch_bounds__(N, TOP && N > 64 ? 8 : 1) k_join(VocabLaunch a)
 {
     typedef typename T::raw raw;
     __shared__ typename std::conditional<KIND != kLogprobs, Entries<N>, int>::type entries;
-    __shared__ u64 keys[TOP ? kMaxJoin : 1], found[TOP ? kMaxTop : 1];
-    const uint32_t row = a.row0 + blockIdx.x;
-    const raw *p = (const raw *)a.logits + row_offset(a.r, row, a.slogits);
+    __shared__ typename std::conditional<TOP, TopLds<N>, int>::type top;
+    const RowAt row = row_at(a.r, a.row0 + blockIdx.x);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
     const int tid = threadIdx.x, lane = tid & 63, splits = a.splits;
+    const int64_t part = (int64_t)blockIdx.x * splits;
+    const Span<T> s(p, a.r.cols);
+    // (all loads that do not wait for another)
+    const float *pieces = TOP && a.pieces ? a.pieces + part * a.pieces_per_part : nullptr;
+    float mine[kOwnPieces], edge = -kInf;
+    if constexpr (TOP) {
+#pragma unroll
+        for (int i = 0; i < kOwnPieces; i++) mine[i] = pieces && i * N + tid < splits * a.pieces_per_part ? pieces[i * N + tid] : -kInf;
+        if (tid < s.edges()) edge = load1<T>(p + s.edge(tid));
+    }
+    Sums sum;
+    if (lane < splits) {
+        const float *in = a.parts + (part + lane) * 4;
+        sum.peak = in[0]; sum.s = in[1]; sum.w = in[2];
+    }
     int token = 0;
     if constexpr (KIND == kLogprobs) {
         if (is_padding(a, row, token)) { padding_logprobs<N>(a, row); return; }
     } else {
-        const Span<T> s(p, a.r.cols);
         clear(entries);
         __syncthreads();
         if (tid < 64) read_entries<T>(entries, a, row, p, s, 0, 0, false);
@@ -677,41 +938,19 @@ __global__ void __launch_bounds__(N) k_join(VocabLaunch a)
         if (entries.live == 0) { padding_distill(a, row); return; }
     }
     const float token_logit = KIND == kLogprobs && token >= 0 ? load1<T>(p + token) : 0.f;
-    const int64_t part = (int64_t)blockIdx.x * splits;
-    Sums sum;
-    sum.m = 0.f;
-    if (lane < splits) {
-        const float *in = a.parts + (part + lane) * 4;
-        sum.peak = in[0]; sum.s = in[1]; sum.w = in[2];
-        sum.m = sum.peak == -kInf ? 0.f : sum.peak;
-    }
     const float peak = wave_max(sum.peak);
-    move_to<true>(sum, peak == -kInf ? 0.f : peak, a.c);
+    move<true>(sum, (sum.peak - peak) * a.c, 0.f);
     sum.s = group_sum<64>(sum.s);
     sum.w = group_sum<64>(sum.w);
     sum.peak = peak;
+    const u64 *found = nullptr;
+    int nfound = 0;
     if constexpr (TOP) {
-        // the parts' lists descend: a key's place is the number of larger ones in each
-        const int k = a.top, n = splits * k;
-        for (int i = tid; i < n; i += N) keys[i] = a.part_keys[part * k + i];
-        for (int i = tid; i < k; i += N) found[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += N) {
-            const u64 key = keys[i];
-            int place = 0;
-            for (int q = 0; q < splits && key && place < k; q++) {
-                int lo = 0, hi = k;
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (keys[q * k + mid] > key) lo = mid + 1; else hi = mid;
-                }
-                place += lo;
-            }
-            if (key && place < k) found[place] = key;
-        }
-        __syncthreads();
+        if (fabsf(peak) < kInf && sum.s < kInf)
+            nfound = largest<T, N>(top, p, s, pieces, mine, edge, splits, a.pieces_per_part, (s.nvec + splits - 1) / splits, peak, a.top);
+        found = top.found;
     }
-    if constexpr (KIND == kLogprobs) finish_logprobs<N>(a, row, sum, token_logit, found);
+    if constexpr (KIND == kLogprobs) finish_logprobs<N>(a, row, sum, token_logit, found, nfound);
     else if (tid < 64) {
         Slope g;
         finish_distill(a, entries, row, sum, false, g);
@@ -724,9 +963,17 @@ constexpr int kGradThreads = 256;
 
 // Writes vector j of a row, whose elements are f.
 template <typename T>
-EWF_OPS_DEV void store_vector(typename T::raw *out, const Span<T> &s, int j, const float *f)
+EWF_OPS_DEV void store_vector(typename T::raw *out, const Span<T> &s, int j, const float *f, int nt = 0)
 {
-    store16<T>(out + s.head + (int64_t)j * Vec16<T>::V, pack16<T>(f));
+    u32x4 *to = (u32x4 *)(out + s.head) + j;
+    if (NTBITS & 4) __builtin_nontemporal_store(pack16<T>(f), to);
+    else *to = pack16<T>(f);
+}
+template <typename T>
+EWF_OPS_DEV u32x4 load_vector(const typename T::raw *p, const Span<T> &s, int j, int nt)
+{
+    const typename Vec16<T>::at *from = (const typename Vec16<T>::at *)(p + s.head) + j;
+    return NTBITS & 2 ? __builtin_nontemporal_load(from) : *from;
 }
 
 // One workgroup a piece of U vectors a thread of a row.  dx_j = c (g ([j = token] - p_j) - h p_j (log p_j + entropy))
@@ -735,9 +982,10 @@ __global__ void __launch_bounds__(kGradThreads) k_logprobs_grad(VocabLaunch a)
 {
     typedef typename T::raw raw;
     constexpr int V = Vec16<T>::V, N = kGradThreads;
-    const uint32_t pieces = (uint32_t)a.splits, row = a.row0 + blockIdx.x / pieces, piece = blockIdx.x - blockIdx.x / pieces * pieces;
-    const raw *p = (const raw *)a.logits + row_offset(a.r, row, a.slogits);
-    raw *out = (raw *)a.dlogits + row_offset(a.r, row, a.sdlogits);
+    const uint32_t pieces = (uint32_t)a.splits, piece = blockIdx.x % pieces;
+    const RowAt row = row_at(a.r, a.row0 + blockIdx.x / pieces);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    raw *out = (raw *)a.dlogits + at(row, a.sdlogits);
     const Span<T> s(out, a.r.cols);
     const int tid = threadIdx.x, j0 = (int)piece * (U * N) + tid;
     const bool edge = piece == 0 && tid < s.edges();
@@ -754,12 +1002,12 @@ __global__ void __launch_bounds__(kGradThreads) k_logprobs_grad(VocabLaunch a)
 #pragma unroll
     for (int u = 0; u < U; u++) {
         v[u] = u32x4{0u, 0u, 0u, 0u};
-        if (j0 + u * N < s.nvec) v[u] = load16<T>(p + s.head + (int64_t)(j0 + u * N) * V);
+        if (j0 + u * N < s.nvec) v[u] = load_vector<T>(p, s, j0 + u * N, 0);
     }
     const float x = edge ? load1<T>(p + s.edge(tid)) : 0.f;
-    const float peak = a.peak[row_offset(a.r, row, a.speak)], logsum = a.logsum[row_offset(a.r, row, a.slogsum)];
-    const float g = a.dlogprob ? a.dlogprob[row_offset(a.r, row, a.sdlogprob)] * a.scale : 0.f;
-    const float h = ENT ? a.dentropy[row_offset(a.r, row, a.sdentropy)] * a.scale : 0.f, H = ENT ? a.entropy[row_offset(a.r, row, a.sentropy)] : 0.f;
+    const float peak = a.peak[at(row, a.speak)], logsum = a.logsum[at(row, a.slogsum)];
+    const float g = a.dlogprob ? a.dlogprob[at(row, a.sdlogprob)] * a.scale : 0.f;
+    const float h = ENT ? a.dentropy[at(row, a.sdentropy)] * a.scale : 0.f, H = ENT ? a.entropy[at(row, a.sentropy)] : 0.f;
     const bool none = peak == -kInf;                     // (no logit at all: no gradient)
     const float ref = none ? 0.f : peak, off = none ? 0.f : logsum * kLog2E;
     const float A = none ? 0.f : -g - (ENT ? h * H : 0.f), B = none ? 0.f : -h * kLn2, hot = none ? 0.f : g;
@@ -774,7 +1022,7 @@ __global__ void __launch_bounds__(kGradThreads) k_logprobs_grad(VocabLaunch a)
         float f[V];
 #pragma unroll
         for (int e = 0; e < V; e++) f[e] = slope(element<T>(v[u], e), c + e);
-        store_vector<T>(out, s, j, f);
+        store_vector<T>(out, s, j, f, 0);
     }
     if (edge) store1<T>(out + s.edge(tid), slope(x, s.edge(tid)));
 }
@@ -807,9 +1055,10 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
     typedef typename T::raw raw;
     constexpr int V = Vec16<T>::V, N = kGradThreads;
     __shared__ Entries<N> l;
-    const uint32_t pieces = (uint32_t)a.splits, row = a.row0 + blockIdx.x / pieces, piece = blockIdx.x - blockIdx.x / pieces * pieces;
-    const raw *p = (const raw *)a.logits + row_offset(a.r, row, a.slogits);
-    raw *out = (raw *)a.dlogits + row_offset(a.r, row, a.sdlogits);
+    const uint32_t pieces = (uint32_t)a.splits, piece = blockIdx.x % pieces;
+    const RowAt row = row_at(a.r, a.row0 + blockIdx.x / pieces);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    raw *out = (raw *)a.dlogits + at(row, a.sdlogits);
     const Span<T> s(out, a.r.cols);
     const int tid = threadIdx.x, begin = (int)piece * (U * N), j0 = begin + tid;
     const int end = begin + U * N < s.nvec ? begin + U * N : s.nvec;
@@ -818,16 +1067,16 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
 #pragma unroll
     for (int u = 0; u < U; u++) {
         v[u] = u32x4{0u, 0u, 0u, 0u};
-        if (j0 + u * N < end) v[u] = load16<T>(p + s.head + (int64_t)(j0 + u * N) * V);
+        if (j0 + u * N < end) v[u] = load_vector<T>(p, s, j0 + u * N, 0);
     }
     const float x = edge ? load1<T>(p + s.edge(tid)) : 0.f;
     clear(l);
     __syncthreads();
     if (tid < 64) read_entries<T>(l, a, row, p, s, begin, end, piece == 0);
     __syncthreads();
-    const float peak = a.peak[row_offset(a.r, row, a.speak)], logsum = a.logsum[row_offset(a.r, row, a.slogsum)];
-    const float tail = a.with_tail ? a.tail[row_offset(a.r, row, a.stail)] : 0.f;
-    const float weight = a.dloss ? a.dloss[row_offset(a.r, row, a.sdloss)] : 1.f;
+    const float peak = a.peak[at(row, a.speak)], logsum = a.logsum[at(row, a.slogsum)];
+    const float tail = a.with_tail ? a.tail[at(row, a.stail)] : 0.f;
+    const float weight = a.dloss ? a.dloss[at(row, a.sdloss)] : 1.f;
     Slope g = slope_of(a, peak, logsum, tail, l.tail_q, l.total_q, weight);
     const bool padding = l.live == 0;
     if (tid < a.entries) {
@@ -848,7 +1097,7 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
         if (padding)
 #pragma unroll
             for (int e = 0; e < V; e++) f[e] = 0.f;
-        store_vector<T>(out, s, j, f);
+        store_vector<T>(out, s, j, f, 0);
     }
     if (edge) {
         const int k = l.edge[tid];
@@ -867,9 +1116,9 @@ __global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
     constexpr int V = Vec16<T>::V;
     __shared__ float sums[48];
     __shared__ Entries<N> l;
-    const uint32_t row = a.row0 + blockIdx.x;
-    const raw *p = (const raw *)a.logits + row_offset(a.r, row, a.slogits);
-    raw *out = (raw *)a.dlogits + row_offset(a.r, row, a.sdlogits);
+    const RowAt row = row_at(a.r, a.row0 + blockIdx.x);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    raw *out = (raw *)a.dlogits + at(row, a.sdlogits);
     const Span<T> s(out, a.r.cols);
     const int tid = threadIdx.x;
     const bool edge = tid < s.edges();
@@ -877,7 +1126,7 @@ __global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
 #pragma unroll
     for (int u = 0; u < NV; u++) {
         v[u] = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
-        if (tid + u * N < s.nvec) v[u] = load16<T>(p + s.head + (int64_t)(tid + u * N) * V);
+        if (tid + u * N < s.nvec) v[u] = load_vector<T>(p, s, tid + u * N, 0);
     }
     float x = edge ? load1<T>(p + s.edge(tid)) : -kInf;
     clear(l);
@@ -894,7 +1143,7 @@ __global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
         return;
     }
     const uint32_t held = trips_with_entries(l);
-    const int on_edge = tid < 16 ? l.edge[tid] : -1;
+    const int on_edge = tid < kEdges ? l.edge[tid] : -1;
     if (a.with_tail) {
         // the entries are left out of the sums: their logits are held apart, and their gradients replace what becomes of these
 #pragma unroll
@@ -945,7 +1194,7 @@ __global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
         total = __shfl(total, 0);
     }
     if (tid < 64) {
-        sum.peak = peak; sum.m = ref; sum.s = total;
+        sum.peak = peak; sum.s = total;
         Slope g;
         finish_distill(a, l, row, sum, true, g);
     }
@@ -959,7 +1208,7 @@ __global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
 #pragma unroll
         for (int e = 0; e < V; e++) f[e] = coef * __builtin_amdgcn_exp2f(fmaf(element<T>(v[u], e) - from, a.c, -off));
         if (held >> u & 1) put_entries<V>(l, u, s.head, f);
-        store_vector<T>(out, s, j, f);
+        store_vector<T>(out, s, j, f, 0);
     }
     if (edge) store1<T>(out + s.edge(tid), on_edge >= 0 ? l.grad[on_edge] : coef * __builtin_amdgcn_exp2f(fmaf(x - from, a.c, -off)));
 }
@@ -980,8 +1229,9 @@ void by_rows(VocabLaunch a, int64_t blocks_per_row, int threads, F &&launch)
 {
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 31) / threads / blocks_per_row);
     for (int64_t row = 0; row < a.r.rows; row += most) {
-        a.row0 = (uint32_t)row;
         const int64_t rows = std::min<int64_t>(most, a.r.rows - row);
+        a.row0 = (uint32_t)row;
+        a.rows = (uint32_t)rows;
         launch(a, dim3((unsigned)(rows * blocks_per_row)), (unsigned)rows);
     }
 }
@@ -991,13 +1241,15 @@ int vectors(const VocabLaunch &a) { return (a.r.cols + (a.dtype == EWF_F32 ? 4 :
 template <typename T, int N, bool ENT, bool TOP, int KIND>
 void run_rows(const VocabLaunch &a, hipStream_t stream)
 {
+    constexpr bool kLong = N > 64;
     by_rows(a, a.splits, N, [&](VocabLaunch b, dim3 grid, unsigned rows) {
-        if (b.splits > 1) {      // (all launches' parts are apart)
-            b.parts += (int64_t)b.row0 * b.splits * 4;
-            if (TOP) b.part_keys += (int64_t)b.row0 * b.splits * b.top;
-        }
-        hipLaunchKernelGGL((k_rows<T, N, ENT, TOP, KIND>), grid, dim3(N), 0, stream, b);
-        if (b.splits > 1) hipLaunchKernelGGL((k_join<T, TOP ? 1024 : 64, TOP, KIND>), dim3(rows), dim3(TOP ? 1024 : 64), 0, stream, b);
+        if (b.parts) b.parts += (int64_t)b.row0 * b.splits * 4;          // (all launches' parts are apart)
+        if (b.pieces) b.pieces += (int64_t)b.row0 * b.splits * b.pieces_per_part;
+        grid.x = std::min(grid.x, (unsigned)b.resident);
+        if (kLong && b.stream) hipLaunchKernelGGL((k_rows<T, N, ENT, TOP && kLong, KIND, kLong>), grid, dim3(N), 0, stream, b);
+        else hipLaunchKernelGGL((k_rows<T, N, ENT, TOP && kLong, KIND, false>), grid, dim3(N), 0, stream, b);
+        constexpr int J = TOP && kLong ? 256 : 64;
+        if (b.parts) hipLaunchKernelGGL((k_join<T, J, TOP, KIND>), dim3(rows), dim3(J), 0, stream, b);
     });
 }
 
@@ -1022,8 +1274,7 @@ struct RunRows {
     template <typename T> void operator()() const
     {
         if (a.threads == 64) run_kind<T, 64>(a, stream);
-        else if (a.threads == 256) run_kind<T, 256>(a, stream);
-        else run_kind<T, 1024>(a, stream);
+        else run_kind<T, 256>(a, stream);
     }
 };
 
@@ -1089,12 +1340,20 @@ void plan_vocab(VocabLaunch &a, int units)
 {
     const int n = vectors(a);
     a.held = a.entries && a.dlogits && n <= kHeldVectors;
-    a.threads = n <= 256 ? 64 : a.r.rows < (uint32_t)units ? 1024 : 256;
+    a.threads = n <= 256 ? 64 : 256;
+    // few rows are shared by workgroups that take 1024 vectors at least, where a second launch costs less than what it saves: one row of 131072 float32
+    // takes 20 us whole, 7.7 in 32 parts; eight rows of 50257 bfloat16 8.1 us whole (and 8.1 in 6 parts), with 20 alternatives, which need the
+    // second launch anyway, 17.3 and 12.2
     a.splits = 1;
-    if (a.r.rows < (uint32_t)units && n > 32768) {
-        a.splits = (int)std::min<int64_t>(std::min<int64_t>(64, n / 8192), (2 * units + a.r.rows - 1) / a.r.rows);
-        if (a.top) a.splits = std::min(a.splits, kMaxJoin / a.top);
-    }
+    if (a.r.rows < (uint32_t)units && n >= (a.top ? 2048 : 12288))
+        a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, n / 1024), (2 * units + a.r.rows - 1) / a.r.rows));
+    // (the largest a row can have: its vectors begin at its first whole 16 bytes)
+    if (a.top && a.threads == 256) a.pieces_per_part = ((n + a.splits - 1) / a.splits + kPieceTrips * 256 - 1) / (kPieceTrips * 256) * (256 / kPieceLanes);
+    // workgroups that stay: as many as share the rows evenly
+    const int64_t room = (int64_t)units * 2048 / a.threads, items = (int64_t)a.r.rows * a.splits, each = (items + room - 1) / room;
+    a.resident = each ? (int)((items + each - 1) / each) : 0;
+    // logits that the memory-side cache cannot keep pass it by: bfloat16 [4096, 32768] 51.7 us, passing 45.6; [2048, 32768] 27.2 and 24.7; [1024, 32768] 14.3 and 15.7
+    a.stream = (int64_t)a.r.rows * a.r.cols * (a.dtype == EWF_F32 ? 4 : 2) >= (int64_t)128 << 20;
 }
 
 void launch_token_logprobs(const VocabLaunch &a, hipStream_t stream) { by_type(a.dtype, RunRows{a, stream}); }
