@@ -430,7 +430,8 @@ typedef struct {
 } ewf_distill_args;
 ewf_status ewf_distill_workspace(const ewf_distill_args *a, size_t *workspace_bytes);
 ewf_status ewf_distill(const ewf_distill_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
-ewf_status ewf_distill_grad(const ewf_distill_args *a, void *hip_stream);
+ewf_status ewf_distill_grad_workspace(const ewf_distill_args *a, size_t *workspace_bytes);
+ewf_status ewf_distill_grad(const ewf_distill_args *a, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 const char *ewf_last_error(void);
 

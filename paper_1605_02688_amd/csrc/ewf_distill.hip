@@ -1,0 +1,301 @@
+// The loss of a student's logits against a teacher's entries, and its gradient, by itself or in the loss's own sweep.
+#include "ewf_vocab_rows.h"
+
+namespace ewf {
+
+namespace {
+
+// One wavefront a row: what the gradients of a row need, from the statistics that the loss has saved.
+template <typename T>
+__global__ void __launch_bounds__(64) k_distill_prepare(VocabLaunch a)
+{
+    typedef typename T::raw raw;
+    __shared__ Entries<64> l;
+    const RowAt row = row_at(a.r, a.row0 + blockIdx.x);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    const Stats r = {a.peak[at(row, a.speak)], a.logsum[at(row, a.slogsum)], a.with_tail ? a.tail[at(row, a.stail)] : 0.f};
+    take_entries<T>(l, a, row, p, Span<T>(p, a.r.cols), 0, 0, false);
+    __syncthreads();
+    prepare_gradients(a, l, row, r, prepared_row(a, blockIdx.x));
+}
+
+constexpr int kGradThreads = 256, kGradVectors = 2;
+
+// One workgroup a piece of a row: the element-wise gradient, and the entries' that lie in it, each in the list of the thread that takes its vector
+// or its edge.
+template <typename T, bool STREAM>
+__global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
+{
+    typedef typename T::raw raw;
+    constexpr int V = Vec16<T>::V, N = kGradThreads, U = kGradVectors;
+    __shared__ int head[N], next[kMaxTop], index[kMaxTop];
+    __shared__ float grad[kMaxTop];
+    const uint32_t pieces = (uint32_t)a.splits, piece = blockIdx.x % pieces, in_launch = blockIdx.x / pieces;
+    const RowAt row = row_at(a.r, a.row0 + in_launch);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    raw *out = (raw *)a.dlogits + at(row, a.sdlogits);
+    const Span<T, kLine> s(out, a.r.cols);
+    const int tid = threadIdx.x, begin = (int)piece * (U * N), end = begin + U * N < s.nvec ? begin + U * N : s.nvec;
+    const bool edge = piece == 0 && tid < s.edges();
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        v[u] = u32x4{0u, 0u, 0u, 0u};
+        if (begin + u * N + tid < end) v[u] = load_vector<T, STREAM>(p + s.head, begin + u * N, tid);
+    }
+    const float x = edge ? load1<T>(p + s.edge(tid)) : 0.f;
+    const Prepared *prepared = prepared_row(a, in_launch);
+    const Prepared::Entry e = tid < a.entries ? prepared->entry[tid] : Prepared::Entry{-1, 0.f};
+    const Exponent t = prepared->exponent(a.c);
+    const float coef = prepared->coef;
+    const bool padding = prepared->padding;
+    head[tid] = -1;
+    __syncthreads();
+    if (e.index >= 0) {
+        const int j = s.inside(e.index) ? (e.index - s.head) / V - begin : -1;
+        const int owner = j >= 0 ? (j < U * N ? j % N : -1) : s.inside(e.index) || piece ? -1 : s.edge_of(e.index);
+        index[tid] = e.index;
+        grad[tid] = e.grad;
+        if (owner >= 0) next[tid] = atomicExch(&head[owner], tid);
+    }
+    __syncthreads();
+    const int list = head[tid];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int j = begin + u * N + tid;
+        if (j >= end) continue;
+        float f[V], q[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) f[i] = element<T>(v[u], i);
+        t.of<V>(f, q);
+#pragma unroll
+        for (int i = 0; i < V; i++) f[i] = coef * __builtin_amdgcn_exp2f(q[i]);
+        for (int k = list; k >= 0; k = next[k]) {
+            const int at = index[k] - s.head - j * V;    // (another vector's, or an edge's: outside)
+            const float g = grad[k];
+#pragma unroll
+            for (int i = 0; i < V; i++) f[i] = i == at ? g : f[i];
+        }
+        if (padding)
+#pragma unroll
+            for (int i = 0; i < V; i++) f[i] = 0.f;
+        store_vector<T>(out + s.head, begin + u * N, tid, f);
+    }
+    if (edge) {
+        float q;
+        t.of<1>(&x, &q);
+        q = coef * __builtin_amdgcn_exp2f(q);
+        for (int k = list; k >= 0; k = next[k]) q = index[k] == s.edge(tid) ? grad[k] : q;
+        store1<T>(out + s.edge(tid), padding ? 0.f : q);
+    }
+}
+
+// A workgroup holds a row in registers, NV vectors a thread, and takes rows one after the other: logits are read once, a vector's registers
+// take the next row's as soon as its gradients are written.  Between the two barriers of a row its sums are taken as its vectors arrive; the
+// next row's entries are read behind them.
+template <typename T, int N, int NV, bool STREAM>
+__global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
+{
+    typedef typename T::raw raw;
+    constexpr int V = Vec16<T>::V, W = N / 64, LINE = N > 64 ? kLine : 16;
+    typedef Span<T, LINE> RowSpan;
+    __shared__ float parts[2][2][16];
+    __shared__ Entries<N> lists[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t i = blockIdx.x;
+    RowAt row = row_at(a.r, a.row0 + i);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    raw *out = (raw *)a.dlogits + at(row, a.sdlogits);
+    RowSpan s(out, a.r.cols);
+    u32x4 v[NV];
+    float x;
+    auto fetch = [&](u32x4 &v, const raw *p, const RowSpan &s, int u) {
+        if (u * N + tid < s.nvec) v = load_vector<T, STREAM>(p + s.head, u * N, tid);
+        else v = u32x4{kNothing<T>, kNothing<T>, kNothing<T>, kNothing<T>};
+    };
+#pragma unroll
+    for (int u = 0; u < NV; u++) fetch(v[u], p, s, u);
+    x = tid < s.edges() ? load1<T>(p + s.edge(tid)) : -kInf;
+    if (tid < 64) take_entries<T>(lists[0], a, row, p, s, 0, s.nvec, true);
+    for (int turn = 0;; turn ^= 1) {
+        const Entries<N> &l = lists[turn];
+        __syncthreads();
+        const bool padding = l.live == 0;
+        const uint32_t held = trips_with_entries(l);
+        const int on_edge = tid < s.edges() ? l.edge[tid] : -1;
+        // the next row, its entries on their way while this one's sums are taken
+        const uint32_t next = i + gridDim.x;
+        const bool more = next < a.rows;
+        const RowAt nrow = row_at(a.r, a.row0 + (more ? next : i));
+        const raw *np = (const raw *)a.logits + at(nrow, a.slogits);
+        raw *nout = (raw *)a.dlogits + at(nrow, a.sdlogits);
+        const RowSpan ns(nout, a.r.cols);
+        RawEntries entries;
+        const bool reader = more && tid < 64;
+        if (reader) read_entries(entries, a, nrow);
+        Sums sum;
+#pragma unroll
+        for (int u = 0; u < NV; u++) {
+            if (__any(u * N + tid < s.nvec)) {
+                float f[V];
+#pragma unroll
+                for (int e = 0; e < V; e++) f[e] = element<T>(v[u], e);
+                if (a.with_tail && held >> u & 1)       // (what no entry names: the entries' own sum is taken with them)
+                    each_entry<V>(l, u, s.head, [&](int at, int) {
+#pragma unroll
+                        for (int e = 0; e < V; e++) f[e] = e == at ? -kInf : f[e];
+                    });
+                add<false, V>(sum, f, max_of<V>(f), a.c, a.lag);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // (logits are unpacked again below: kept unpacked they would not fit)
+#pragma unroll
+        for (int u = 0; u < NV; u++) asm volatile("" : "+v"(v[u]));
+        if (reader) read_logits<T>(entries, a, np);
+        const float own = a.with_tail && on_edge >= 0 ? -kInf : x;
+        add<false, 1>(sum, &own, own, a.c, a.lag);
+        sum = wave_sums<false>(sum, a.c);
+        if (W > 1) {
+            if (lane == 0) { parts[turn][0][wave] = sum.peak; parts[turn][1][wave] = sum.s; }
+            __syncthreads();
+            sum = joined_sums<W, false>(parts[turn][0], parts[turn][1], nullptr, a.c);
+        }
+        settle<false>(sum, a.c);
+        if (beyond(sum.peak, a.c)) sum_again<T, N>(a, p, s, 0, s.nvec, true, a.with_tail, l, &parts[turn][0][0], sum);
+        Stats r = stats_of(a, l, sum);
+        r = {scalar(r.peak), scalar(r.logsum), scalar(r.tail)};
+        if (wave == W - 1) {
+            if (!padding) finish_distill(a, l, row, r);
+            else if (lane == 0) {
+                a.loss[at(row, a.sloss)] = 0.f;
+                if (a.peak) a.peak[at(row, a.speak)] = 0.f;
+                if (a.logsum) a.logsum[at(row, a.slogsum)] = 0.f;
+                if (a.tail) a.tail[at(row, a.stail)] = 0.f;
+            }
+        }
+        const Slope g(a, l, r, a.dloss ? a.dloss[at(row, a.sdloss)] : 1.f);
+        if (reader) rank_entries<T>(lists[turn ^ 1], entries, a, ns, 0, ns.nvec, true);
+#pragma unroll
+        for (int u = 0; u < NV; u++) {
+            const int j = u * N + tid;
+            if (j < s.nvec) {
+                float f[V], t[V];
+#pragma unroll
+                for (int e = 0; e < V; e++) f[e] = element<T>(v[u], e);
+                g.rest.template of<V>(f, t);
+#pragma unroll
+                for (int e = 0; e < V; e++) f[e] = g.coef * __builtin_amdgcn_exp2f(t[e]);
+                if (held >> u & 1)
+                    each_entry<V>(l, u, s.head, [&](int at, int k) {
+                        const float d = g.entry(l, k);
+#pragma unroll
+                        for (int e = 0; e < V; e++) f[e] = e == at ? d : f[e];
+                    });
+                if (padding)
+#pragma unroll
+                    for (int e = 0; e < V; e++) f[e] = 0.f;
+                store_vector<T>(out + s.head, u * N, tid, f);
+            }
+            if (more) fetch(v[u], np, ns, u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < s.edges()) {
+            float t;
+            g.rest.template of<1>(&x, &t);
+            store1<T>(out + s.edge(tid), padding ? 0.f : on_edge >= 0 ? g.entry(l, on_edge) : g.coef * __builtin_amdgcn_exp2f(t));
+        }
+        if (!more) return;
+        x = tid < ns.edges() ? load1<T>(np + ns.edge(tid)) : -kInf;
+        i = next;
+        row = nrow;
+        p = np;
+        out = nout;
+        s = ns;
+    }
+}
+
+struct RunRows {
+    const VocabLaunch &a;
+    hipStream_t stream;
+    template <typename T, int N> void go() const
+    {
+        if (a.with_tail) run_rows<T, N, false, false, kDistillTail>(a, stream);
+        else run_rows<T, N, false, false, kDistill>(a, stream);
+    }
+    template <typename T> void operator()() const
+    {
+        if (a.threads == 64) go<T, 64>();
+        else go<T, 256>();
+    }
+};
+
+struct RunPrepare {
+    const VocabLaunch &a;
+    hipStream_t stream;
+    template <typename T> void operator()() const
+    {
+        by_rows(a, 1, 64, [&](VocabLaunch b, dim3 grid, unsigned) {
+            b.prepared = (char *)b.prepared + b.row0 * prepared_bytes(b.entries);
+            hipLaunchKernelGGL((k_distill_prepare<T>), grid, dim3(64), 0, stream, b);
+        });
+    }
+};
+
+struct RunGrad {
+    VocabLaunch a;
+    hipStream_t stream;
+    template <typename T> void operator()()
+    {
+        a.splits = std::max(1, (vectors(a) + kGradVectors * kGradThreads - 1) / (kGradVectors * kGradThreads));
+        by_rows(a, a.splits, kGradThreads, [&](VocabLaunch b, dim3 grid, unsigned) {
+            b.prepared = (char *)b.prepared + b.row0 * prepared_bytes(b.entries);
+            if (b.stream) hipLaunchKernelGGL((k_distill_grad<T, true>), grid, dim3(kGradThreads), 0, stream, b);
+            else hipLaunchKernelGGL((k_distill_grad<T, false>), grid, dim3(kGradThreads), 0, stream, b);
+        });
+    }
+};
+
+struct RunHeld {
+    const VocabLaunch &a;
+    hipStream_t stream;
+    template <typename T, int N, int NV> void go() const
+    {
+        by_rows(a, 1, N, [&](const VocabLaunch &b, dim3 grid, unsigned) {
+            grid.x = std::min(grid.x, (unsigned)b.resident);
+            if (N > 64 && b.stream) hipLaunchKernelGGL((k_distill_held<T, N, NV, (N > 64)>), grid, dim3(N), 0, stream, b);
+            else hipLaunchKernelGGL((k_distill_held<T, N, NV, false>), grid, dim3(N), 0, stream, b);
+        });
+    }
+    template <typename T> void operator()() const
+    {
+        const int n = vectors(a);
+        if (n <= 64) go<T, 64, 1>();
+        else if (n <= 128) go<T, 64, 2>();
+        else if (n <= 256) go<T, 64, 4>();
+        else if (n <= 512) go<T, 256, 2>();
+        else if (n <= 1024) go<T, 256, 4>();
+        else if (n <= 2048) go<T, 256, 8>();
+        else if (n <= 4096) go<T, 1024, 4>();
+        else if (n <= 8192) go<T, 1024, 8>();
+        else if (n <= 12288) go<T, 1024, 12>();
+        else go<T, 1024, 16>();
+    }
+};
+
+}  // namespace
+
+void launch_distill_grad(const VocabLaunch &a, hipStream_t stream)
+{
+    by_type(a.dtype, RunPrepare{a, stream});
+    by_type(a.dtype, RunGrad{a, stream});
+}
+
+void launch_distill(const VocabLaunch &a, hipStream_t stream)
+{
+    if (a.held) return by_type(a.dtype, RunHeld{a, stream});
+    by_type(a.dtype, RunRows{a, stream});                   // (prepares the gradients too)
+    if (a.dlogits) by_type(a.dtype, RunGrad{a, stream});
+}
+
+}  // namespace ewf

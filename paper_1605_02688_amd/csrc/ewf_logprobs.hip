@@ -1,0 +1,144 @@
+// Log probabilities of given tokens with entropy and the largest alternatives, and their gradient; the plan of all operators over rows of logits.
+#include "ewf_vocab_rows.h"
+
+namespace ewf {
+
+namespace {
+
+constexpr int kGradThreads = 256, kGradVectors = 2;
+
+// One workgroup a piece of a row: dx_j = scale (g ([j = token] - p_j) - h p_j (log p_j + entropy)).
+template <typename T, bool ENT, bool STREAM>
+__global__ void __launch_bounds__(kGradThreads) k_logprobs_grad(VocabLaunch a)
+{
+    typedef typename T::raw raw;
+    constexpr int V = Vec16<T>::V, N = kGradThreads, U = kGradVectors;
+    const uint32_t pieces = (uint32_t)a.splits, piece = blockIdx.x % pieces;
+    const RowAt row = row_at(a.r, a.row0 + blockIdx.x / pieces);
+    const raw *p = (const raw *)a.logits + at(row, a.slogits);
+    raw *out = (raw *)a.dlogits + at(row, a.sdlogits);
+    const Span<T, kLine> s(out, a.r.cols);
+    const int tid = threadIdx.x, begin = (int)piece * (U * N), j0 = begin + tid;
+    const bool edge = piece == 0 && tid < s.edges();
+    int token;
+    if (is_padding(a, row, token)) {
+        const float zero[V] = {};
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (j0 + u * N < s.nvec) store_vector<T>(out + s.head, begin + u * N, tid, zero);
+        if (edge) store1<T>(out + s.edge(tid), 0.f);
+        return;
+    }
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        v[u] = u32x4{0u, 0u, 0u, 0u};
+        if (j0 + u * N < s.nvec) v[u] = load_vector<T, STREAM>(p + s.head, begin + u * N, tid);
+    }
+    const float x = edge ? load1<T>(p + s.edge(tid)) : 0.f;
+    const float peak = a.peak[at(row, a.speak)], logsum = a.logsum[at(row, a.slogsum)];
+    const float g = a.dlogprob ? a.dlogprob[at(row, a.sdlogprob)] * a.scale : 0.f;
+    const float h = ENT ? a.dentropy[at(row, a.sdentropy)] * a.scale : 0.f, H = ENT ? a.entropy[at(row, a.sentropy)] : 0.f;
+    const bool none = peak == -kInf;                     // (no logit at all: no gradient)
+    const Exponent e(none ? 0.f : peak, none ? 0.f : logsum * kLog2E, a.c);
+    // p = r 2^t, log p = (t + rest) ln 2
+    const float r = none ? 0.f : __builtin_amdgcn_exp2f(e.rest), hot = none ? 0.f : g;
+    const float A = r * (-g - (ENT ? h * fmaf(e.rest, kLn2, H) : 0.f)), B = r * -h * kLn2;
+    auto slope = [&](float t) {
+        const float q = __builtin_amdgcn_exp2f(t);
+        return q * (ENT ? fmaf(B, fmaxf(t, kFloor), A) : A);
+    };
+    // (of another piece's token: no vector of this one)
+    const int in = token - s.head, token_vec = s.inside(token) ? in / V : -1, token_at = in % V;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        const int j = j0 + u * N;
+        if (j >= s.nvec) continue;
+        float f[V], t[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) f[i] = element<T>(v[u], i);
+        e.of<V>(f, t);
+#pragma unroll
+        for (int i = 0; i < V; i++) f[i] = slope(t[i]);
+        if (j == token_vec)
+#pragma unroll
+            for (int i = 0; i < V; i++) f[i] += i == token_at ? hot : 0.f;
+        store_vector<T>(out + s.head, begin + u * N, tid, f);
+    }
+    if (edge) {
+        float t;
+        e.of<1>(&x, &t);
+        store1<T>(out + s.edge(tid), slope(t) + (s.edge(tid) == token ? hot : 0.f));
+    }
+}
+
+template <typename T, int N>
+void run_kind(const VocabLaunch &a, hipStream_t stream)
+{
+    if (a.top) {
+        if (a.entropy) run_rows<T, N, true, true, kLogprobs>(a, stream);
+        else run_rows<T, N, false, true, kLogprobs>(a, stream);
+    } else {
+        if (a.entropy) run_rows<T, N, true, false, kLogprobs>(a, stream);
+        else run_rows<T, N, false, false, kLogprobs>(a, stream);
+    }
+}
+
+struct RunRows {
+    const VocabLaunch &a;
+    hipStream_t stream;
+    template <typename T> void operator()() const
+    {
+        if (a.threads == 64) run_kind<T, 64>(a, stream);
+        else run_kind<T, 256>(a, stream);
+    }
+};
+
+struct RunGrad {
+    VocabLaunch a;
+    hipStream_t stream;
+    template <typename T, bool ENT> void go()
+    {
+        const int pieces = std::max(1, (vectors(a) + kGradVectors * kGradThreads - 1) / (kGradVectors * kGradThreads));
+        a.splits = pieces;
+        by_rows(a, pieces, kGradThreads, [&](const VocabLaunch &b, dim3 grid, unsigned) {
+            if (b.stream) hipLaunchKernelGGL((k_logprobs_grad<T, ENT, true>), grid, dim3(kGradThreads), 0, stream, b);
+            else hipLaunchKernelGGL((k_logprobs_grad<T, ENT, false>), grid, dim3(kGradThreads), 0, stream, b);
+        });
+    }
+    template <typename T> void operator()()
+    {
+        if (a.dentropy) go<T, true>();
+        else go<T, false>();
+    }
+};
+
+}  // namespace
+
+// Workgroups of a compute unit that hold rows of n vectors.
+static int held_workgroups(int n) { return n <= 256 ? 16 : n <= 2048 ? 4 : 1; }
+
+void plan_vocab(VocabLaunch &a, int units)
+{
+    const int n = vectors(a);
+    a.held = a.entries && a.dlogits && a.loss && n <= kHeldVectors;
+    a.threads = n <= 256 ? 64 : 256;
+    // few rows are shared by workgroups that take 1024 vectors at least, where a second launch costs less than what it saves: one row of 131072 float32
+    // takes 20 us whole, 7.7 in 32 parts; eight rows of 50257 bfloat16 8.1 us whole (and 8.1 in 6 parts), with 20 alternatives, which need the
+    // second launch anyway, 17.3 and 12.2
+    a.splits = 1;
+    if (a.r.rows < (uint32_t)units && n >= (a.top ? 2048 : 12288) && !a.held && (a.loss || !a.dlogits))
+        a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, n / 1024), (2 * units + a.r.rows - 1) / a.r.rows));
+    // (the largest a row can have: its vectors begin at its first whole 16 bytes)
+    if (a.top && a.threads == 256) a.pieces_per_part = ((n + a.splits - 1) / a.splits + kPieceTrips * 256 - 1) / (kPieceTrips * 256) * (256 / kPieceLanes);
+    // workgroups that stay: as many as share the rows evenly
+    const int64_t room = (int64_t)units * (a.held ? held_workgroups(n) : 2048 / a.threads), items = (int64_t)a.r.rows * a.splits, each = (items + room - 1) / room;
+    a.resident = each ? (int)((items + each - 1) / each) : 0;
+    // logits that the memory-side cache cannot keep pass it by: bfloat16 [4096, 32768] 51.7 us, passing 45.6; [2048, 32768] 27.2 and 24.7; [1024, 32768] 14.3 and 15.7
+    a.stream = (int64_t)a.r.rows * a.r.cols * (a.dtype == EWF_F32 ? 4 : 2) >= (int64_t)128 << 20;
+}
+
+void launch_token_logprobs(const VocabLaunch &a, hipStream_t stream) { by_type(a.dtype, RunRows{a, stream}); }
+void launch_token_logprobs_grad(const VocabLaunch &a, hipStream_t stream) { by_type(a.dtype, RunGrad{a, stream}); }
+
+}  // namespace ewf

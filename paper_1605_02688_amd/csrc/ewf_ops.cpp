@@ -1,5 +1,5 @@
 // The operators of sequence models: argument checks and layouts.  The kernels are in ewf_norm.hip, ewf_act8.hip,
-// ewf_recurrence.hip and ewf_vocab.hip; everything that they assume about their operands is established here.
+// ewf_recurrence.hip, ewf_logprobs.hip and ewf_distill.hip; everything that they assume about their operands is established here.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -544,7 +544,7 @@ ewf_status logprobs_layout(const ewf_token_logprobs_args *a, bool grad, VocabLau
         v.c.check_results({{"dlogits", "logits"}});
     }
     ewf_status st = v.end();
-    if (st == EWF_OK && !grad) plan_vocab(n, device_cu_count());
+    if (st == EWF_OK) plan_vocab(n, device_cu_count());
     return st;
 }
 
@@ -573,12 +573,11 @@ ewf_status distill_layout(const ewf_distill_args *a, bool grad, VocabLaunch &n)
     n.dlogits = a->dlogits.ptr;
     v.c.check_results({{"dlogits", "logits"}});
     ewf_status st = v.end();
-    if (st == EWF_OK && !grad) plan_vocab(n, device_cu_count());
+    if (st == EWF_OK) plan_vocab(n, device_cu_count());
     return st;
 }
 
-// The parts of rows that several workgroups share, and the statistics of a loss whose gradient is a launch of its own and which
-// keeps none.
+// The parts of rows that several workgroups share, their largest logits, and what a gradient in a launch of its own needs.
 size_t vocab_workspace(VocabLaunch &n, void *workspace)
 {
     size_t bytes = 0;
@@ -590,11 +589,7 @@ size_t vocab_workspace(VocabLaunch &n, void *workspace)
     const size_t rows = n.r.rows, parts = rows * (size_t)n.splits;
     if (n.splits > 1 || n.top) n.parts = (float *)take(parts * 4 * sizeof(float));
     if (n.pieces_per_part) n.pieces = (float *)take(parts * (size_t)n.pieces_per_part * sizeof(float));
-    if (n.entries && n.dlogits && !n.held) {
-        const RowStride dense{(int64_t)n.r.n1, 1};
-        if (!n.peak) { n.peak = (float *)take(rows * sizeof(float)); n.speak = dense; }
-        if (!n.logsum) { n.logsum = (float *)take(rows * sizeof(float)); n.slogsum = dense; }
-    }
+    if (n.entries && n.dlogits && !n.held) n.prepared = take(rows * (kPreparedBytes + (size_t)n.entries * kPreparedEntryBytes));
     return bytes;
 }
 
@@ -658,11 +653,24 @@ ewf_status ewf_distill(const ewf_distill_args *a, void *workspace, size_t worksp
     });
 }
 
-ewf_status ewf_distill_grad(const ewf_distill_args *a, void *hip_stream)
+ewf_status ewf_distill_grad_workspace(const ewf_distill_args *a, size_t *workspace_bytes)
+{
+    return guarded([&]() -> ewf_status {
+        if (!workspace_bytes) { set_error("null argument"); return EWF_EINVAL; }
+        VocabLaunch n;
+        ewf_status st = distill_layout(a, true, n);
+        if (st == EWF_OK) *workspace_bytes = vocab_workspace(n, nullptr);
+        return st;
+    });
+}
+
+ewf_status ewf_distill_grad(const ewf_distill_args *a, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     return guarded([&]() -> ewf_status {
         VocabLaunch n;
         ewf_status st = distill_layout(a, true, n);
+        if (st != EWF_OK) return st;
+        st = workspace_fits(vocab_workspace(n, workspace), workspace, workspace_bytes);
         if (st != EWF_OK || n.r.rows == 0) return st;
         return launched("distillation, backward", [&] { launch_distill_grad(n, (hipStream_t)hip_stream); });
     });

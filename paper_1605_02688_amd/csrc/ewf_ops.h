@@ -82,6 +82,7 @@ struct VocabLaunch {
     float *parts;                        // [rows][splits][4]: peak, sums; null where rows are finished by the workgroup that sums them
 float *pieces;                       // [rows][splits][pieces_per_part]: the largest logits of a part's pieces
     int pieces_per_part;
+    void *prepared;                      // a loss whose gradient is a launch of its own: what that needs of each row, prepared_bytes
 };
 
 // ---- kernels' launchers (device translation units).  They launch on `stream` and report nothing: the caller asks the runtime.
@@ -92,6 +93,7 @@ void launch_layer_norm_grad(const NormLaunch &a, ihipStream_t *stream);
 void launch_activation(const ActLaunch &a, ihipStream_t *stream);
 void launch_activation_grad(const ActLaunch &a, ihipStream_t *stream);
 void launch_read8(const ActLaunch &a, ihipStream_t *stream);
+constexpr size_t kPreparedBytes = 32, kPreparedEntryBytes = 8;
 // Chooses the workgroups of launch_token_logprobs and launch_distill: fills threads, splits and held.
 void plan_vocab(VocabLaunch &a, int units);
 void launch_token_logprobs(const VocabLaunch &a, ihipStream_t *stream);

@@ -158,7 +158,8 @@ _sigs = {
     "ewf_token_logprobs_grad": (_i32, [ctypes.POINTER(ewf_token_logprobs_args), _vp]),
     "ewf_distill_workspace": (_i32, [ctypes.POINTER(ewf_distill_args), ctypes.POINTER(ctypes.c_size_t)]),
     "ewf_distill": (_i32, [ctypes.POINTER(ewf_distill_args), _vp, ctypes.c_size_t, _vp]),
-    "ewf_distill_grad": (_i32, [ctypes.POINTER(ewf_distill_args), _vp]),
+    "ewf_distill_grad_workspace": (_i32, [ctypes.POINTER(ewf_distill_args), ctypes.POINTER(ctypes.c_size_t)]),
+    "ewf_distill_grad": (_i32, [ctypes.POINTER(ewf_distill_args), _vp, ctypes.c_size_t, _vp]),
     "ewf_last_error": (ctypes.c_char_p, []),
     "ewf_debug_graph_count": (_i32, [_vp]),
     "ewf_debug_graph_node": (_i32, [_vp, _i32, ctypes.POINTER(ewf_node_info)]),
@@ -934,5 +935,5 @@ dlogits may lie over logits.""")
 distill = Operator("ewf_distill", _distill, True, """distill(logits, teacher_values, teacher_indices, loss, *, peak=None, logsum=None, tail=None,
 dloss=None, dlogits=None, scale=1.0, teacher_scale=1.0, workspace=None, stream=0): the loss against a teacher's top logits, or with tail against its
 top log probabilities and their remainder, and with dlogits the gradient for the weights dloss (absent: 1) in the same call.""")
-distill_grad = Operator("ewf_distill_grad", _distill_grad, False, """distill_grad(logits, teacher_values, teacher_indices, dlogits, *, peak, logsum,
-tail=None, dloss=None, scale=1.0, teacher_scale=1.0, stream=0): the gradient of distill's loss, from what it saved.""")
+distill_grad = Operator("ewf_distill_grad", _distill_grad, True, """distill_grad(logits, teacher_values, teacher_indices, dlogits, *, peak, logsum,
+tail=None, dloss=None, scale=1.0, teacher_scale=1.0, workspace=None, stream=0): the gradient of distill's loss, from what it saved.""")
