@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
 // take the next row's as soon as its gradients are written.  Between the two barriers of a row its sums are taken as its vectors arrive; the
 // next row's entries are read behind them.
 template <typename T, int N, int NV, bool STREAM>
-__global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
+__global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch a)
 {
     typedef typename T::raw raw;
     constexpr int V = Vec16<T>::V, W = N / 64, LINE = N > 64 ? kLine : 16;
@@ -176,30 +176,39 @@ __global__ void __launch_bounds__(N) k_distill_held(VocabLaunch a)
         }
         const Slope g(a, l, r, a.dloss ? a.dloss[at(row, a.sdloss)] : 1.f);
         if (reader) rank_entries<T>(lists[turn ^ 1], entries, a, ns, 0, ns.nvec, true);
+        float coef = g.coef, point = g.rest.k;
+        if (padding) {                                   // (whatever its logits are)
+            coef = point = 0.f;
+#pragma unroll
+            for (int u = 0; u < NV; u++) v[u] = u32x4{0u, 0u, 0u, 0u};
+        }
+        if (g.rest.as_is)                                // (the type's lowest or largest numbers: element by element, before the entries')
+            for (int c = s.head + tid; c < s.head + s.nvec * V; c += N) {
+                const float y = load1<T>(p + c);
+                float t;
+                g.rest.template of<1>(&y, &t);
+                t = g.coef * __builtin_amdgcn_exp2f(t);
+                for (int k = 0; k < a.entries; k++)
+                    if (l.index[k] == c) t = g.entry(l, k);
+                store1<T>(out + c, padding ? 0.f : t);
+            }
 #pragma unroll
         for (int u = 0; u < NV; u++) {
             const int j = u * N + tid;
-            if (j < s.nvec) {
-                float f[V], t[V];
+            if (j < s.nvec && !g.rest.as_is) {
+                float f[V];
 #pragma unroll
                 for (int e = 0; e < V; e++) f[e] = element<T>(v[u], e);
-                g.rest.template of<V>(f, t);
 #pragma unroll
-                for (int e = 0; e < V; e++) f[e] = g.coef * __builtin_amdgcn_exp2f(t[e]);
-                if (held >> u & 1)
-                    each_entry<V>(l, u, s.head, [&](int at, int k) {
-                        const float d = g.entry(l, k);
-#pragma unroll
-                        for (int e = 0; e < V; e++) f[e] = e == at ? d : f[e];
-                    });
-                if (padding)
-#pragma unroll
-                    for (int e = 0; e < V; e++) f[e] = 0.f;
+                for (int e = 0; e < V; e++) f[e] = coef * __builtin_amdgcn_exp2f(fmaf(f[e], a.c, -point));
                 store_vector<T>(out + s.head, u * N, tid, f);
             }
             if (more) fetch(v[u], np, ns, u);
             __builtin_amdgcn_sched_barrier(0);
         }
+        // the entries' gradients, each by the thread that wrote its vector (and after that: a thread's stores keep their order)
+        for (int k = g.rest.as_is ? -1 : l.head[tid]; k >= 0; k = l.next[k])
+            if (l.trip[k] >= 0) store1<T>(out + l.index[k], g.entry(l, k));
         if (tid < s.edges()) {
             float t;
             g.rest.template of<1>(&x, &t);
@@ -276,8 +285,9 @@ struct RunHeld {
         else if (n <= 512) go<T, 256, 2>();
         else if (n <= 1024) go<T, 256, 4>();
         else if (n <= 2048) go<T, 256, 8>();
-        else if (n <= 4096) go<T, 1024, 4>();
-        else if (n <= 8192) go<T, 1024, 8>();
+        else if (n <= 4096) go<T, 256, 16>();
+        else if (n <= 6144) go<T, 512, 12>();
+        else if (n <= 8192) go<T, 512, 16>();
         else if (n <= 12288) go<T, 1024, 12>();
         else go<T, 1024, 16>();
     }

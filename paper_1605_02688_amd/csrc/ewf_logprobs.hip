@@ -116,7 +116,7 @@ struct RunGrad {
 }  // namespace
 
 // Workgroups of a compute unit that hold rows of n vectors.
-static int held_workgroups(int n) { return n <= 256 ? 16 : n <= 2048 ? 4 : 1; }
+static int held_workgroups(int n) { return n <= 256 ? 16 : n <= 2048 ? 5 : n <= 4096 ? 4 : n <= 8192 ? 2 : 1; }
 
 void plan_vocab(VocabLaunch &a, int units)
 {

@@ -159,6 +159,7 @@ EWF_OPS_DEV bool beyond(float peak, float c) { return fabsf(peak) < kInf && !(fa
 struct Exponent {
     float c, k, ref, off, rest;
     bool as_is;
+    EWF_OPS_DEV Exponent() {}
     EWF_OPS_DEV Exponent(float ref, float off, float c) : c(c), ref(scalar(ref)), off(scalar(off))
     {
         const float a = rintf(ref * c), b = rintf(off);

@@ -198,9 +198,9 @@ EWF_OPS_DEV void finish_distill(const VocabLaunch &a, const Entries<N> &l, const
     }
 }
 
-EWF_OPS_DEV void padding_distill(const VocabLaunch &a, const RowAt &row)
+EWF_OPS_DEV void padding_distill(const VocabLaunch &a, const RowAt &row, int thread)
 {
-    if (threadIdx.x) return;
+    if (thread) return;
     if (a.loss) a.loss[at(row, a.sloss)] = 0.f;
     if (a.peak) a.peak[at(row, a.speak)] = 0.f;
     if (a.logsum) a.logsum[at(row, a.slogsum)] = 0.f;
@@ -211,6 +211,7 @@ EWF_OPS_DEV void padding_distill(const VocabLaunch &a, const RowAt &row)
 struct Slope {
     Exponent rest, p;
     float coef, mass, factor;
+    EWF_OPS_DEV Slope() {}
     template <int N>
     EWF_OPS_DEV Slope(const VocabLaunch &a, const Entries<N> &l, const Stats &r, float weight)
         : rest(ref(r), off(a, l, r) * kLog2E, a.c), p(ref(r), r.peak == -kInf ? 0.f : r.logsum * kLog2E, a.c)

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(N) k_rows(VocabLaunch a)
                 if (a.prepared) prepare_gradients(a, entries, row, r, prepared_row(a, t.part));
             }
         } else if (!parts) {
-            padding_distill(a, row);
+            padding_distill(a, row, tid);
             if (a.prepared && tid == 0) prepared_row(a, t.part)->padding = 1;
         }
         if (N > 64 || KIND != kLogprobs) __syncthreads();          // (LDS is the next item's)
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(N, TOP && N > 64 ? 8 : 1) k_join(VocabLaunch a
         if (tid < 64) take_entries<T>(entries, a, row, p, s, 0, 0, false);
         __syncthreads();
         if (entries.live == 0) {
-            padding_distill(a, row);
+            padding_distill(a, row, tid);
             if (a.prepared && tid == 0) prepared_row(a, blockIdx.x)->padding = 1;
             return;
         }
