@@ -2,8 +2,8 @@
 //
 // With c = scale log2 e a logit x stands for 2^(c x).  A thread adds e = 2^(c x - m), and for the entropy e (c x - m), about a whole number m that lags
 // behind: it moves only where a logit is 2^8 beyond it, so that moves are rare, exact, and e cannot overflow; c x - m is one multiply-add with one
-// rounding.  Threads' sums are moved to a common m and added in a fixed order, and come out about the row's largest logit.  Where c x itself leaves float32
-// (rows of the type's lowest or largest numbers) a row is swept again about its largest.
+// rounding.  Threads' sums are moved to a common m and added in a fixed order, and come out about the row's largest logit.  Where c x has no
+// fraction left or leaves float32 (logits beyond 2^22, rows of the type's lowest number) a row is swept again about its largest.
 #pragma once
 
 #include <algorithm>
@@ -152,10 +152,10 @@ EWF_OPS_DEV float max_of(const float *x)
 
 // A whole number of powers of two near a largest logit: what sums of a wavefront are brought to.
 EWF_OPS_DEV float point_of(float peak, float c) { return peak == -kInf ? 0.f : rintf(peak * c); }
-// Whether a row whose largest logit this is cannot be summed about such a point.
-EWF_OPS_DEV bool beyond(float peak, float c) { return fabsf(peak) < kInf && !(fabsf(peak * c) < 0x1p100f); }
+// Whether a row whose largest logit this is cannot be summed about such a point: whole numbers and c x have to keep their fractions.
+EWF_OPS_DEV bool beyond(float peak, float c) { return fabsf(peak) < kInf && !(fabsf(peak * c) < 0x1p22f); }
 
-// 2^(c (x - ref) - off) of logits x, one multiply-add each: as 2^rest 2^(c x - k), k a whole number.  Where c ref is no float32, as it is written.
+// 2^(c (x - ref) - off) of logits x, one multiply-add each: as 2^rest 2^(c x - k), k a whole number.  Rows beyond that (see above) as it is written.
 struct Exponent {
     float c, k, ref, off, rest;
     bool as_is;

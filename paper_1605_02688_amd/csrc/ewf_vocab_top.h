@@ -161,7 +161,7 @@ EWF_OPS_DEV int largest(TopLds<N> &l, const typename T::raw *row, const Span<T> 
         if (l.total >= k && l.upto <= kChosen && end_of(l.bin)) {
             bound = end_of(l.bin);
             const float floor = floor_of(bound);
-            each_piece([&](float x, int i) { if (x >= floor) l.chosen[atomicAdd(&l.nchosen, 1)] = i; });
+            each_piece([&](float x, int i) { if (x > -kInf && x >= floor) l.chosen[atomicAdd(&l.nchosen, 1)] = i; });        // (l.upto of them)
             if (tid < s.edges()) collect(edge, s.edge(tid));
             __syncthreads();
             // half a wavefront takes a piece

@@ -351,3 +351,239 @@ def test_strides_and_alignments(dtype):
             check_distilled(x, values, indices, True, dict(loss=loss, peak=peak, logsum=logsum, tail=tail), dx, 1.0, 1.0, gp)
             assert (room[:, :, :5 - off] == 77).all() and (room[:, :, 5 - off + cols:] == 77).all()
             assert first.shape == dx.shape
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("cols", (5, 300, 3000, 9001, 40000))
+def test_logits_of_any_size(dtype, cols):
+    dt, g = DT[dtype], gen(cols + 1)
+    sizes = (1e-6, 1e-2, 50.0, 3e3, 2e4) if dtype == "f16" else (1e-30, 1e-3, 50.0, 3e3, 1e5, 3e6, 1e9, 1e20, 1e37)
+    for scale in (1.0, 2.0 ** -20, 2.0 ** 20):
+        say("sizes", dtype, cols, scale)
+        x = torch.stack([torch.randn(cols, generator=g, device="cuda") * z + c * z for z in sizes for c in (0.0, 5.0, -5.0)]).to(dt)
+        rows = x.shape[0]
+        tokens = torch.randint(0, cols, (rows,), generator=g, device="cuda").to(torch.int32)
+        tokens[::2] = x[::2].float().argmax(1).to(torch.int32)
+        out = scored(x, tokens, scale, 3)
+        check_scored(x, tokens, out, scale, 3)
+        gp, ge = torch.randn(rows, generator=g, device="cuda"), torch.randn(rows, generator=g, device="cuda")
+        dx = torch.full_like(x, 77)
+        run(ewf.token_logprobs_grad, x, tokens, gp, dx, peak=out["peak"], logsum=out["logsum"], entropy=out["entropy"], dentropy=ge, scale=scale)
+        want, bound = ref.token_logprobs_grad(x, tokens, gp, ge, out["peak"], out["logsum"], out["entropy"], scale, dt)
+        # (a product that leaves the type is not what this is about)
+        fine = want.abs() < 0.5 * torch.finfo(dt).max
+        ref.close("dlogits", torch.where(fine, dx.double(), 0.0), torch.where(fine, want, 0.0), torch.where(fine, bound, 0.0))
+        k = min(cols, 4)
+        index = torch.topk(x.float(), k, 1).indices.to(torch.int32)
+        index[:, 0] = tokens
+        values = torch.log_softmax(torch.randn(rows, k, generator=g, device="cuda"), 1) - 0.5
+        for tail in (False, True):
+            for step in (True, False):
+                got, dx = distilled(x, values, index, tail, scale=scale, gradient=step)
+                if not step:
+                    dx = torch.full_like(x, 77)
+                    run(ewf.distill_grad, x, values, index, dx, peak=got["peak"], logsum=got["logsum"], tail=got.get("tail"), scale=scale)
+                want, bound = ref.distill_grad(x, values, index, got["peak"], got["logsum"], got.get("tail"), None, scale, 1.0, dt)
+                fine = want.abs() < 0.5 * torch.finfo(dt).max
+                ref.close("dlogits", torch.where(fine, dx.double(), 0.0), torch.where(fine, want, 0.0), torch.where(fine, bound, 0.0))
+                loss = ref.distill(x, values, index, scale, 1.0, tail)
+                for n, v in got.items():
+                    few = loss[n].abs() < 1e38
+                    ref.close(n, torch.where(few, v.double(), 0.0), torch.where(few, loss[n], 0.0), torch.where(few, loss["e_" + n], 0.0))
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
+def test_one_row_alone(dtype):
+    # rank 1: the rows' tensors have no axis
+    for cols in (100, 5000, 70000):
+        g = gen(cols)
+        x = logits_of(g, cols, dtype=DT[dtype])
+        token = torch.tensor(cols // 3, dtype=torch.int32, device="cuda")
+        logprob, peak, logsum = (torch.full((), 77.0, device="cuda") for _ in range(3))
+        tv, ti = torch.full((3,), 77.0, device="cuda"), torch.full((3,), 77, dtype=torch.int32, device="cuda")
+        run(ewf.token_logprobs, x, token, logprob, peak=peak, logsum=logsum, top_values=tv, top_indices=ti)
+        check_scored(x.view(1, -1), token.view(1), dict(logprob=logprob.view(1), peak=peak.view(1), logsum=logsum.view(1), top_values=tv.view(1, 3),
+                                                        top_indices=ti.view(1, 3)), 1.0, 3)
+        loss, dx = torch.full((), 77.0, device="cuda"), torch.empty_like(x)
+        run(ewf.distill, x, tv, ti, loss, peak=peak, logsum=logsum, dlogits=dx)
+        check_distilled(x.view(1, -1), tv.view(1, 3), ti.view(1, 3), False, dict(loss=loss.view(1), peak=peak.view(1), logsum=logsum.view(1)), dx.view(1, -1), 1.0,
+                        1.0, None)
+
+
+# ------------------------------------------------------------------ streams, graphs, several calls at once
+
+def vocab_calls(g):
+    """One bound call of every operator and form on tensors of its own: [(call, results)]."""
+    made = []
+
+    def bound(op, results, *args, **kw):
+        made.append((op.bind(*args, workspace=work_for(op, *args, **kw), **kw), results))
+
+    new = lambda *s, dtype=torch.float32: torch.empty(s, dtype=dtype, device="cuda")
+    for rows, cols, dt, k in ((300, 5001, torch.bfloat16, 7), (2, 300000, torch.float32, 20), (40, 700, torch.float16, 3), (5, 270000, torch.bfloat16, 64)):
+        x, tokens = logits_of(g, rows, cols, dtype=dt), tokens_of(g, rows, cols=cols)
+        logprob, peak, logsum, entropy, tv, ti = new(rows), new(rows), new(rows), new(rows), new(rows, k), new(rows, k, dtype=torch.int32)
+        bound(ewf.token_logprobs, (logprob, peak, logsum, entropy, tv, ti), x, tokens, logprob, peak=peak, logsum=logsum, entropy=entropy, top_values=tv,
+              top_indices=ti, scale=0.8)
+        dx = torch.empty_like(x)
+        bound(ewf.token_logprobs_grad, (dx,), x, tokens, torch.randn(rows, generator=g, device="cuda"), dx, peak=peak, logsum=logsum, entropy=entropy,
+              dentropy=torch.randn(rows, generator=g, device="cuda"), scale=0.8)
+        y = logits_of(g, rows, cols, dtype=dt)
+        loss, p2, l2, tail, dy, dz = new(rows), new(rows), new(rows), new(rows), torch.empty_like(y), torch.empty_like(y)
+        bound(ewf.distill, (loss, p2, l2, tail, dy), y, tv, ti, loss, peak=p2, logsum=l2, tail=tail, dlogits=dy)
+        bound(ewf.distill_grad, (dz,), y, tv, ti, dz, peak=p2, logsum=l2, tail=tail)
+        only = new(rows)
+        bound(ewf.distill, (only,), y, tv, ti, only)
+    return made
+
+
+def clear(calls):
+    for _, results in calls:
+        for r in results:
+            r.view(-1).view(torch.uint8).zero_()
+
+
+def same(a, b):
+    return torch.equal(a.view(-1).view(torch.uint8), b.view(-1).view(torch.uint8))
+
+
+def test_all_in_a_captured_graph():
+    calls = vocab_calls(gen(50))
+    for call, _ in calls:
+        call.launch(stream())
+    torch.cuda.synchronize()
+    eager = [[r.clone() for r in results] for _, results in calls]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            for call, _ in calls:
+                call.launch(side.cuda_stream)
+    torch.cuda.current_stream().wait_stream(side)
+    for replay in range(4):
+        clear(calls)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for (_, results), want in zip(calls, eager):
+            assert all(same(r, e) for r, e in zip(results, want)), replay
+        # eager work and the same operators between the replays, the workspaces left dirty
+        assert torch.isfinite(torch.randn(1 << 16, device="cuda").sum())
+        for call, _ in calls:
+            call.launch(stream())
+        torch.cuda.synchronize()
+
+
+def test_calls_on_several_streams_at_once():
+    sets = [vocab_calls(gen(60 + k)) for k in range(3)]
+    for calls in sets:
+        for call, _ in calls:
+            call.launch(stream())
+    torch.cuda.synchronize()
+    want = [[[r.clone() for r in results] for _, results in calls] for calls in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for calls in sets:
+        clear(calls)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, calls in zip(streams, sets):
+            for call, _ in calls:
+                call.launch(s.cuda_stream)
+    torch.cuda.synchronize()
+    for calls, w in zip(sets, want):
+        for (_, results), e in zip(calls, w):
+            assert all(same(r, x) for r, x in zip(results, e))
+
+
+def test_workspaces_of_the_wrong_size_are_refused():
+    x = torch.randn(1, 300000, device="cuda")
+    peak = torch.empty(1, device="cuda")
+    n = ewf.token_logprobs.workspace_bytes(x, peak=peak)
+    assert n > 16
+    with pytest.raises(ewf.EwfError) as e:
+        ewf.token_logprobs(x, peak=peak, workspace=torch.empty(n - 16, dtype=torch.uint8, device="cuda"), stream=stream())
+    assert e.value.status == ewf.ENOMEM
+
+
+# ------------------------------------------------------------------ all together
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+def test_a_student_learns_from_a_teacher(dtype):
+    """A teacher's pass writes its likeliest tokens, a student's step reads them: loss and gradient in one call, through the projection to the
+    hidden rows, and beside it an entropy term by the tokens' log probabilities; each step against the formulas, and the whole
+    gradient against differences of the objective in 64 bits."""
+    g = gen(80)
+    dt, B, T, H, V, k = DT[dtype], 3, 30, 24, 501, 16
+    hidden = torch.randn(B, T, H, generator=g, device="cuda")
+    wt, ws = (torch.randn(H, V, generator=g, device="cuda") * s for s in (0.9, 0.7))
+    teacher, student = (hidden @ wt).to(dt), (hidden @ ws).to(dt)
+    tokens = tokens_of(g, B, T, cols=V)
+    out = scored(teacher, tokens, 1.0, k)
+    check_scored(teacher, tokens, out, 1.0, k)
+    # rows of padding have no alternatives: no loss, no gradient
+    dloss = torch.rand(B, T, generator=g, device="cuda")
+    got, dx = distilled(student, out["top_values"], out["top_indices"], True, dloss=dloss)
+    check_distilled(student, out["top_values"], out["top_indices"], True, got, dx, 1.0, 1.0, dloss)
+    pad = (tokens < 0) | (tokens >= V)
+    assert pad.any() and (got["loss"][pad] == 0).all() and (dx[pad] == 0).all()
+    own = scored(student, tokens)
+    de = torch.randn(B, T, generator=g, device="cuda")
+    de_x = torch.empty_like(student)
+    run(ewf.token_logprobs_grad, student, tokens, None, de_x, peak=own["peak"], logsum=own["logsum"], entropy=own["entropy"], dentropy=de)
+    if dtype == "f32":
+        dw = hidden.reshape(-1, H).t().double() @ (dx + de_x).reshape(-1, V).double()
+        values, index = out["top_values"], out["top_indices"]
+
+        def objective(w):
+            x = (hidden.double() @ w).reshape(-1, V)
+            loss = ref.distill(x, values, index, 1.0, 1.0, True)["loss"]
+            return float((loss * dloss.reshape(-1)).sum() + (ref.token_logprobs(x, tokens, 1.0)["entropy"] * de.reshape(-1)).sum())
+
+        for _ in range(4):
+            step = torch.randn(H, V, generator=g, device="cuda", dtype=torch.float64)
+            h = 1e-5
+            slope = (objective(ws.double() + h * step) - objective(ws.double() - h * step)) / (2 * h)
+            # float32 logits are half a step off, as are their gradients: about 1e-6 of the products' sum of magnitudes
+            room = 1e-5 * float((dw.abs() * step.abs()).sum())
+            assert abs(slope - float((dw * step).sum())) < room, (slope, float((dw * step).sum()), room)
+
+
+# ------------------------------------------------------------------ beyond 2^31 elements
+
+def test_logits_of_more_than_2_31_elements():
+    rows, cols, bf = 17000, 131072, torch.bfloat16
+    g = gen(90)
+    x = torch.empty(rows, cols, dtype=bf, device="cuda")
+    for r in range(0, rows, 1000):
+        x[r:r + 1000] = torch.randn(min(1000, rows - r), cols, generator=g, device="cuda") * 3
+    tokens = tokens_of(g, rows, cols=cols)
+    say("more than 2^31", rows, cols)
+    out = scored(x, tokens, 1.0, 20)
+    parts = (slice(0, 3), slice(16383, 16387), slice(rows - 3, rows))
+    for part in parts:
+        check_scored(x[part], tokens[part], {n: t[part] for n, t in out.items()}, 1.0, 20)
+    gp = torch.randn(rows, generator=g, device="cuda")
+    dx = torch.empty_like(x)
+    run(ewf.token_logprobs_grad, x, tokens, gp, dx, peak=out["peak"], logsum=out["logsum"])
+    for part in parts:
+        want, bound = ref.token_logprobs_grad(x[part], tokens[part], gp[part], None, out["peak"][part], out["logsum"][part], None, 1.0, bf)
+        ref.close("dlogits", dx[part], want, bound)
+    values, index = out["top_values"], out["top_indices"]
+    got, _ = distilled(x, values, index, True, dloss=gp, into=dx)
+    for part in parts:
+        check_distilled(x[part], values[part], index[part], True, {n: t[part] for n, t in got.items()}, dx[part], 1.0, 1.0, gp[part])
+    run(ewf.distill_grad, x, values, index, x, peak=got["peak"], logsum=got["logsum"], tail=got["tail"], dloss=gp)
+    assert all(torch.equal(x[part].isnan(), dx[part].isnan()) and (x[part].double() - dx[part].double()).abs().max() < 1e-2 for part in parts)
+    del x, dx
+    torch.cuda.empty_cache()
+
+
+def test_a_row_of_the_longest():
+    cols = 1 << 24
+    g = gen(91)
+    x = logits_of(g, 2, cols, dtype=torch.bfloat16)
+    tokens = torch.tensor([cols - 1, 5], dtype=torch.int32, device="cuda")
+    out = scored(x, tokens, 1.0, 128)
+    check_scored(x, tokens, out, 1.0, 128)
+    got, dx = distilled(x, out["top_values"], out["top_indices"], True)
+    check_distilled(x, out["top_values"], out["top_indices"], True, got, dx, 1.0, 1.0, None)

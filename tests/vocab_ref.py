@@ -12,6 +12,8 @@ import torch
 from tests.operators_ref import U, close, stored  # noqa: F401
 
 INF = float("inf")
+NOTHING = 2.0 ** -125                    # the native exponential is zero below 2^-126; the rest of its exponent is at most one power of two
+MOST = 2.0 ** 128 - 2.0 ** 103          # the largest float32 and half a step
 
 
 def chain(cols):
@@ -24,6 +26,8 @@ def sound(out):
     """Bounds where there is a number to be near to: elsewhere results are what they are (an infinity, a NaN, the zeros of padding)."""
     for n in [n for n in out if n.startswith("e_")]:
         if n[2:] in out:
+            # (results are float32: what that does not reach is an infinity)
+            out[n[2:]] = torch.where(out[n[2:]].abs() > MOST, out[n[2:]].sign() * INF, out[n[2:]])
             out[n] = torch.where(torch.isfinite(out[n]) & torch.isfinite(out[n[2:]]), out[n], 0.0)
     return out
 
@@ -128,12 +132,12 @@ def token_logprobs_grad(x, tokens, dlogprob, dentropy, peak, logsum, entropy, sc
     if dlogprob is not None:
         g = dlogprob.unsqueeze(1)
         dx += g * (hot - p)
-        bound += g.abs() * (p * (rel + 6 * U) + 4 * U * hot)
+        bound += g.abs() * (p * (rel + 6 * U) + 4 * U * hot + NOTHING)
     if dentropy is not None:
         h, H = dentropy.unsqueeze(1), entropy.unsqueeze(1)
         lp = torch.where(p > 0, logp, 0.0)
         dx -= h * p * (lp + H)
-        bound += h.abs() * p * ((lp.abs() + H.abs()) * (rel + 8 * U) + rel)
+        bound += h.abs() * (p * ((lp.abs() + H.abs()) * (rel + 8 * U) + rel) + NOTHING * (130 + H.abs()))
     dx, bound = dx * scale, bound * scale
     dx = torch.where(pad.unsqueeze(1), 0.0, dx)
     bound = torch.where(pad.unsqueeze(1), 0.0, bound + 2 * U * dx.abs())
@@ -228,7 +232,7 @@ def distill_grad(x, values, indices, peak, logsum, tail, dloss, scale, teacher_s
     e_mass = (q * (e_q + 16 * U)).sum(1, keepdim=True) if tail is not None else 0.0
     if tail is None:
         dx = mass * p - hit
-        bound = p * mass * (rel + 6 * U) + e_hit
+        bound = p * mass * (rel + 6 * U) + e_hit + NOTHING
     else:
         tail = tail.reshape(-1).double()
         logpt = torch.where((tail == -INF) | (peak == -INF), -INF, tail - logsum)
@@ -243,7 +247,7 @@ def distill_grad(x, values, indices, peak, logsum, tail, dloss, scale, teacher_s
         rel_t = rel + 4 * U * (tail.abs().clamp_max(800.0) + logsum.abs().clamp_max(800.0)).nan_to_num(800.0, 800.0, 800.0).unsqueeze(1)
         # behind the entries: p / p_t (m p_t - q_t)
         inner = (mass * pt - rest).abs() * rel_t + mass * pt * (rel_t + 6 * U) + pt * (e_mass + e_r) + e_r + 2 * U * rest
-        bound = torch.where(free & counts, part * inner + 6 * U * part * (mass * pt + rest), p * (mass * (rel + 6 * U) + e_mass + e_r) + e_hit)
+        bound = torch.where(free & counts, part * inner + 6 * U * part * (mass * pt + rest), p * (mass * (rel + 6 * U) + e_mass + e_r) + e_hit) + NOTHING
     live = there.any(1, keepdim=True)
     dx = torch.where(live, dx * w, 0.0)
     bound = torch.where(live, bound * w.abs(), 0.0) + 4 * U * dx.abs()
