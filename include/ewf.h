@@ -381,7 +381,7 @@ ewf_status ewf_recurrence_grad(const ewf_recurrence_args *a, void *workspace, si
  * top_values, their log p.  scale is one over the temperature, 2^-64 .. 2^64.
  * tokens is int32, top_indices int32 [..., k], top_values float32 [..., k], the other results float32, each with the shape of logits
  * without its last axis; every result is optional, logprob comes with tokens.  Without tokens all rows count; with them a
- * row whose token is outside 0 .. cols - 1 is padding: its logits are not read, its results are 0, and it has no alternatives.
+ * row whose token is outside 0 .. cols - 1 is padding: what its logits hold has no effect, its results are 0, and it has no alternatives.
  * Alternatives that do not exist (logits of minus infinity, k > cols) have index -1 and value minus infinity.  In a row without any logit above
  * minus infinity peak, logsum and logprob are minus infinity and entropy is 0.  A row that holds a NaN or plus infinity has NaN in all its
  * results, and indices -1.  The lowest finite number is a logit like others.
@@ -412,7 +412,7 @@ ewf_status ewf_token_logprobs_grad(const ewf_token_logprobs_args *a, void *hip_s
  *     loss = sum_i q_i (log q_i - log p_(index i)) + q_t (log q_t - log p_t),
  *     dlogits_j = dloss scale (m p_j - sum of the q_i with index j, or where there is no such entry - q_t p_j / p_t),   m = q_t + sum q;
  * a tail with p_t < 2^-126 (nothing is left of the vocabulary, or masks) does not count: q_t is taken as 0.
- * Terms with q = 0 count 0.  A row without entries is padding, its logits are not read, results and gradients are 0; so are loss and gradient
+ * Terms with q = 0 count 0.  A row without entries is padding: what its logits hold has no effect, results and gradients are 0; so are loss and gradient
  * where all values are minus infinity and there is no tail.  A student's row without any logit above minus infinity has p = 0 and, where some
  * q > 0, an infinite loss.  A NaN or plus infinity among a row's logits, or among the values of entries that exist, makes its loss and gradient
  * NaN or infinite (logits: NaN).

@@ -7,7 +7,9 @@ namespace {
 
 constexpr int kGradThreads = 256, kGradVectors = 2;
 
-// One workgroup a piece of a row: dx_j = scale (g ([j = token] - p_j) - h p_j (log p_j + entropy)).
+// One workgroup a piece of a row, element-wise, so that memory bounds it: bfloat16 [4096, 50257] 128 us (6.4 TB/s; a copy of these bytes 126), float16
+// [750, 33279] 17.5.  Pieces of 8 KB: a copy takes 126 to 131 us with one to four vectors a thread, 192 with eight.
+//     dx_j = scale (g ([j = token] - p_j) - h p_j (log p_j + entropy))
 template <typename T, bool ENT, bool STREAM>
 __global__ void __launch_bounds__(kGradThreads) k_logprobs_grad(VocabLaunch a)
 {
@@ -115,14 +117,16 @@ struct RunGrad {
 
 }  // namespace
 
-// Workgroups of a compute unit that hold rows of n vectors.
+// Workgroups of a compute unit that hold rows of n vectors: as many as their registers (and below 256 vectors their LDS) leave room for.
 static int held_workgroups(int n) { return n <= 256 ? 16 : n <= 2048 ? 5 : n <= 4096 ? 4 : n <= 8192 ? 2 : 1; }
 
 void plan_vocab(VocabLaunch &a, int units)
 {
     const int n = vectors(a);
     a.held = a.entries && a.dlogits && a.loss && n <= kHeldVectors;
-    a.threads = n <= 256 ? 64 : 256;
+    // a wavefront a row where there are wavefronts for all compute units, bfloat16: [16384, 2048] 19.4 us, on 256 threads 40.9; [16384, 4096] 31.7 and 52.7;
+    // [8192, 12000] 39.2 and 43.7; but [4096, 32768] 50.5 and 45.8, [600, 16000] 9.4 and 8.2.  Alternatives of rows above 256 vectors need the 256 threads' pieces.
+    a.threads = n <= 256 || (!a.top && n <= 2048 && a.r.rows >= (uint32_t)(4 * units)) ? 64 : 256;
     // few rows are shared by workgroups that take 1024 vectors at least, where a second launch costs less than what it saves: one row of 131072 float32
     // takes 20 us whole, 7.7 in 32 parts; eight rows of 50257 bfloat16 8.1 us whole (and 8.1 in 6 parts), with 20 alternatives, which need the
     // second launch anyway, 17.3 and 12.2

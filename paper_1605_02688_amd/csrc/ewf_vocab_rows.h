@@ -91,7 +91,14 @@ EWF_OPS_DEV void sum_again(const VocabLaunch &a, const typename T::raw *p, const
     sum.w = group_sum<16>((tid & 15) < N / 64 ? lds[16 + (tid & 15)] : 0.f);
 }
 
-// A workgroup takes rows, or parts of rows (a.splits of each), one after the other, the next one's first vectors in flight while it finishes.  Where rows
+// A workgroup takes rows, or parts of rows (a.splits of each), one after the other; a vector's registers take the next vector as soon as it is summed, the
+// last ones the next row's first, which are in flight while this row is finished.
+//
+// Memory bounds it: bfloat16 [2048, 131072] 84 us (6.4 TB/s), [4096, 50257] 68 to 72 (6.0), float32 [1280, 10000] 11.1, with 7 vector instructions a logit of
+// which one is the exponential.  On the way (bfloat16 [4096, 50257]): a row a workgroup, sums about a logit 79.7; loads past the caches 75.7; the largest
+// of three by one instruction, and vectors taken in turn rather than copied from a second set, 71.7.  Six or eight vectors in flight: 68 and 70 there,
+// but float32 [1280, 10000] 11.6 and 12.1; half as many workgroups 73.1 and 13.6.  Rows that begin on cache lines: no change.
+// Where rows
 // have parts or alternatives are asked for it leaves sums and, TOP, the largest of their pieces in the workspace.
 template <typename T, int N, bool ENT, bool TOP, int KIND, bool STREAM>
 __global__ void __launch_bounds__(N) k_rows(VocabLaunch a)
@@ -260,7 +267,9 @@ __global__ void __launch_bounds__(N) k_rows(VocabLaunch a)
     }
 }
 
-// Joins the parts of a row.
+// Joins the parts of a row, and finds its alternatives: 2048 rows of 131072 bfloat16 with 64 of them in 23 to 27 us (84 MB of pieces' lines read again), one row in 6 to 8,
+// a chain of loads that wait for each other (parts, pieces, the chosen pieces, their vectors).  Within the first kernel the choice took 80 us more there than sums alone:
+// its registers leave one workgroup a compute unit, which loads nothing meanwhile.
 template <typename T, int N, bool TOP, int KIND>
 __global__ void __launch_bounds__(N, TOP && N > 64 ? 8 : 1) k_join(VocabLaunch a)
 {

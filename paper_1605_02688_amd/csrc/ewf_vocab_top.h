@@ -17,7 +17,8 @@ EWF_OPS_DEV uint32_t ordered(float x)
 EWF_OPS_DEV float unordered(uint32_t k) { return bits_to_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 EWF_OPS_DEV u64 key_of(float x, uint32_t at) { return x > -kInf ? (u64)ordered(x) << 32 | (uint32_t)~at : 0; }
 
-// The largest logits of pieces of a row: a piece is what kPieceLanes lanes (a cache line) take in kPieceTrips trips.
+// The largest logits of pieces of a row: a piece is what kPieceLanes lanes (a cache line) take in kPieceTrips trips.  Threads' own largest in
+// their place name vectors that lie in lines of their own, which brings nearly all of a row back: [2048, 131072] with 64 alternatives 190 us, 117 so.
 constexpr int kPieceLanes = 8, kPieceTrips = 4;
 constexpr int kCandidates = 512;         // logits that a row's last selection ranks
 constexpr int kBins = 1024, kBinShift = 16, kChosen = 320;
