@@ -46,10 +46,10 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
     }
     const float x = edge ? load1<T>(p + s.edge(tid)) : 0.f;
     const Prepared *prepared = prepared_row(a, in_launch);
-    const Prepared::Entry e = tid < a.entries ? prepared->entry[tid] : Prepared::Entry{-1, 0.f};
+    const bool padding = prepared->padding;              // (then nothing else is there)
+    const Prepared::Entry e = tid < a.entries && !padding ? prepared->entry[tid] : Prepared::Entry{-1, 0.f};
     const Exponent t = prepared->exponent(a.c);
     const float coef = prepared->coef;
-    const bool padding = prepared->padding;
     head[tid] = -1;
     __syncthreads();
     if (e.index >= 0) {

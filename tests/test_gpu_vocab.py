@@ -250,6 +250,33 @@ def test_distill(dtype, cols):
         assert torch.equal(y, alone)
 
 
+@pytest.mark.parametrize("fill", (0x00, 0x01, 0x7F, 0xFF))
+def test_whatever_a_workspace_holds(fill):
+    # rows of padding among others, in every form that has a workspace
+    g = gen(4)
+    for dtype, rows, cols in (("bf16", 9, 140003), ("f32", 6, 300001), ("f16", 2, 400000), ("bf16", 30, 9000)):
+        say("workspace", fill, dtype, rows, cols)
+        x = logits_of(g, rows, cols, dtype=DT[dtype])
+        values, index = entries_of(g, x, 20, True, ragged=True)
+        index[0] = -1
+        tokens = tokens_of(g, rows, cols=cols)
+        filled = lambda op, *args, **kw: torch.full((max(16, op.workspace_bytes(*args, **kw)),), fill, dtype=torch.uint8, device="cuda")
+        new = lambda *s, dtype=torch.float32: torch.full(s, 77, dtype=dtype, device="cuda")
+        out = dict(peak=new(rows), logsum=new(rows), tail=new(rows))
+        loss, dx, dy = new(rows), torch.full_like(x, 77), torch.full_like(x, 77)
+        args, kw = (x, values, index, loss), dict(dlogits=dx, **out)
+        ewf.distill(*args, workspace=filled(ewf.distill, *args, **kw), stream=stream(), **kw)
+        check_distilled(x, values, index, True, dict(loss=loss, **out), dx, 1.0, 1.0, None)
+        args, kw = (x, values, index, dy), out
+        ewf.distill_grad(*args, workspace=filled(ewf.distill_grad, *args, **kw), stream=stream(), **kw)
+        check_distilled(x, values, index, True, dict(loss=loss, **out), dy, 1.0, 1.0, None)
+        scores = dict(peak=new(rows), logsum=new(rows), entropy=new(rows), top_values=new(rows, 9), top_indices=new(rows, 9, dtype=torch.int32))
+        lp = new(rows)
+        args = (x, tokens, lp)
+        ewf.token_logprobs(*args, workspace=filled(ewf.token_logprobs, *args, **scores), stream=stream(), **scores)
+        check_scored(x, tokens, dict(logprob=lp, **scores), 1.0, 9)
+
+
 @pytest.mark.parametrize("dtype", sorted(DT))
 @pytest.mark.parametrize("cols", (9, 300, 5000, 20011, 150000))
 def test_an_index_that_comes_twice(dtype, cols):
