@@ -7,11 +7,11 @@ namespace {
 
 // One wavefront a row: what the gradients of a row need, from the statistics that the loss has saved.  4096 rows of 32 entries take 8 to 9 us; the kernel below would
 // have to do it for each piece of a row (102 us in place of 91 for both).
-template <typename T>
+template <typename T, int K>
 __global__ void __launch_bounds__(64) k_distill_prepare(VocabLaunch a)
 {
     typedef typename T::raw raw;
-    __shared__ Entries<64> l;
+    __shared__ Entries<64, K> l;
     const RowAt row = row_at(a.r, a.row0 + blockIdx.x);
     const raw *p = (const raw *)a.logits + at(row, a.slogits);
     const Stats r = {a.peak[at(row, a.speak)], a.logsum[at(row, a.slogsum)], a.with_tail ? a.tail[at(row, a.stail)] : 0.f};
@@ -100,14 +100,14 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
 // 232 us (4.6 TB/s; without any arithmetic 207, without the stores 143), float32 [1280, 50257] 105.  Tried there: the next row's sums begun amid this one's
 // gradients 267 (a wait for a load waits for the stores before it), loads before stores, entries ranked behind the gradients, plain loads or stores: no
 // gain.  Registers hold a row with nothing spilled only if logits are unpacked twice.
-template <typename T, int N, int NV, bool STREAM>
+template <typename T, int N, int NV, int K, bool STREAM>
 __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch a)
 {
     typedef typename T::raw raw;
     constexpr int V = Vec16<T>::V, W = N / 64, LINE = N > 64 ? kLine : 16;
     typedef Span<T, LINE> RowSpan;
     __shared__ float parts[2][2][16];
-    __shared__ Entries<N> lists[2];
+    __shared__ Entries<N, K> lists[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t i = blockIdx.x;
     RowAt row = row_at(a.r, a.row0 + i);
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch 
     x = tid < s.edges() ? load1<T>(p + s.edge(tid)) : -kInf;
     if (tid < 64) take_entries<T>(lists[0], a, row, p, s, 0, s.nvec, true);
     for (int turn = 0;; turn ^= 1) {
-        const Entries<N> &l = lists[turn];
+        const Entries<N, K> &l = lists[turn];
         __syncthreads();
         const bool padding = l.live == 0;
         const uint32_t held = trips_with_entries(l);
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch 
         const raw *np = (const raw *)a.logits + at(nrow, a.slogits);
         raw *nout = (raw *)a.dlogits + at(nrow, a.sdlogits);
         const RowSpan ns(nout, a.r.cols);
-        RawEntries entries;
+        RawEntries<K> entries;
         const bool reader = more && tid < 64;
         if (reader) read_entries(entries, a, nrow);
         Sums sum;
@@ -234,15 +234,20 @@ __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch 
 struct RunRows {
     const VocabLaunch &a;
     hipStream_t stream;
-    template <typename T, int N> void go() const
+    template <typename T, int N, int K> void go() const
     {
-        if (a.with_tail) run_rows<T, N, false, false, kDistillTail>(a, stream);
-        else run_rows<T, N, false, false, kDistill>(a, stream);
+        if (a.with_tail) run_rows<T, N, false, false, kDistillTail, K>(a, stream);
+        else run_rows<T, N, false, false, kDistill, K>(a, stream);
+    }
+    template <typename T, int K> void run() const
+    {
+        if (a.threads == 64) go<T, 64, K>();
+        else go<T, 256, K>();
     }
     template <typename T> void operator()() const
     {
-        if (a.threads == 64) go<T, 64>();
-        else go<T, 256>();
+        if (a.entries <= 64) run<T, 64>();
+        else run<T, kMaxTop>();
     }
 };
 
@@ -253,7 +258,8 @@ struct RunPrepare {
     {
         by_rows(a, 1, 64, [&](VocabLaunch b, dim3 grid, unsigned) {
             b.prepared = (char *)b.prepared + b.row0 * prepared_bytes(b.entries);
-            hipLaunchKernelGGL((k_distill_prepare<T>), grid, dim3(64), 0, stream, b);
+            if (b.entries <= 64) hipLaunchKernelGGL((k_distill_prepare<T, 64>), grid, dim3(64), 0, stream, b);
+            else hipLaunchKernelGGL((k_distill_prepare<T, kMaxTop>), grid, dim3(64), 0, stream, b);
         });
     }
 };
@@ -275,28 +281,36 @@ struct RunGrad {
 struct RunHeld {
     const VocabLaunch &a;
     hipStream_t stream;
-    template <typename T, int N, int NV> void go() const
+    template <typename T, int N, int NV, int K> void go() const
     {
         by_rows(a, 1, N, [&](const VocabLaunch &b, dim3 grid, unsigned) {
             grid.x = std::min(grid.x, (unsigned)b.resident);
-            if (N > 64 && b.stream) hipLaunchKernelGGL((k_distill_held<T, N, NV, (N > 64)>), grid, dim3(N), 0, stream, b);
-            else hipLaunchKernelGGL((k_distill_held<T, N, NV, false>), grid, dim3(N), 0, stream, b);
+            if (N > 64 && b.stream) hipLaunchKernelGGL((k_distill_held<T, N, NV, K, (N > 64)>), grid, dim3(N), 0, stream, b);
+            else hipLaunchKernelGGL((k_distill_held<T, N, NV, K, false>), grid, dim3(N), 0, stream, b);
         });
+    }
+    template <typename T, int K> void run() const
+    {
+        const int n = vectors(a);
+        if (a.threads == 64) {
+            if (n <= 64) go<T, 64, 1, K>();
+            else if (n <= 128) go<T, 64, 2, K>();
+            else if (n <= 256) go<T, 64, 4, K>();
+            else if (n <= 512) go<T, 64, 8, K>();
+            else go<T, 64, 16, K>();
+        } else if (n <= 512) go<T, 256, 2, K>();
+        else if (n <= 1024) go<T, 256, 4, K>();
+        else if (n <= 2048) go<T, 256, 8, K>();
+        else if (n <= 4096) go<T, 256, 16, K>();
+        else if (n <= 6144) go<T, 512, 12, K>();
+        else if (n <= 8192) go<T, 512, 16, K>();
+        else if (n <= 12288) go<T, 1024, 12, K>();
+        else go<T, 1024, 16, K>();
     }
     template <typename T> void operator()() const
     {
-        const int n = vectors(a);
-        if (n <= 64) go<T, 64, 1>();
-        else if (n <= 128) go<T, 64, 2>();
-        else if (n <= 256) go<T, 64, 4>();
-        else if (n <= 512) go<T, 256, 2>();
-        else if (n <= 1024) go<T, 256, 4>();
-        else if (n <= 2048) go<T, 256, 8>();
-        else if (n <= 4096) go<T, 256, 16>();
-        else if (n <= 6144) go<T, 512, 12>();
-        else if (n <= 8192) go<T, 512, 16>();
-        else if (n <= 12288) go<T, 1024, 12>();
-        else go<T, 1024, 16>();
+        if (a.entries <= 64) run<T, 64>();
+        else run<T, kMaxTop>();
     }
 };
 

@@ -117,8 +117,12 @@ struct RunGrad {
 
 }  // namespace
 
-// Workgroups of a compute unit that hold rows of n vectors: as many as their registers (and below 256 vectors their LDS) leave room for.
-static int held_workgroups(int n) { return n <= 256 ? 16 : n <= 2048 ? 5 : n <= 4096 ? 4 : n <= 8192 ? 2 : 1; }
+// Workgroups of a compute unit that hold rows of n vectors: as many as their registers (and for one wavefront's up to 256 vectors their LDS) leave room for.
+static int held_workgroups(int threads, int n, int entries)
+{
+    if (threads == 64) return n <= 256 && entries <= 64 ? 32 : 16;
+    return n <= 2048 ? 5 : n <= 4096 ? 4 : n <= 8192 ? 2 : 1;
+}
 
 void plan_vocab(VocabLaunch &a, int units)
 {
@@ -131,12 +135,16 @@ void plan_vocab(VocabLaunch &a, int units)
     // takes 20 us whole, 7.7 in 32 parts; eight rows of 50257 bfloat16 8.1 us whole (and 8.1 in 6 parts), with 20 alternatives, which need the
     // second launch anyway, 17.3 and 12.2
     a.splits = 1;
+    // a wavefront holds a row where each SIMD has more than one (bfloat16, 20 entries: [2048, 2000] 12.7 us, [1500, 2000] 12.1, on 256 threads 12.8 and 14.4; but
+    // [1024, 2000] 11.4 and 9.8, [64, 2000] 9.9 and 7.5), a long one two: [8192, 4000] 38 and 55, [8192, 7000] 62 and 73, [2048, 4000] 16.8 and 18.3,
+    // [2048, 7000] 22.1 and 22.2, but [1024, 4000] 14.5 and 10.9
+    if (a.held) a.threads = n <= 64 || (n <= 256 && a.r.rows > (uint32_t)(4 * units)) || (n <= 1024 && a.r.rows >= (uint32_t)(8 * units)) ? 64 : 256;
     if (a.r.rows < (uint32_t)units && n >= (a.top ? 2048 : 12288) && !a.held && (a.loss || !a.dlogits))
         a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, n / 1024), (2 * units + a.r.rows - 1) / a.r.rows));
     // (the largest a row can have: its vectors begin at its first whole 16 bytes)
     if (a.top && a.threads == 256) a.pieces_per_part = ((n + a.splits - 1) / a.splits + kPieceTrips * 256 - 1) / (kPieceTrips * 256) * (256 / kPieceLanes);
     // workgroups that stay: as many as share the rows evenly
-    const int64_t room = (int64_t)units * (a.held ? held_workgroups(n) : 2048 / a.threads), items = (int64_t)a.r.rows * a.splits, each = (items + room - 1) / room;
+    const int64_t room = (int64_t)units * (a.held ? held_workgroups(a.threads, n, a.entries) : 2048 / a.threads), items = (int64_t)a.r.rows * a.splits, each = (items + room - 1) / room;
     a.resident = each ? (int)((items + each - 1) / each) : 0;
     // logits that the memory-side cache cannot keep pass it by: bfloat16 [4096, 32768] 51.7 us, passing 45.6; [2048, 32768] 27.2 and 24.7; [1024, 32768] 14.3 and 15.7
     a.stream = (int64_t)a.r.rows * a.r.cols * (a.dtype == EWF_F32 ? 4 : 2) >= (int64_t)128 << 20;

@@ -10,13 +10,14 @@ namespace ewf {
 namespace {
 
 // The entries of a row in LDS.  An entry inside the row's vectors is in the list of the thread that takes its vector (thread = vector mod N),
-// one on an edge in the list of that edge's thread, with no trip.
-template <int N>
+// one on an edge in the list of that edge's thread, with no trip.  K, 64 or 128, is what a row can have: with 64 of them a lane has one, and LDS lets more
+// workgroups share a compute unit (bfloat16 [16384, 1000], 20 entries: 36 us, with room for 128 always 39).
+template <int N, int K>
 struct Entries {
     int head[N];                                        // last entry of each thread's list, -1
-    int next[kMaxTop], index[kMaxTop], trip[kMaxTop];
-    float q[kMaxTop], logq[kMaxTop], logit[kMaxTop];
-    float all[kMaxTop];                                 // of all entries with the same index
+    int next[K], index[K], trip[K];
+    float q[K], logq[K], logit[K];
+    float all[K];                                       // of all entries with the same index
     int edge[kEdges];                                   // an entry on each edge element, -1
     float tail_q, total_q;                              // 1 - sum q; sum q
     float peak, sum;                                    // of the logits that they name: the largest, the sum about it
@@ -33,58 +34,70 @@ EWF_OPS_DEV float load_teacher(const VocabLaunch &a, int64_t at)
 // LDS that one wavefront writes and reads itself.
 EWF_OPS_DEV void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
-// A wavefront reads a row's entries, two a lane: indices and values, then the logits that they name ...
-struct RawEntries { int c[2]; float v[2], x[2]; };
+// A wavefront reads a row's entries, one or two a lane: indices and values, then the logits that they name ...
+template <int K>
+struct RawEntries { int c[K / 64]; float v[K / 64], x[K / 64]; };
 
-EWF_OPS_DEV void read_entries(RawEntries &r, const VocabLaunch &a, const RowAt &row)
+template <int K>
+EWF_OPS_DEV void read_entries(RawEntries<K> &r, const VocabLaunch &a, const RowAt &row)
 {
     const int64_t values = at(row, a.steacher_values), indices = at(row, a.steacher_indices);
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int h = 0; h < K / 64; h++) {
         const int i = h * 64 + (threadIdx.x & 63);
         r.c[h] = i < a.entries ? a.teacher_indices[indices + i] : -1;
         r.v[h] = i < a.entries ? load_teacher(a, values + i) : 0.f;
     }
 }
 
-template <typename T>
-EWF_OPS_DEV void read_logits(RawEntries &r, const VocabLaunch &a, const typename T::raw *logits)
+template <typename T, int K>
+EWF_OPS_DEV void read_logits(RawEntries<K> &r, const VocabLaunch &a, const typename T::raw *logits)
 {
 #pragma unroll
-    for (int h = 0; h < 2; h++) r.x[h] = (uint32_t)r.c[h] < (uint32_t)a.r.cols ? load1<T>(logits + r.c[h]) : 0.f;
+    for (int h = 0; h < K / 64; h++) r.x[h] = (uint32_t)r.c[h] < (uint32_t)a.r.cols ? load1<T>(logits + r.c[h]) : 0.f;
+}
+
+// q = e^(v - m), their sum
+template <int H>
+EWF_OPS_DEV float exponentials(const float *v, float m, float *q)
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < H; h++) sum += q[h] = expf(v[h] - m);
+    return sum;
 }
 
 // ... and ranks them; the others see them behind a barrier.  The vectors of this workgroup are j0 .. j1 - 1 (thread (j - j0) mod N takes vector j);
 // `edges`: and the edges.
-template <typename T, int N, typename S>
-EWF_OPS_DEV void rank_entries(Entries<N> &l, const RawEntries &r, const VocabLaunch &a, const S &s, int j0, int j1, bool edges)
+template <typename T, int N, int K, typename S>
+EWF_OPS_DEV void rank_entries(Entries<N, K> &l, const RawEntries<K> &r, const VocabLaunch &a, const S &s, int j0, int j1, bool edges)
 {
     constexpr int V = Vec16<T>::V;
+    constexpr int H = K / 64;
     const int lane = threadIdx.x & 63;
     const int *c = r.c;
     const float *x = r.x;
-    float v[2];
-    bool live[2];
+    float v[H];
+    bool live[H];
+    int some = 0;
     for (int i = lane; i < N; i += 64) l.head[i] = -1;
     for (int i = lane; i < kEdges; i += 64) l.edge[i] = -1;
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int h = 0; h < H; h++) {
         live[h] = (uint32_t)c[h] < (uint32_t)s.cols;
         v[h] = live[h] ? r.v[h] * a.teacher_scale : -kInf;
+        some += __popcll(__ballot(live[h]));
     }
-    const int some = __popcll(__ballot(live[0])) + __popcll(__ballot(live[1]));
-    float q[2], tail = 0.f, total;
+    float q[H], tail = 0.f, total;
     if (a.with_tail) {
-        q[0] = expf(v[0]); q[1] = expf(v[1]);
-        total = group_sum<64>(q[0] + q[1]);
+        total = group_sum<64>(exponentials<H>(v, 0.f, q));
         tail = fmaxf(1.f - total, 0.f);
         if (!(total < kInf)) tail = total - total;      // (a NaN stays one)
     } else {
-        const float top = wave_max(fmaxf(v[0], v[1])), m = top == -kInf ? 0.f : top;
-        q[0] = expf(v[0] - m); q[1] = expf(v[1] - m);
-        const float sum = group_sum<64>(q[0] + q[1]), log_sum = logf(sum);
+        const float top = wave_max(fmaxf(v[0], v[H - 1])), m = top == -kInf ? 0.f : top;
+        const float sum = group_sum<64>(exponentials<H>(v, m, q)), log_sum = logf(sum);
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
+        for (int h = 0; h < H; h++) {
             q[h] = sum == 0.f ? 0.f : q[h] / sum;
             v[h] = v[h] - m - log_sum;
         }
@@ -92,9 +105,9 @@ EWF_OPS_DEV void rank_entries(Entries<N> &l, const RawEntries &r, const VocabLau
     }
     if (lane == 0) { l.tail_q = tail; l.total_q = total; l.live = some; }
     wave_fence();
-    int owner[2];
+    int owner[H];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int h = 0; h < H; h++) {
         const int i = h * 64 + lane;
         l.index[i] = live[h] ? c[h] : -1;
         l.q[i] = live[h] ? q[h] : 0.f;
@@ -117,9 +130,9 @@ EWF_OPS_DEV void rank_entries(Entries<N> &l, const RawEntries &r, const VocabLau
     }
     wave_fence();
     // entries of the same index are in the same list; their probabilities are added in the entries' order
-    bool first[2];
+    bool first[H];
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int h = 0; h < H; h++) {
         const int i = h * 64 + lane;
         bool again = false;
         first[h] = live[h];
@@ -135,18 +148,18 @@ EWF_OPS_DEV void rank_entries(Entries<N> &l, const RawEntries &r, const VocabLau
         }
         l.all[i] = all;
     }
-    const float peak = wave_max(fmaxf(first[0] ? x[0] : -kInf, first[1] ? x[1] : -kInf)), ref = peak == -kInf ? 0.f : peak;
+    const float peak = wave_max(fmaxf(first[0] ? x[0] : -kInf, first[H - 1] ? x[H - 1] : -kInf)), ref = peak == -kInf ? 0.f : peak;
     float e = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; h++) e += first[h] ? __builtin_amdgcn_exp2f((x[h] - ref) * a.c) : 0.f;
+    for (int h = 0; h < H; h++) e += first[h] ? __builtin_amdgcn_exp2f((x[h] - ref) * a.c) : 0.f;
     e = group_sum<64>(e);
     if (lane == 0) { l.peak = peak; l.sum = e; }
 }
 
-template <typename T, int N, typename S>
-EWF_OPS_DEV void take_entries(Entries<N> &l, const VocabLaunch &a, const RowAt &row, const typename T::raw *logits, const S &s, int j0, int j1, bool edges)
+template <typename T, int N, int K, typename S>
+EWF_OPS_DEV void take_entries(Entries<N, K> &l, const VocabLaunch &a, const RowAt &row, const typename T::raw *logits, const S &s, int j0, int j1, bool edges)
 {
-    RawEntries r;
+    RawEntries<K> r;
     read_entries(r, a, row);
     read_logits<T>(r, a, logits);
     rank_entries<T>(l, r, a, s, j0, j1, edges);
@@ -157,8 +170,8 @@ EWF_OPS_DEV bool tail_counts(float tail, float logsum) { return tail - logsum >=
 // A row's statistics from its sums: of all logits, or with a tail of those that no entry names.
 struct Stats { float peak, logsum, tail; };
 
-template <int N>
-EWF_OPS_DEV Stats stats_of(const VocabLaunch &a, const Entries<N> &l, const Sums &sum)
+template <int N, int K>
+EWF_OPS_DEV Stats stats_of(const VocabLaunch &a, const Entries<N, K> &l, const Sums &sum)
 {
     Stats r = {sum.peak, 0.f, -kInf};
     float total = sum.s;
@@ -175,14 +188,14 @@ EWF_OPS_DEV Stats stats_of(const VocabLaunch &a, const Entries<N> &l, const Sums
 }
 
 // Writes the loss and the statistics: one wavefront.
-template <int N>
-EWF_OPS_DEV void finish_distill(const VocabLaunch &a, const Entries<N> &l, const RowAt &row, const Stats &r)
+template <int N, int K>
+EWF_OPS_DEV void finish_distill(const VocabLaunch &a, const Entries<N, K> &l, const RowAt &row, const Stats &r)
 {
     const int lane = threadIdx.x & 63;
     const bool none = r.logsum == -kInf;
     float loss = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int h = 0; h < K / 64; h++) {
         const int i = h * 64 + lane;
         const float q = l.q[i], logp = none ? -kInf : fmaf(l.logit[i] - r.peak, a.scale, -r.logsum);
         if (l.index[i] >= 0 && q != 0.f) loss += q * (l.logq[i] - logp);
@@ -212,8 +225,8 @@ struct Slope {
     Exponent rest, p;
     float coef, mass, factor;
     EWF_OPS_DEV Slope() {}
-    template <int N>
-    EWF_OPS_DEV Slope(const VocabLaunch &a, const Entries<N> &l, const Stats &r, float weight)
+    template <int N, int K>
+    EWF_OPS_DEV Slope(const VocabLaunch &a, const Entries<N, K> &l, const Stats &r, float weight)
         : rest(ref(r), off(a, l, r) * kLog2E, a.c), p(ref(r), r.peak == -kInf ? 0.f : r.logsum * kLog2E, a.c)
     {
         factor = scalar(weight * a.scale);
@@ -226,8 +239,8 @@ struct Slope {
         }
         coef = scalar(r.peak == -kInf ? 0.f : coef * __builtin_amdgcn_exp2f(rest.rest));        // (a student without a logit: p = 0)
     }
-    template <int N>
-    EWF_OPS_DEV float entry(const Entries<N> &l, int k) const
+    template <int N, int K>
+    EWF_OPS_DEV float entry(const Entries<N, K> &l, int k) const
     {
         float t;
         p.of<1>(&l.logit[k], &t);
@@ -235,13 +248,13 @@ struct Slope {
     }
 private:
     static EWF_OPS_DEV float ref(const Stats &r) { return r.peak == -kInf ? 0.f : r.peak; }
-    template <int N>
-    static EWF_OPS_DEV bool with_rest(const VocabLaunch &a, const Entries<N> &l, const Stats &r)
+    template <int N, int K>
+    static EWF_OPS_DEV bool with_rest(const VocabLaunch &a, const Entries<N, K> &l, const Stats &r)
     {
         return a.with_tail && tail_counts(r.tail, r.logsum) && l.tail_q > 0.f;
     }
-    template <int N>
-    static EWF_OPS_DEV float off(const VocabLaunch &a, const Entries<N> &l, const Stats &r)
+    template <int N, int K>
+    static EWF_OPS_DEV float off(const VocabLaunch &a, const Entries<N, K> &l, const Stats &r)
     {
         return r.peak == -kInf ? 0.f : with_rest(a, l, r) ? r.tail : r.logsum;
     }
@@ -261,8 +274,8 @@ inline __host__ __device__ size_t prepared_bytes(int entries) { return kPrepared
 EWF_OPS_DEV Prepared *prepared_row(const VocabLaunch &a, uint32_t in_launch) { return (Prepared *)((char *)a.prepared + in_launch * prepared_bytes(a.entries)); }
 
 // One wavefront; the same gradient stands at each entry of an index.
-template <int N>
-EWF_OPS_DEV void prepare_gradients(const VocabLaunch &a, const Entries<N> &l, const RowAt &row, const Stats &r, Prepared *to)
+template <int N, int K>
+EWF_OPS_DEV void prepare_gradients(const VocabLaunch &a, const Entries<N, K> &l, const RowAt &row, const Stats &r, Prepared *to)
 {
     const Slope g(a, l, r, a.dloss ? a.dloss[at(row, a.sdloss)] : 1.f);
     const int lane = threadIdx.x & 63;
@@ -276,8 +289,8 @@ EWF_OPS_DEV void prepare_gradients(const VocabLaunch &a, const Entries<N> &l, co
 }
 
 // The trips of this thread that hold entries, as bits.
-template <int N>
-EWF_OPS_DEV uint32_t trips_with_entries(const Entries<N> &l)
+template <int N, int K>
+EWF_OPS_DEV uint32_t trips_with_entries(const Entries<N, K> &l)
 {
     uint32_t m = 0;
     for (int k = l.head[threadIdx.x]; k >= 0; k = l.next[k])
@@ -286,8 +299,8 @@ EWF_OPS_DEV uint32_t trips_with_entries(const Entries<N> &l)
 }
 
 // Calls to(e, k) for the elements e of this thread's vector of a trip that entries k name.
-template <int V, int N, typename F>
-EWF_OPS_DEV void each_entry(const Entries<N> &l, int trip, int head, F &&to)
+template <int V, int N, int K, typename F>
+EWF_OPS_DEV void each_entry(const Entries<N, K> &l, int trip, int head, F &&to)
 {
     for (int k = l.head[threadIdx.x]; k >= 0; k = l.next[k])
         if (l.trip[k] == trip) to((l.index[k] - head) % V, k);

@@ -100,13 +100,13 @@ EWF_OPS_DEV void sum_again(const VocabLaunch &a, const typename T::raw *p, const
 // but float32 [1280, 10000] 11.6 and 12.1; half as many workgroups 73.1 and 13.6.  Rows that begin on cache lines: no change.
 // Where rows
 // have parts or alternatives are asked for it leaves sums and, TOP, the largest of their pieces in the workspace.
-template <typename T, int N, bool ENT, bool TOP, int KIND, bool STREAM>
+template <typename T, int N, bool ENT, bool TOP, int KIND, int K, bool STREAM>
 __global__ void __launch_bounds__(N) k_rows(VocabLaunch a)
 {
     typedef typename T::raw raw;
     constexpr int V = Vec16<T>::V, U = kPieceTrips;
     __shared__ float sums[48];
-    __shared__ typename std::conditional<KIND != kLogprobs, Entries<N>, int>::type entries;
+    __shared__ typename std::conditional<KIND != kLogprobs, Entries<N, K>, int>::type entries;
     const int tid = threadIdx.x;
     const bool parts = a.parts != nullptr;
     const uint32_t splits = (uint32_t)a.splits, items = a.rows * splits;
@@ -270,11 +270,11 @@ __global__ void __launch_bounds__(N) k_rows(VocabLaunch a)
 // Joins the parts of a row, and finds its alternatives: 2048 rows of 131072 bfloat16 with 64 of them in 23 to 27 us (84 MB of pieces' lines read again), one row in 6 to 8,
 // a chain of loads that wait for each other (parts, pieces, the chosen pieces, their vectors).  Within the first kernel the choice took 80 us more there than sums alone:
 // its registers leave one workgroup a compute unit, which loads nothing meanwhile.
-template <typename T, int N, bool TOP, int KIND>
+template <typename T, int N, bool TOP, int KIND, int K>
 __global__ void __launch_bounds__(N, TOP && N > 64 ? 8 : 1) k_join(VocabLaunch a)
 {
     typedef typename T::raw raw;
-    __shared__ typename std::conditional<KIND != kLogprobs, Entries<N>, int>::type entries;
+    __shared__ typename std::conditional<KIND != kLogprobs, Entries<N, K>, int>::type entries;
     __shared__ typename std::conditional<TOP, TopLds<N>, int>::type top;
     const RowAt row = row_at(a.r, a.row0 + blockIdx.x);
     const raw *p = (const raw *)a.logits + at(row, a.slogits);
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(N, TOP && N > 64 ? 8 : 1) k_join(VocabLaunch a
     }
 }
 
-template <typename T, int N, bool ENT, bool TOP, int KIND>
+template <typename T, int N, bool ENT, bool TOP, int KIND, int K = 0>
 void run_rows(const VocabLaunch &a, hipStream_t stream)
 {
     constexpr bool kLong = N > 64;
@@ -336,10 +336,10 @@ void run_rows(const VocabLaunch &a, hipStream_t stream)
         if (b.pieces) b.pieces += (int64_t)b.row0 * b.splits * b.pieces_per_part;
         if (b.prepared) b.prepared = (char *)b.prepared + b.row0 * prepared_bytes(b.entries);
         grid.x = std::min(grid.x, (unsigned)b.resident);
-        if (kLong && b.stream) hipLaunchKernelGGL((k_rows<T, N, ENT, TOP && kLong, KIND, kLong>), grid, dim3(N), 0, stream, b);
-        else hipLaunchKernelGGL((k_rows<T, N, ENT, TOP && kLong, KIND, false>), grid, dim3(N), 0, stream, b);
+        if (kLong && b.stream) hipLaunchKernelGGL((k_rows<T, N, ENT, TOP && kLong, KIND, K, kLong>), grid, dim3(N), 0, stream, b);
+        else hipLaunchKernelGGL((k_rows<T, N, ENT, TOP && kLong, KIND, K, false>), grid, dim3(N), 0, stream, b);
         constexpr int J = TOP && kLong ? 256 : 64;
-        if (b.parts) hipLaunchKernelGGL((k_join<T, J, TOP, KIND>), dim3(rows), dim3(J), 0, stream, b);
+        if (b.parts) hipLaunchKernelGGL((k_join<T, J, TOP, KIND, K>), dim3(rows), dim3(J), 0, stream, b);
     });
 }
 

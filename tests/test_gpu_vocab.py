@@ -278,6 +278,41 @@ def test_whatever_a_workspace_holds(fill):
 
 
 @pytest.mark.parametrize("dtype", sorted(DT))
+@pytest.mark.parametrize("rows,vectors", ((9001, 50), (9001, 101), (2200, 250), (9001, 251), (5003, 501), (4500, 1019)))
+def test_more_rows_than_wavefronts_hold_at_once(dtype, rows, vectors):
+    # each kind of row in turn with the others: masked, padded, huge, not finite, named twice
+    dt = DT[dtype]
+    cols = vectors * 16 // dt.itemsize + 3
+    for k, tail in ((20, True), (100, True), (64, False)):
+        say("many", dtype, rows, cols, k, tail)
+        g = gen(rows + cols + k)
+        x = logits_of(g, rows, cols, dtype=dt)
+        values, index = entries_of(g, x, k, tail, ragged=True)
+        twice = torch.arange(rows, device="cuda") % 5 == 1
+        index[twice, 3:7] = index[twice, 2:3]
+        values[twice] -= 3.0
+        x[2::7, : cols // 2] = -math.inf
+        x[4::31, cols // 3] = math.nan
+        x[6::41] = -math.inf
+        x[8::37] *= 2000.0 if dtype == "f16" else 3e6
+        dloss = torch.randn(rows, generator=g, device="cuda")
+        out, dx = distilled(x, values, index, tail, dloss=dloss)
+        # what the oracle does not have: a student's or a teacher's NaN, a student without a logit
+        there = (index >= 0) & (index < cols)
+        live, none = there.any(1), (x == -math.inf).all(1)
+        nan = live & (torch.isnan(x).any(1) | ((there & torch.isnan(values)).any(1) & ~none))
+        assert torch.isnan(out["loss"][nan]).all() and torch.isnan(dx[nan]).all()
+        named = torch.zeros((rows, cols + 1), dtype=torch.bool, device="cuda").scatter_(1, torch.where(there, index, cols).long(), True)[:, :cols]
+        assert (dx[none & live][~named[none & live]] == 0).all()
+        assert ((out["loss"] == math.inf) | torch.isnan(out["loss"]))[none & live].all()
+        fine = ~nan & ~(none & live)
+        check_distilled(x[fine], values[fine], index[fine], tail, {n: t[fine] for n, t in out.items()}, dx[fine], 1.0, 1.0, dloss[fine])
+        y = x.clone()
+        again, _ = distilled(y, values, index, tail, dloss=dloss, into=y)
+        assert torch.equal(torch.nan_to_num(y), torch.nan_to_num(dx)) and torch.equal(torch.nan_to_num(again["loss"]), torch.nan_to_num(out["loss"]))
+
+
+@pytest.mark.parametrize("dtype", sorted(DT))
 @pytest.mark.parametrize("cols", (9, 300, 5000, 20011, 150000))
 def test_an_index_that_comes_twice(dtype, cols):
     dt, g = DT[dtype], gen(cols)
