@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
 // next row's entries are read behind them.
 //
 // Memory bounds it where several rows share a compute unit: bfloat16 [4096, 50257] (two) 163 us, 5.1 TB/s; in one workgroup of 1024 threads 190, in two sweeps 200.
+// Shorter rows by single wavefronts wait for their entries, which only other rows hide: [8192, 7000] 62 us, 3.7 TB/s; [16384, 1000] 35, 1.9.
 // A row of more than 8192 vectors has a compute unit to itself, which loads nothing from its last vector's arrival to its first gradients: [2048, 131072]
 // 232 us (4.6 TB/s; without any arithmetic 207, without the stores 143), float32 [1280, 50257] 105.  Tried there: the next row's sums begun amid this one's
 // gradients 267 (a wait for a load waits for the stores before it), loads before stores, entries ranked behind the gradients, plain loads or stores: no

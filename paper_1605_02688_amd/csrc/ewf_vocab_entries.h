@@ -11,7 +11,7 @@ namespace {
 
 // The entries of a row in LDS.  An entry inside the row's vectors is in the list of the thread that takes its vector (thread = vector mod N),
 // one on an edge in the list of that edge's thread, with no trip.  K, 64 or 128, is what a row can have: with 64 of them a lane has one, and LDS lets more
-// workgroups share a compute unit (bfloat16 [16384, 1000], 20 entries: 36 us, with room for 128 always 39).
+// workgroups share a compute unit (bfloat16 [16384, 1000], 20 entries: 35 us, with room for 128 always 39).
 template <int N, int K>
 struct Entries {
     int head[N];                                        // last entry of each thread's list, -1
