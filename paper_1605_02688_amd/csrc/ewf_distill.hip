@@ -97,10 +97,12 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(VocabLaunch a)
 //
 // Memory bounds it where several rows share a compute unit: bfloat16 [4096, 50257] (two) 163 us, 5.1 TB/s; in one workgroup of 1024 threads 190, in two sweeps 200.
 // Shorter rows by single wavefronts wait for their entries, which only other rows hide: [8192, 7000] 62 us, 3.7 TB/s; [16384, 1000] 35, 1.9.
-// A row of more than 8192 vectors has a compute unit to itself, which loads nothing from its last vector's arrival to its first gradients: [2048, 131072]
-// 232 us (4.6 TB/s; without any arithmetic 207, without the stores 143), float32 [1280, 50257] 105.  Tried there: the next row's sums begun amid this one's
-// gradients 267 (a wait for a load waits for the stores before it), loads before stores, entries ranked behind the gradients, plain loads or stores: no
-// gain.  Registers hold a row with nothing spilled only if logits are unpacked twice.
+// A row of more than 8192 vectors has a compute unit to itself, and no register is free for the next one from its last vector's arrival to its first
+// gradients; the first half of the next row comes into the cache meanwhile: [2048, 131072] 212 us (5.1 TB/s), without that 232 (without any arithmetic either 207,
+// without the stores 143), with a quarter 222, the whole row 239 (the compute units of one cache have 8 MB of rows, twice what it keeps), from the sums' begin
+// on 220; float32 [1280, 50257] 95 and 105; below 8192 vectors no gain.  Tried there: the next row's sums begun amid this one's gradients 267 (a wait
+// for a load waits for the stores before it), loads before stores, entries ranked behind the gradients, plain loads or stores: no gain.  Registers hold a row with nothing
+// spilled only if logits are unpacked twice.
 template <typename T, int N, int NV, int K, bool STREAM>
 __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch a)
 {
@@ -161,6 +163,9 @@ __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch 
 #pragma unroll
         for (int u = 0; u < NV; u++) asm volatile("" : "+v"(v[u]));
         if (reader) read_logits<T>(entries, a, np);
+        // (one element of each cache line)
+        raw ahead = {};
+        if (N == 1024 && more && tid * 16 < ns.nvec) ahead = *(const raw *)((const char *)(np + ns.head) + tid * 128);
         const float own = a.with_tail && on_edge >= 0 ? -kInf : x;
         add<false, 1>(sum, &own, own, a.c, a.lag);
         sum = wave_sums<false>(sum, a.c);
@@ -214,6 +219,7 @@ __global__ void __launch_bounds__(N, NV > 8 ? 4 : 1) k_distill_held(VocabLaunch 
             if (more) fetch(v[u], np, ns, u);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (N == 1024) asm volatile("" :: "v"((int)*(const uint16_t *)&ahead));
         // the entries' gradients, each by the thread that wrote its vector (and after that: a thread's stores keep their order)
         for (int k = g.rest.as_is ? -1 : l.head[tid]; k >= 0; k = l.next[k])
             if (l.trip[k] >= 0) store1<T>(out + l.index[k], g.entry(l, k));
