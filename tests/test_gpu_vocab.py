@@ -278,8 +278,9 @@ def test_whatever_a_workspace_holds(fill):
 
 
 @pytest.mark.parametrize("dtype", sorted(DT))
-@pytest.mark.parametrize("rows,vectors", ((9001, 50), (9001, 101), (2200, 250), (9001, 251), (5003, 501), (4500, 1019)))
-def test_more_rows_than_wavefronts_hold_at_once(dtype, rows, vectors):
+@pytest.mark.parametrize("rows,vectors", ((9001, 50), (9001, 101), (2200, 250), (9001, 251), (5003, 501), (4500, 1019), (1500, 1500), (1100, 3001), (700, 5000), (600, 7001), (301, 9001),
+                                           (560, 12500)))
+def test_more_rows_than_are_held_at_once(dtype, rows, vectors):
     # each kind of row in turn with the others: masked, padded, huge, not finite, named twice
     dt = DT[dtype]
     cols = vectors * 16 // dt.itemsize + 3
