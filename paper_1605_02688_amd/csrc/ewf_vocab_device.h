@@ -2,8 +2,9 @@
 //
 // With c = scale log2 e a logit x stands for 2^(c x).  A thread adds e = 2^(c x - m), and for the entropy e (c x - m), about a whole number m that lags
 // behind: it moves only where a logit is 2^8 beyond it, so that moves are rare, exact, and e cannot overflow; c x - m is one multiply-add with one
-// rounding.  Threads' sums are moved to a common m and added in a fixed order, and come out about the row's largest logit.  Where c x has no
-// fraction left or leaves float32 (logits beyond 2^22, rows of the type's lowest number) a row is swept again about its largest.
+// rounding.  Threads' sums are moved to a common m and added in a fixed order, and come out about the row's largest logit.  Points lie from -2^22 on:
+// lower, c x has no fraction left and a point made of it is off by more powers of two than e has (masks of -1e10 and the like), and beside a larger logit
+// nothing is left of what lies there.  A row whose largest logit is beyond 2^22 (or leaves float32, as the type's lowest number) is swept again about that.
 #pragma once
 
 #include <algorithm>
@@ -88,9 +89,12 @@ EWF_OPS_DEV RowAt row_at(const Rows &r, uint32_t row)
 }
 EWF_OPS_DEV int64_t at(const RowAt &row, const RowStride &s) { return (int64_t)row.outer * s.outer + (int64_t)row.inner * s.inner; }
 
+// The lowest point.
+constexpr float kLowest = -0x1p22f;
+
 // Sums of a thread: s of the e, w of e times their exponent, about m, which moves for a logit above `limit`; peak is the largest logit.
 struct Sums {
-    float m = -1e38f, limit = -kInf, s = 0.f, w = 0.f, peak = -kInf;
+    float m = kLowest, limit = -kInf, s = 0.f, w = 0.f, peak = -kInf;
 };
 
 // Moves the point from `from` to `to` powers of two, upwards (sums of nothing move anywhere).  The product is rounded here and not contracted into the
@@ -150,8 +154,8 @@ EWF_OPS_DEV float max_of(const float *x)
     return V % 2 ? m : max3(m, x[V - 1], x[V - 1]);
 }
 
-// A whole number of powers of two near a largest logit: what sums of a wavefront are brought to.
-EWF_OPS_DEV float point_of(float peak, float c) { return peak == -kInf ? 0.f : rintf(peak * c); }
+// A whole number of powers of two near a largest logit: what sums of a wavefront are brought to (threads' points are no further up).
+EWF_OPS_DEV float point_of(float peak, float c) { return fmaxf(rintf(peak * c), kLowest); }
 // Whether a row whose largest logit this is cannot be summed about such a point: whole numbers and c x have to keep their fractions.
 EWF_OPS_DEV bool beyond(float peak, float c) { return fabsf(peak) < kInf && !(fabsf(peak * c) < 0x1p22f); }
 
