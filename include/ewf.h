@@ -384,7 +384,7 @@ ewf_status ewf_recurrence_grad(const ewf_recurrence_args *a, void *workspace, si
  * row whose token is outside 0 .. cols - 1 is padding: what its logits hold has no effect, its results are 0, and it has no alternatives.
  * Alternatives that do not exist (logits of minus infinity, k > cols) have index -1 and value minus infinity.  In a row without any logit above
  * minus infinity peak, logsum and logprob are minus infinity and entropy is 0.  A row that holds a NaN or plus infinity has NaN in all its
- * results, and indices -1.  The lowest finite number is a logit like others.
+ * results, and indices -1.  Finite numbers are logits like others, masks of -1e30 and the lowest number among them.
  *
  * ewf_token_logprobs_grad: with g = dlogprob and h = dentropy (float32, one of them at least; dlogprob comes with tokens, dentropy with
  * entropy)
@@ -404,7 +404,8 @@ ewf_status ewf_token_logprobs_grad(const ewf_token_logprobs_args *a, void *hip_s
 
 /* The loss of rows of a student's logits (as above) against a teacher's entries: teacher_indices (int32 [..., k], k = 1 .. 128)
  * and teacher_values ([..., k], teacher_dtype: dtype or EWF_F32).  An entry whose index is outside 0 .. cols - 1 does not exist, whatever its
- * value; an index that comes twice counts with both its probabilities.  log p as above.
+ * value; an index that comes twice counts with both its probabilities.  log p as above (minus infinity, and a loss with q > 0 infinite, where
+ * it leaves float32).
  * Without `tail`, q = softmax(teacher_scale teacher_values) over the entries that exist, and
  *     loss = sum_i q_i (log q_i - log p_(index i)),   dlogits_j = dloss scale (p_j - sum of the q_i with index j).
  * With `tail` the values are log probabilities (as ewf_token_logprobs writes top_values), q_i = exp(teacher_scale value_i), and the rest of the

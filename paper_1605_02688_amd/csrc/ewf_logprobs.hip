@@ -129,6 +129,9 @@ static int held_workgroups(int threads, int n, int entries)
 void plan_vocab(VocabLaunch &a, int units)
 {
     const int n = vectors(a);
+    // however few the rows are: losses first and gradients behind them, which parts of rows may share, take longer (20 entries and a tail, one row of 8192 vectors 14.0 us held
+    // and 18.9 apart in bfloat16, 10.8 and 16.3 in float32; 32 rows of 12288 17.2 and 19.3, 13.8 and 18.2; 128 of 16384 21.0 and 30.6, 17.3 and 28.5), but for up to 32 rows of
+    // 16384 vectors of 16 bits (19 to 20 and 16 to 19)
     a.held = a.entries && a.dlogits && a.loss && n <= kHeldVectors;
     // a wavefront a row where there are wavefronts for all compute units, bfloat16: [16384, 2048] 19.4 us, on 256 threads 40.9; [16384, 4096] 31.7 and 52.7;
     // [8192, 12000] 39.2 and 43.7; but [4096, 32768] 50.5 and 45.8, [600, 16000] 9.4 and 8.2.  Alternatives of rows above 256 vectors need the 256 threads' pieces.

@@ -80,7 +80,7 @@ struct VocabLaunch {
     int resident;                        // workgroups of launch_token_logprobs and launch_distill, which take rows in turn
     int threads, splits, held, stream;   // a row's workgroup, its workgroups; whether its logits are held in registers; whether they pass caches by
     float *parts;                        // [rows][splits][4]: peak, sums; null where rows are finished by the workgroup that sums them
-float *pieces;                       // [rows][splits][pieces_per_part]: the largest logits of a part's pieces
+    float *pieces;                       // [rows][splits][pieces_per_part]: the largest logits of a part's pieces
     int pieces_per_part;
     void *prepared;                      // a loss whose gradient is a launch of its own: what that needs of each row, prepared_bytes
 };
@@ -94,7 +94,7 @@ void launch_activation(const ActLaunch &a, ihipStream_t *stream);
 void launch_activation_grad(const ActLaunch &a, ihipStream_t *stream);
 void launch_read8(const ActLaunch &a, ihipStream_t *stream);
 constexpr size_t kPreparedBytes = 32, kPreparedEntryBytes = 8;
-// Chooses the workgroups of launch_token_logprobs and launch_distill: fills threads, splits and held.
+// Chooses the workgroups of launch_token_logprobs and launch_distill: fills held, threads, splits, pieces_per_part, resident and stream.
 void plan_vocab(VocabLaunch &a, int units);
 void launch_token_logprobs(const VocabLaunch &a, ihipStream_t *stream);
 void launch_token_logprobs_grad(const VocabLaunch &a, ihipStream_t *stream);
